@@ -1,0 +1,330 @@
+"""What is timed of the student's operators: the calls that training and serving a student network make.
+
+A student learns from an ensemble's class probabilities (``distill_topk``), is built of pre-normalised gated blocks
+(``add_rms_norm``, ``gated_ff`` and their gradients) and answers in 8 bits (``add_rms_norm_q8``, ``quantize_rows``,
+``q8_matmul``).  Where ``own`` is false ``run`` computes the same in elementary torch operations in 32 bits.
+"""
+import math
+
+import torch
+
+own = False
+
+DEV = "cuda"
+EPS = 1e-6
+DTYPES = {"bf16": torch.bfloat16, "fp32": torch.float32}
+
+
+def listed():
+    return [
+        # one row answered: the norm in front of an 8-bit product, where the launch is what counts
+        dict(name="norm_q8_row", op="norm_q8", T=1, D=1024, dtype="bf16"),
+        # the norm's gradients in a training step over a whole epoch's slice of rows
+        dict(name="norm_backward", op="norm_bwd", T=65_536, D=1024, dtype="bf16"),
+        # weights laid out once when a student is loaded
+        dict(name="quantize_weights", op="quantize", T=4096, D=1024, dtype="fp32"),
+        # hidden values of the validation rows between the two 8-bit products
+        dict(name="quantize_hidden", op="quantize", T=20_000, D=2048, dtype="bf16"),
+        # one row through the gate and up projections in 8 bits
+        dict(name="q8_row", op="q8", M=1, K=1024, N=4096, gate="silu", bias=False, dtype="bf16"),
+        # a batch through the down projection, biased as the members' layers are
+        dict(name="q8_batch", op="q8", M=2048, K=2048, N=1024, gate="", bias=True, dtype="bf16"),
+        # all validation rows through the gated projections, an odd number of them
+        dict(name="q8_rows", op="q8", M=20_011, K=1024, N=4096, gate="silu", bias=False, dtype="bf16"),
+        # one row through a block in bf16: the weights' bytes count
+        dict(name="ff_row", op="ff_fwd", T=1, D=1024, F=4096, act="silu", residual=True, dtype="bf16"),
+        # a small table's block in fp32, sizes that are no multiple of anything
+        dict(name="ff_ragged_fp32", op="ff_train", T=300, D=37, F=301, act="gelu", residual=True, dtype="fp32"),
+        # a training step of a wide block: forward and all gradients
+        dict(name="ff_train", op="ff_train", T=16_384, D=1024, F=4096, act="silu", residual=True, dtype="bf16"),
+        # a batch against the ensemble's most likely classes of a ten-class table
+        dict(name="distill_classes", op="distill", T=1024, V=10, k=4, tau=2.0, dtype="fp32"),
+        # a teacher over a large set of classes, of which its top 32 are kept
+        dict(name="distill_wide", op="distill", T=4096, V=32_000, k=32, tau=1.5, dtype="bf16"),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _width(rng, lo, hi):
+    """A width: as often a multiple of 64 as any number at all."""
+    w = _log(rng, lo, hi)
+    return max(64, (w + 32) // 64 * 64) if rng.random() < 0.5 else w
+
+
+def draw(rng):
+    op = rng.choice(["norm_q8", "norm_fwd", "norm_bwd", "quantize", "q8", "q8", "ff_fwd", "ff_train", "distill"])
+    dtype = "fp32" if rng.random() < 0.25 else "bf16"
+    if op in ("norm_q8", "norm_fwd", "norm_bwd", "quantize"):
+        c = dict(op=op, T=_log(rng, 1, 65_536), D=_width(rng, 8, 8192), dtype=dtype)
+        c["T"] = max(1, min(c["T"], (1 << 26) // c["D"] // (2 if dtype == "fp32" else 1)))
+        return c
+    if op == "q8":
+        c = dict(op=op, M=_log(rng, 1, 20_011), K=_width(rng, 8, 4096), N=_width(rng, 8, 4096),
+                 gate=rng.choice(["", "", "silu", "gelu"]), bias=rng.random() < 0.5, dtype=dtype)
+        c["M"] = max(1, min(c["M"], int(1.6e11 // (2 * c["K"] * c["N"] * (2 if c["gate"] else 1)))))
+        return c
+    if op == "distill":
+        c = dict(op=op, T=_log(rng, 1, 16_384), V=_log(rng, 2, 64_000), tau=round(rng.uniform(0.5, 4.0), 2),
+                 dtype=dtype)
+        c["T"] = max(1, min(c["T"], (1 << 27) // c["V"] // (2 if dtype == "fp32" else 1)))
+        c["k"] = rng.randint(1, min(64, c["V"]))
+        return c
+    c = dict(op=op, T=_log(rng, 1, 16_384), D=_width(rng, 16, 2048), F=_width(rng, 16, 4096),
+             act=rng.choice(["silu", "gelu", "relu"]), residual=rng.random() < 0.7, dtype=dtype)
+    c["T"] = max(1, min(c["T"], int((1.5e11 if dtype == "fp32" else 1.2e12) // (18 * c["D"] * c["F"]))))
+    return c
+
+
+# ------------------------------------------------------------------ inputs
+def _generator(seed):
+    return torch.Generator(device=DEV).manual_seed((0x9E3779B97F4A7C15 * (int(seed) + 1)) % (1 << 62))
+
+
+def _normal(g, *shape, std=1.0):
+    return torch.randn(*shape, generator=g, device=DEV) * std
+
+
+def _bytes(case):
+    return 4 if case["dtype"] == "fp32" else 2
+
+
+def prepare(case, seed):
+    g = _generator(seed)
+    op, dt = case["op"], DTYPES[case["dtype"]]
+    s = dict(case=case)
+    if op in ("norm_q8", "norm_fwd"):
+        # a residual stream with a few loud channels, the branch added to it, a trained weight
+        T, D = case["T"], case["D"]
+        loud = 1 + 8 * (torch.rand(D, generator=g, device=DEV) < 0.01)
+        s.update(x=_normal(g, T, D, std=0.5).to(dt), r=(_normal(g, T, D) * loud).to(dt),
+                 w=1 + _normal(g, D, std=0.1))
+    elif op == "norm_bwd":
+        T, D = case["T"], case["D"]
+        x = _normal(g, T, D).to(dt)
+        s.update(s=x, w=1 + _normal(g, D, std=0.1), dy=_normal(g, T, D, std=1e-2).to(dt),
+                 ds=_normal(g, T, D, std=1e-2).to(dt), rstd=(x.float().square().mean(1) + EPS).rsqrt())
+    elif op == "quantize":
+        x = _normal(g, case["T"], case["D"])
+        x[:: 97] *= 30  # rows of another size
+        s.update(x=x.to(dt))
+    elif op == "q8":
+        M, K, N = case["M"], case["K"], case["N"] * (2 if case["gate"] else 1)
+        s.update(x=torch.clamp(_normal(g, M, K, std=32).round(), -127, 127).to(torch.int8),
+                 xs=torch.rand(M, generator=g, device=DEV) * 0.02 + 0.01,
+                 w=torch.clamp(_normal(g, N, K, std=36).round(), -127, 127).to(torch.int8),
+                 ws=(torch.rand(N, generator=g, device=DEV) + 0.5) / (36 * math.sqrt(K)),
+                 b=_normal(g, N, std=0.1) if case["bias"] else None)
+    elif op in ("ff_fwd", "ff_train"):
+        T, D, F = case["T"], case["D"], case["F"]
+        s.update(x=_normal(g, T, D).to(dt), wgu=_normal(g, 2 * F, D, std=D ** -0.5).to(dt),
+                 wd=_normal(g, D, F, std=F ** -0.5).to(dt), r=_normal(g, T, D).to(dt) if case["residual"] else None)
+        if op == "ff_train":
+            s["dy"] = _normal(g, T, D, std=1e-2).to(dt)
+    else:
+        # a student's logits; a teacher's top classes of a distribution like the student's, some rows with
+        # fewer than k classes (-1), padding rows of weight 0
+        T, V, k = case["T"], case["V"], case["k"]
+        z = _normal(g, T, V, std=2.0)
+        teacher, idx = (z + _normal(g, T, V)).topk(k, 1)
+        gone = torch.rand(T, k, generator=g, device=DEV) < 0.05
+        weight = torch.full((T,), 1.0 / T, device=DEV)
+        weight[torch.rand(T, generator=g, device=DEV) < 0.1] = 0.0
+        s.update(z=z.to(dt), t=teacher.contiguous(), idx=torch.where(gone, -1, idx).to(torch.int32), weight=weight)
+    return s
+
+
+# --------------------------------------------------------------- plain form
+def _act(a, g):
+    if a == "silu":
+        return g / (1 + torch.exp(-g))
+    if a == "gelu":
+        return 0.5 * g * (1 + torch.erf(g * math.sqrt(0.5)))
+    return torch.clamp(g, min=0)
+
+
+def _act_grad(a, g):
+    if a == "silu":
+        p = 1 / (1 + torch.exp(-g))
+        return p * (1 + g * (1 - p))
+    if a == "gelu":
+        return 0.5 * (1 + torch.erf(g * math.sqrt(0.5))) + g * torch.exp(-0.5 * g * g) * (0.5 / math.pi) ** 0.5
+    return (g > 0).to(g.dtype)
+
+
+def _codes(t):
+    """t in 8 bits by rows: whole numbers and the row's largest magnitude."""
+    a = t.abs().amax(1, keepdim=True)
+    inv = torch.where(a > 0, torch.div(torch.full_like(a, 127.0), a), torch.zeros_like(a))
+    return torch.round(t * inv), a
+
+
+def _plain(case, s):
+    op, dt = case["op"], DTYPES[case["dtype"]]
+    if op in ("norm_q8", "norm_fwd"):
+        x = s["x"].float() + s["r"].float()
+        rho = 1 / torch.sqrt(x.square().mean(1, keepdim=True) + EPS)
+        if op == "norm_fwd":
+            return dict(sum=x.to(dt), out=(x * rho * s["w"]).to(dt), rstd=rho[:, 0])
+        q, a = _codes(x * s["w"])
+        return dict(sum=x.to(dt), value=q * (a * rho / 127))
+    if op == "norm_bwd":
+        x, dy, rho = s["s"].float(), s["dy"].float(), s["rstd"][:, None]
+        g = dy * s["w"]
+        dx = rho * (g - x * (rho * rho * (g * x).mean(1, keepdim=True))) + s["ds"].float()
+        return dict(dx=dx.to(dt), dw=(dy * x * rho).sum(0))
+    if op == "quantize":
+        q, a = _codes(s["x"].float())
+        return q * (a / 127)
+    if op == "q8":
+        out = (s["x"].float() @ s["w"].float().t()) * (s["xs"][:, None] * s["ws"])
+        if s["b"] is not None:
+            out = out + s["b"]
+        if case["gate"]:
+            out = _act(case["gate"], out[:, :case["N"]]) * out[:, case["N"]:]
+        return out.to(dt)
+    if op in ("ff_fwd", "ff_train"):
+        F, x, wgu, wd = case["F"], s["x"].float(), s["wgu"].float(), s["wd"].float()
+        gu = x @ wgu.t()
+        g, u = gu[:, :F], gu[:, F:]
+        h = _act(case["act"], g) * u
+        y = h @ wd.t()
+        if s["r"] is not None:
+            y = y + s["r"].float()
+        if op == "ff_fwd":
+            return y.to(dt)
+        dy = s["dy"].float()
+        dh = dy @ wd
+        dgu = torch.cat([dh * u * _act_grad(case["act"], g), dh * _act(case["act"], g)], 1)
+        return dict(y=y.to(dt), dx=(dgu @ wgu).to(dt), dwgu=(dgu.t() @ x).to(dt), dwd=(dy.t() @ h).to(dt))
+    tau, weight, there = case["tau"], s["weight"][:, None], s["idx"] >= 0
+    z = s["z"].float() / tau
+    e = torch.exp(z - z.amax(1, keepdim=True))
+    total = e.sum(1, keepdim=True)
+    lse = z.amax(1, keepdim=True) + torch.log(total)
+    t = torch.where(there, s["t"] / tau, -math.inf)
+    top = t.amax(1, keepdim=True)
+    top = torch.where(top > -math.inf, top, torch.zeros_like(top))
+    p = torch.exp(t - top)
+    norm = p.sum(1, keepdim=True)
+    some = norm > 0
+    norm = torch.where(some, norm, torch.ones_like(norm))
+    p = p / norm
+    at = s["idx"].clamp(min=0).long()
+    gap = torch.where(there, (t - top - torch.log(norm)) - (z.gather(1, at) - lse), torch.zeros_like(p))
+    loss = (weight * tau * tau * (p * gap).sum(1, keepdim=True))[:, 0]
+    grad = torch.where(some, e / total, torch.zeros_like(e)).scatter_add(1, at, -p) * (weight * tau)
+    return dict(loss=loss, grad=grad.to(dt))
+
+
+# -------------------------------------------------------- the framework's own
+def _own(case, s):
+    from paper_2607_05380_amd import ops
+    op, dt = case["op"], DTYPES[case["dtype"]]
+    if op == "norm_fwd":
+        out, total, rstd = ops.add_rms_norm(s["x"], s["w"], residual=s["r"], eps=EPS)
+        return dict(sum=total, out=out, rstd=rstd)
+    if op == "norm_q8":
+        q, scale, total = ops.add_rms_norm_q8(s["x"], s["w"], residual=s["r"], eps=EPS)
+        return dict(sum=total, value=q * scale[:, None])
+    if op == "norm_bwd":
+        dx, dw = ops.rms_norm_backward(s["dy"], s["s"], s["w"], s["rstd"], ds=s["ds"])
+        return dict(dx=dx, dw=dw)
+    if op == "quantize":
+        q, scale = ops.quantize_rows(s["x"])
+        return q * scale[:, None]
+    if op == "q8":
+        return ops.q8_matmul(s["x"], s["xs"], s["w"], s["ws"], bias=s["b"], gate=case["gate"] or None, dtype=dt)
+    if op == "ff_fwd":
+        return ops.gated_ff(s["x"], s["wgu"], s["wd"], act=case["act"], residual=s["r"])
+    if op == "ff_train":
+        y, saved = ops.gated_ff(s["x"], s["wgu"], s["wd"], act=case["act"], residual=s["r"], save=True)
+        dx, dwgu, dwd = ops.gated_ff_backward(s["dy"], s["x"], s["wgu"], s["wd"], saved, act=case["act"])
+        return dict(y=y, dx=dx, dwgu=dwgu, dwd=dwd)
+    loss, grad = ops.distill_topk(s["z"], s["idx"], s["t"], temperature=case["tau"], row_weight=s["weight"])
+    return dict(loss=loss, grad=grad)
+
+
+def run(state):
+    return (_own if own else _plain)(state["case"], state)
+
+
+# ------------------------------------------------------------------ in 64 bits
+def exact(case, seed):
+    """The operators' definitions in 64 bits, gradients by differentiating them where that is the shorter way."""
+    s = {k: v.double() if torch.is_tensor(v) and v.is_floating_point() else v for k, v in prepare(case, seed).items()}
+    op = case["op"]
+
+    def act(v):
+        return {"silu": lambda: v * torch.sigmoid(v), "gelu": lambda: torch.nn.functional.gelu(v),
+                "relu": lambda: v.relu()}[case.get("gate") or case["act"]]()
+
+    def eight(v):
+        scale = v.abs().max(1, keepdim=True).values / 127
+        return torch.where(scale > 0, (v / scale).round(), 0.0) * scale
+
+    if op in ("norm_q8", "norm_fwd"):
+        total = s["x"] + s["r"]
+        rstd = (total.pow(2).mean(-1, keepdim=True) + EPS).pow(-0.5)
+        if op == "norm_q8":
+            return dict(sum=total, value=eight(total * rstd * s["w"]))
+        return dict(sum=total, out=total * rstd * s["w"], rstd=rstd[:, 0])
+    if op == "norm_bwd":
+        # dL/ds of s rho(s) w with rho as given: the derivative of rho is -rho^3 s / D
+        x, rho = s["s"], s["rstd"].unsqueeze(1)
+        inner = (s["dy"] * s["w"] * x).sum(1, keepdim=True)
+        return dict(dx=s["ds"] + rho * s["w"] * s["dy"] - rho ** 3 / case["D"] * inner * x,
+                    dw=torch.einsum("td,td,to->d", s["dy"], x, rho))
+    if op == "quantize":
+        return eight(s["x"])
+    if op == "q8":
+        out = torch.mm(s["x"].double(), s["w"].double().t()) * s["xs"].unsqueeze(1) * s["ws"].unsqueeze(0)
+        out = out if s["b"] is None else out + s["b"]
+        return act(out[:, :case["N"]]) * out[:, case["N"]:] if case["gate"] else out
+    if op in ("ff_fwd", "ff_train"):
+        x, wgu, wd = (s[k].requires_grad_(op == "ff_train") for k in ("x", "wgu", "wd"))
+        gate, up = torch.mm(x, wgu.t()).split(case["F"], 1)
+        y = torch.mm(act(gate) * up, wd.t())
+        y = y if s["r"] is None else y + s["r"]
+        if op == "ff_fwd":
+            return y
+        dx, dwgu, dwd = torch.autograd.grad(y, (x, wgu, wd), s["dy"])
+        return dict(y=y.detach(), dx=dx, dwgu=dwgu, dwd=dwd)
+    tau, there = case["tau"], s["idx"] >= 0
+    logq = torch.log_softmax(s["z"] / tau, 1)
+    rows = there.any(1, keepdim=True)
+    logp = torch.log_softmax(torch.where(there | ~rows, s["t"] / tau, -torch.inf), 1)
+    p = torch.where(there, logp.exp(), 0.0)
+    at = s["idx"].clamp(min=0).long()
+    loss = tau ** 2 * torch.where(there, p * (logp - logq.gather(1, at)), 0.0).sum(1) * s["weight"]
+    target = torch.zeros_like(logq).scatter_add(1, at, p)
+    return dict(loss=loss, grad=torch.where(rows, logq.exp() - target, 0.0) * tau * s["weight"].unsqueeze(1))
+
+
+# ------------------------------------------------------------------------ work
+def work(case):
+    """Every input read once and every output written once; the operations of the definition."""
+    op, e = case["op"], _bytes(case)
+    if op in ("norm_q8", "norm_fwd"):
+        T, D = case["T"], case["D"]
+        return dict(bytes=T * D * (3 * e + (1 if op == "norm_q8" else e)) + 4 * D + 4 * T, flops=8 * T * D)
+    if op == "norm_bwd":
+        T, D = case["T"], case["D"]
+        return dict(bytes=T * D * 4 * e + 8 * D + 4 * T, flops=12 * T * D)
+    if op == "quantize":
+        T, D = case["T"], case["D"]
+        return dict(bytes=T * D * (e + 1) + 4 * T, flops=3 * T * D)
+    if op == "q8":
+        M, K, N, w = case["M"], case["K"], case["N"], 2 if case["gate"] else 1
+        return dict(bytes=M * K + w * N * K + e * M * N + 4 * M + 4 * w * N * (2 if case["bias"] else 1),
+                    flops=2 * w * M * N * K)
+    if op in ("ff_fwd", "ff_train"):
+        T, D, F = case["T"], case["D"], case["F"]
+        fwd = e * (2 * T * D + 3 * D * F + (T * D if case["residual"] else 0))
+        if op == "ff_fwd":
+            return dict(bytes=fwd, flops=6 * T * D * F)
+        return dict(bytes=fwd + e * (2 * T * D + 3 * D * F), flops=18 * T * D * F)
+    T, V, k = case["T"], case["V"], case["k"]
+    return dict(bytes=T * V * 2 * e + T * k * 8 + 8 * T, flops=6 * T * V)
