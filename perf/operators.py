@@ -230,7 +230,7 @@ def _own(case, s):
         q, scale, total = ops.add_rms_norm_q8(s["x"], s["w"], residual=s["r"], eps=EPS)
         return dict(sum=total, value=q * scale[:, None])
     if op == "norm_bwd":
-        dx, dw = ops.rms_norm_backward(s["dy"], s["s"], s["w"], s["rstd"], ds=s["ds"])
+        dx, dw = ops.rms_norm_backward(s["dy"], s["s"], s["w"], s["rstd"], dv=s["ds"])
         return dict(dx=dx, dw=dw)
     if op == "quantize":
         q, scale = ops.quantize_rows(s["x"])
