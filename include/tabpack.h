@@ -359,6 +359,85 @@ typedef struct pack_kernel_stat {
 int pack_profile_enable(pack_handle* h, int32_t enable);
 int pack_profile_read(pack_handle* h, pack_kernel_stat* out, int32_t max, int32_t* n);
 
+/* ---------------------------------------------------------------------------
+ * Operators of a student network.  An ensemble of up to 32 members answers
+ * with up to 32 forward passes; these calls train one network on the
+ * ensemble's class probabilities (pack_distill_topk), built of pre-normalised
+ * gated blocks (pack_add_rms_norm, pack_gated_ff_*), and serve it in 8 bits
+ * (pack_add_rms_norm_q8, pack_quantize_rows, pack_q8_matmul).  They need no
+ * handle, keep nothing between calls and allocate nothing.
+ *
+ * Matrices are row-major with a leading dimension (elements from one row to
+ * the next) of at least the row's length; elements of a row are contiguous.
+ * Any alignment of the element type is accepted; where every row starts at a
+ * multiple of 16 bytes and its length is one too, 16-byte accesses are used.
+ * precision is that of the matrices (PACK_PREC_BF16 or PACK_PREC_FP32); sums
+ * are held in fp32 (8-bit products in int32).  Outputs must not overlap inputs
+ * unless a call allows it.  Sizes of 0 rows are accepted and do nothing more
+ * than the outputs of that size need.  Results do not change between runs. */
+
+/* y = v rho w with v = x + residual, rho = (mean_c v^2 + eps)^(-1/2) per row.
+ *   x, residual  device [rows, cols]; residual NULL: v = x
+ *   weight       device fp32 [cols]
+ *   sum_out      device [rows, cols]: v rounded to the precision (the norm
+ *                takes it unrounded), or NULL; may be x or residual itself
+ *   out          device [rows, cols]
+ *   rstd_out     device fp32 [rows]: rho, for the backward pass, or NULL
+ * cols <= PACK_ROW_MAX_COLS, eps >= 0. */
+#define PACK_ROW_MAX_COLS 32768
+int pack_add_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, const float* weight,
+                      int32_t precision, int64_t rows, int32_t cols, float eps, void* sum_out, int64_t lds,
+                      void* out, int64_t ldo, float* rstd_out, hipStream_t stream);
+
+/* The same with y in 8 bits: q[r, c] = rint(v w 127 / max_c|v w|) and
+ * scale[r] = max_c|v w| rho / 127, so that y is q scale.  Ties go to the even
+ * code.  A row whose largest magnitude is 0 (or below 127 / FLT_MAX) has codes
+ * 0 and scale 0; a row that holds an infinity or NaN has codes 0 and scale NaN. */
+int pack_add_rms_norm_q8(const void* x, int64_t ldx, const void* residual, int64_t ldr, const float* weight,
+                         int32_t precision, int64_t rows, int32_t cols, float eps, void* sum_out, int64_t lds,
+                         int8_t* q_out, int64_t ldq, float* scale_out, hipStream_t stream);
+
+/* Rows in 8 bits: q = rint(x 127 / max_c|x|), scale = max_c|x| / 127, with the
+ * rules above (activations: a scale per row; a weight [N, K]: per output). */
+int pack_quantize_rows(const void* x, int64_t ldx, int32_t precision, int64_t rows, int32_t cols, int8_t* q_out,
+                       int64_t ldq, float* scale_out, hipStream_t stream);
+
+/* Gradients of pack_add_rms_norm from its sum v (as it was stored) and rho:
+ * with g = weight dy,
+ *   dx = rho (g - v rho^2 / cols sum_c g v) + dsum   (of x and of the residual)
+ *   dweight = sum over the rows of dy v rho
+ *   dsum     the gradient that reaches v on its other path, or NULL
+ *   dx_out   device [rows, cols]; may be dy or dsum itself
+ *   dweight_out  device fp32 [cols]
+ *   work     device scratch of pack_rms_norm_backward_workspace_size() bytes, 4-byte aligned */
+int pack_rms_norm_backward_workspace_size(int64_t rows, int32_t cols, size_t* bytes);
+int pack_rms_norm_backward(const void* dy, int64_t ldy, const void* sum, int64_t lds, const float* weight,
+                           const float* rstd, const void* dsum, int64_t ldd, int32_t precision, int64_t rows,
+                           int32_t cols, void* dx_out, int64_t ldx, float* dweight_out, void* work,
+                           size_t work_bytes, hipStream_t stream);
+
+/* Distillation from a teacher's top logits.  Row r has k teacher entries
+ * (class idx[r, j], logit teacher[r, j]); with temperature tau, p = softmax of
+ * the row's teacher logits / tau over its entries and q = softmax(logits / tau)
+ * over all classes,
+ *   loss_out[r] = w_r tau^2 sum_j p_j (log p_j - log q_idx_j)
+ *   grad_out[r, c] = d loss_out[r] / d logits[r, c] = w_r tau (q_c - sum over the entries of class c of p_j)
+ *   logits     device [rows, classes]
+ *   idx        device int32 [rows, k]; an entry with a negative index or a
+ *              logit of -inf is left out, several entries may name one class
+ *   teacher    device fp32 [rows, k]
+ *   row_weight device fp32 [rows] or NULL (1): the derivative of the caller's
+ *              total with respect to the row's loss, e.g. 1 / rows
+ *   loss_out   device fp32 [rows]; grad_out device [rows, classes] or NULL
+ * A row of weight 0 and a row without entries have loss and gradient 0,
+ * whatever else they hold.  An index >= classes, a NaN teacher logit or a NaN
+ * logit makes the row's loss and gradient NaN.  1 <= k <=
+ * PACK_DISTILL_MAX_K, temperature > 0. */
+#define PACK_DISTILL_MAX_K 256
+int pack_distill_topk(const void* logits, int64_t ldz, int32_t precision, int64_t rows, int32_t classes,
+                      const int32_t* idx, const float* teacher, int32_t k, float temperature,
+                      const float* row_weight, float* loss_out, void* grad_out, int64_t ldg, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

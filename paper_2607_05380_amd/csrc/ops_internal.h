@@ -1,0 +1,62 @@
+// Launch interface between the host entry points of the student's operators
+// (ops.cpp) and their kernels (kernels_rows.hip, kernels_block.hip).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace tabpack {
+
+int set_error(int code, const char* msg);
+
+constexpr int kRowMaxCols = 32768;   // widest row that the row kernels hold in registers
+constexpr int kDistillMaxK = 256;    // teacher entries per row
+
+// One pass over rows: v = x (+ residual); NORM: y = v rho w; QUANT: 8-bit codes
+// and a scale per row of v or y.
+struct RowArgs {
+  const void* x;
+  const void* residual;   // or NULL
+  const float* weight;    // [cols] (norm)
+  void* sum;              // or NULL: v in the input type
+  void* out;              // y in the input type (norm without codes)
+  int8_t* q;              // codes
+  float* scale;           // [rows]
+  float* rstd;            // [rows] or NULL: rho
+  int64_t rows, ldx, ldr, lds, ldo;
+  int32_t cols;
+  float eps;
+  int32_t vec;            // 1: every row starts at 16 bytes and cols is a multiple of the 16-byte vector
+};
+enum RowMode { ROW_NORM = 0, ROW_NORM_Q8 = 1, ROW_Q8 = 2 };
+hipError_t launch_rows(int prec, RowMode mode, const RowArgs& a, hipStream_t s);
+
+struct NormBwdArgs {
+  const void* sum;
+  const void* dy;
+  const void* dsum;       // or NULL
+  const float* weight;
+  const float* rstd;
+  void* dx;
+  float* dweight;         // [cols]
+  float* partial;         // [norm_bwd_blocks(rows, cols), cols]
+  int64_t rows, lds, ldy, ldd, ldx;
+  int32_t cols, vec;
+};
+int norm_bwd_blocks(int64_t rows, int32_t cols);
+hipError_t launch_norm_bwd(int prec, const NormBwdArgs& a, hipStream_t s);
+
+struct DistillArgs {
+  const void* logits;
+  const int32_t* idx;     // [rows, k]
+  const float* teacher;   // [rows, k]
+  const float* weight;    // [rows] or NULL: 1
+  float* loss;            // [rows]
+  void* grad;             // or NULL
+  int64_t rows, ldz, ldg;
+  int32_t classes, k;
+  float tau;
+  int32_t vec;
+};
+hipError_t launch_distill(int prec, const DistillArgs& a, hipStream_t s);
+
+}  // namespace tabpack

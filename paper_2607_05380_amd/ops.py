@@ -1,0 +1,160 @@
+"""Operators of a student network: binding of the handle-free calls of libtabpack.so.
+
+An ensemble answers with a forward pass of each of its members; a student is one network trained on the ensemble's
+class probabilities and served in 8 bits.  Its parts:
+
+  distill_topk                        the loss against a teacher's top logits and its gradient
+  add_rms_norm, rms_norm_backward     root-mean-square norm of x + residual, and its gradients
+  add_rms_norm_q8, quantize_rows      the norm, or plain rows, as 8-bit codes with a scale per row
+
+Matrices are 2-D device tensors in bfloat16 or float32 whose rows are contiguous (any row stride and alignment).
+Every call runs HIP kernels on the current stream of the tensors' device; ``PackError`` says what an argument
+breaks.  Formulas and rules for empty, masked and non-finite rows are in ``include/tabpack.h``.
+"""
+import torch
+
+from . import tabpack
+from .tabpack import PackError
+
+_PREC = {torch.bfloat16: 0, torch.float32: 1}
+
+
+def _fail(msg):
+    raise PackError(msg)
+
+
+def _matrix(t, name, dtype=None, shape=None):
+    """Checks a 2-D device tensor with contiguous rows; its (address, row stride)."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2):
+        _fail(f"{name} must be a 2-D device tensor")
+    if dtype is not None and t.dtype != dtype:
+        _fail(f"{name} must be {dtype}, not {t.dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        _fail(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+    cols, (ld, inner) = t.shape[1], t.stride()
+    if inner != 1 and cols > 1:
+        _fail(f"{name} must have contiguous rows")
+    if t.shape[0] <= 1:
+        ld = max(ld, cols)
+    if ld < cols:
+        _fail(f"{name} must not have overlapping rows")
+    return t.data_ptr(), ld
+
+
+def _vector(t, name, n, dtype=torch.float32):
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and tuple(t.shape) == (n,)
+            and t.is_contiguous()):
+        _fail(f"{name} must be a contiguous device tensor of {n} {dtype}")
+    return t.data_ptr()
+
+
+def _prec(t, name):
+    if not isinstance(t, torch.Tensor) or t.dtype not in _PREC:
+        _fail(f"{name} must be a bfloat16 or float32 tensor")
+    return _PREC[t.dtype]
+
+
+def _call(fn, *args, like, others=()):
+    """The library call on the current stream of like's device."""
+    for t in others:
+        if t is not None and t.device != like.device:
+            _fail("all tensors must be on one device")
+    lib = tabpack.load_library()
+    dev = like.device.index
+    if dev == torch.cuda.current_device():
+        tabpack._check(getattr(lib, fn)(*args, torch.cuda.current_stream(dev).cuda_stream))
+    else:
+        with torch.cuda.device(dev):
+            tabpack._check(getattr(lib, fn)(*args, torch.cuda.current_stream(dev).cuda_stream))
+
+
+def _bytes(fn, *args):
+    import ctypes
+    n = ctypes.c_size_t()
+    tabpack._check(getattr(tabpack.load_library(), fn)(*args, ctypes.byref(n)))
+    return n.value
+
+
+def _empty(like, *shape, dtype=None):
+    return torch.empty(shape, dtype=dtype or like.dtype, device=like.device)
+
+
+def _norm_inputs(x, weight, residual):
+    prec = _prec(x, "x")
+    xp, ldx = _matrix(x, "x")
+    rows, cols = x.shape
+    rp, ldr = (None, 0) if residual is None else _matrix(residual, "residual", x.dtype, x.shape)
+    return (xp, ldx, rp, ldr, _vector(weight, "weight", cols), prec, rows, cols)
+
+
+def add_rms_norm(x, weight, residual=None, eps=1e-6):
+    """(y, v, rstd): v = x + residual (x itself without one), rstd = (mean v^2 + eps)^(-1/2) per row, y = v rstd weight.
+    x, residual [rows, cols], weight fp32 [cols]; y and v in x's type, rstd fp32 [rows]."""
+    a = _norm_inputs(x, weight, residual)
+    v = x if residual is None else _empty(x, *x.shape)
+    y, rstd = _empty(x, *x.shape), _empty(x, x.shape[0], dtype=torch.float32)
+    _call("pack_add_rms_norm", *a, float(eps), None if residual is None else v.data_ptr(), a[7], y.data_ptr(), a[7],
+          rstd.data_ptr(), like=x, others=(weight, residual))
+    return y, v, rstd
+
+
+def add_rms_norm_q8(x, weight, residual=None, eps=1e-6):
+    """(q, scale, v): add_rms_norm's y as 8-bit codes q (int8 [rows, cols]) and a scale per row (fp32 [rows]);
+    y is q * scale[:, None]."""
+    a = _norm_inputs(x, weight, residual)
+    v = x if residual is None else _empty(x, *x.shape)
+    q, scale = _empty(x, *x.shape, dtype=torch.int8), _empty(x, x.shape[0], dtype=torch.float32)
+    _call("pack_add_rms_norm_q8", *a, float(eps), None if residual is None else v.data_ptr(), a[7], q.data_ptr(),
+          a[7], scale.data_ptr(), like=x, others=(weight, residual))
+    return q, scale, v
+
+
+def rms_norm_backward(dy, v, weight, rstd, dv=None):
+    """(dx, dweight) of add_rms_norm: dx is the gradient of x and of the residual, dv the gradient that reaches the
+    sum v on its other path (None: none).  dx in v's type, dweight fp32."""
+    prec = _prec(v, "v")
+    vp, ldv = _matrix(v, "v")
+    yp, ldy = _matrix(dy, "dy", v.dtype, v.shape)
+    rows, cols = v.shape
+    dp, ldd = (None, 0) if dv is None else _matrix(dv, "dv", v.dtype, v.shape)
+    wp, rp = _vector(weight, "weight", cols), _vector(rstd, "rstd", rows)
+    dx, dw = _empty(v, rows, cols), _empty(v, cols, dtype=torch.float32)
+    work = _empty(v, _bytes("pack_rms_norm_backward_workspace_size", rows, cols), dtype=torch.uint8)
+    _call("pack_rms_norm_backward", yp, ldy, vp, ldv, wp, rp, dp, ldd, prec, rows, cols, dx.data_ptr(), cols,
+          dw.data_ptr(), work.data_ptr(), work.numel(), like=v, others=(dy, weight, rstd, dv))
+    return dx, dw
+
+
+def quantize_rows(x):
+    """(q, scale): rows as 8-bit codes with a scale each; x is about q * scale[:, None]."""
+    prec = _prec(x, "x")
+    xp, ldx = _matrix(x, "x")
+    rows, cols = x.shape
+    q, scale = _empty(x, rows, cols, dtype=torch.int8), _empty(x, rows, dtype=torch.float32)
+    _call("pack_quantize_rows", xp, ldx, prec, rows, cols, q.data_ptr(), cols, scale.data_ptr(), like=x)
+    return q, scale
+
+
+def distill_topk(logits, idx, teacher, temperature=1.0, row_weight=None, grad=True):
+    """(loss, grad): the distillation loss of each row against its teacher entries and its gradient.
+
+    logits [rows, classes]; idx int32 and teacher fp32 [rows, k]: classes and logits of the teacher's entries (a
+    negative index or a logit of -inf: left out); row_weight fp32 [rows]: the factor of each row's loss in the
+    caller's total (None: 1).  loss fp32 [rows]; grad in logits' type, or None with grad=False."""
+    prec = _prec(logits, "logits")
+    zp, ldz = _matrix(logits, "logits")
+    rows, classes = logits.shape
+    _matrix(idx, "idx", torch.int32)
+    k = idx.shape[1]
+    if idx.shape[0] != rows:
+        _fail(f"idx must have {rows} rows, not {idx.shape[0]}")
+    _matrix(teacher, "teacher", torch.float32, (rows, k))
+    if not (idx.is_contiguous() and teacher.is_contiguous()):
+        _fail("idx and teacher must be contiguous")
+    wp = None if row_weight is None else _vector(row_weight, "row_weight", rows)
+    loss = _empty(logits, rows, dtype=torch.float32)
+    g = _empty(logits, rows, classes) if grad else None
+    _call("pack_distill_topk", zp, ldz, prec, rows, classes, idx.data_ptr(), teacher.data_ptr(), k,
+          float(temperature), wp, loss.data_ptr(), g.data_ptr() if grad else None, classes, like=logits,
+          others=(idx, teacher, row_weight))
+    return loss, g

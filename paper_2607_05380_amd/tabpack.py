@@ -27,7 +27,10 @@ SYMBOLS = ["pack_last_error", "pack_init", "pack_destroy", "pack_get_hparams", "
            "pack_select", "pack_member_param_count", "pack_get_params", "pack_set_params",
            "pack_get_grads", "pack_get_moments", "pack_debug_dropout_mask", "pack_debug_activation",
            "pack_profile_enable", "pack_profile_read", "pack_set_active", "pack_predict", "pack_status",
-           "pack_stream_copy", "pack_select_static", "pack_bind_data", "pack_debug_plan"]
+           "pack_stream_copy", "pack_select_static", "pack_bind_data", "pack_debug_plan",
+           # operators of a student network (``ops``)
+           "pack_add_rms_norm", "pack_add_rms_norm_q8", "pack_quantize_rows",
+           "pack_rms_norm_backward_workspace_size", "pack_rms_norm_backward", "pack_distill_topk"]
 
 
 class MemberHP(ctypes.Structure):
@@ -88,6 +91,7 @@ def load_library(path=LIB_PATH):
         raise PackError(f"{path} is missing: build it first (python -m paper_2607_05380_amd.build)")
     L = ctypes.CDLL(path)
     vp, i32, i64, u64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_size_t
+    f32 = ctypes.c_float
     H = vp
     sig = {
         "pack_last_error": ([], ctypes.c_char_p),
@@ -116,6 +120,13 @@ def load_library(path=LIB_PATH):
         "pack_stream_copy": ([vp, vp, sz, vp], ctypes.c_int),
         "pack_bind_data": ([H, vp, i64, vp, sz, vp], ctypes.c_int),
         "pack_debug_plan": ([ctypes.POINTER(PackConfig), vp, ctypes.POINTER(PlanInfo)], ctypes.c_int),
+        "pack_add_rms_norm": ([vp, i64, vp, i64, vp, i32, i64, i32, f32, vp, i64, vp, i64, vp, vp], ctypes.c_int),
+        "pack_add_rms_norm_q8": ([vp, i64, vp, i64, vp, i32, i64, i32, f32, vp, i64, vp, i64, vp, vp], ctypes.c_int),
+        "pack_quantize_rows": ([vp, i64, i32, i64, i32, vp, i64, vp, vp], ctypes.c_int),
+        "pack_rms_norm_backward_workspace_size": ([i64, i32, ctypes.POINTER(sz)], ctypes.c_int),
+        "pack_rms_norm_backward": ([vp, i64, vp, i64, vp, vp, vp, i64, i32, i64, i32, vp, i64, vp, vp, sz, vp],
+                                   ctypes.c_int),
+        "pack_distill_topk": ([vp, i64, i32, i64, i32, vp, vp, i32, f32, vp, vp, vp, i64, vp], ctypes.c_int),
     }
     for name, (args, res) in sig.items():
         fn = getattr(L, name)
