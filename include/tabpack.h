@@ -46,6 +46,7 @@ enum { PACK_TASK_REG_MSE = 0, PACK_TASK_BIN_BCE = 1, PACK_TASK_MULTI_CE = 2 };
 enum { PACK_PREC_BF16 = 0, PACK_PREC_FP32 = 1 };
 enum { PACK_PREDICT_MEMBERS = 0, PACK_PREDICT_ENSEMBLE = 1 };
 enum { PACK_OPT_ADAMW = 0, PACK_OPT_MUON = 1 };
+enum { PACK_ACT_SILU = 0, PACK_ACT_GELU = 1, PACK_ACT_RELU = 2 };
 
 /* Hyperparameters of one base model (Section 3.7: drawn per member from
  * user-given ranges; one hidden width shared by all hidden layers of the
@@ -437,6 +438,62 @@ int pack_rms_norm_backward(const void* dy, int64_t ldy, const void* sum, int64_t
 int pack_distill_topk(const void* logits, int64_t ldz, int32_t precision, int64_t rows, int32_t classes,
                       const int32_t* idx, const float* teacher, int32_t k, float temperature,
                       const float* row_weight, float* loss_out, void* grad_out, int64_t ldg, hipStream_t stream);
+
+/* The gated feed-forward block: with x [tokens, d_in], w_gate_up
+ * [2 hidden, d_in] (the gate rows, then the up rows) and w_down [d_out, hidden],
+ *   [g | u] = x w_gate_up^T,   h = act(g) u,   y = h w_down^T (+ residual).
+ * One kernel computes both projections, the activation and the product; a
+ * second the product with w_down.
+ *   act          PACK_ACT_SILU: g / (1 + e^-g); PACK_ACT_GELU: g (1 + erf(g / sqrt 2)) / 2;
+ *                PACK_ACT_RELU: max(g, 0)
+ *   residual     device [tokens, d_out] or NULL
+ *   gate_up_out  device [tokens, 2 hidden], dense: g and u for the backward
+ *                pass, or NULL
+ *   hidden_out   device [tokens, hidden], dense: h
+ *   out          device [tokens, d_out]
+ *   work         device scratch, 16-byte aligned, of
+ *                pack_gated_ff_workspace_size(..., backward = 0) bytes
+ * All matrices are in the precision; h and the saved g and u are rounded to it
+ * (h is formed from the unrounded ones). */
+int pack_gated_ff_workspace_size(int32_t precision, int64_t tokens, int32_t d_in, int32_t hidden, int32_t d_out,
+                                 int32_t backward, size_t* bytes);
+int pack_gated_ff_forward(const void* x, int64_t ldx, const void* w_gate_up, int64_t ldwg, const void* w_down,
+                          int64_t ldwd, const void* residual, int64_t ldr, int32_t precision, int32_t act,
+                          int64_t tokens, int32_t d_in, int32_t hidden, int32_t d_out, void* gate_up_out,
+                          void* hidden_out, void* out, int64_t ldo, void* work, size_t work_bytes,
+                          hipStream_t stream);
+
+/* Its gradients from dy [tokens, d_out], with g, u and h as the forward pass
+ * wrote them (the residual's gradient is dy itself):
+ *   dh = dy w_down,  dg = dh u act'(g),  du = dh act(g),
+ *   dx = [dg | du] w_gate_up,  dw_gate_up = [dg | du]^T x,  dw_down = dy^T h
+ *   dgate_up     device [tokens, 2 hidden], dense: dg and du (scratch of the
+ *                call; may be gate_up itself)
+ *   dx_out       device [tokens, d_in]; dw_gate_up_out [2 hidden, d_in] and
+ *                dw_down_out [d_out, hidden], dense; each may be NULL
+ * relu'(0) is 0. */
+int pack_gated_ff_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* w_gate_up,
+                           int64_t ldwg, const void* w_down, int64_t ldwd, const void* gate_up, const void* hidden_in,
+                           int32_t precision, int32_t act, int64_t tokens, int32_t d_in, int32_t hidden,
+                           int32_t d_out, void* dgate_up, void* dx_out, int64_t lddx, void* dw_gate_up_out,
+                           void* dw_down_out, void* work, size_t work_bytes, hipStream_t stream);
+
+/* Product of 8-bit codes: out[m, n] = x_scale[m] w_scale[n] sum_k x[m, k] w[n, k] (+ bias[n]),
+ * the sums exact in int32 (depth <= PACK_Q8_MAX_DEPTH).
+ *   gate         -1: w holds `outputs` rows; PACK_ACT_*: w, w_scale and bias
+ *                hold 2 outputs rows (gate rows, then up rows) and out is
+ *                act(gate value) up value
+ *   x            device int8 [rows, depth], x_scale device fp32 [rows]
+ *   w            device int8, w_scale device fp32, bias device fp32 or NULL
+ *   out          device [rows, outputs] in the precision
+ *   work         device scratch, 16-byte aligned, of
+ *                pack_q8_matmul_workspace_size() bytes */
+#define PACK_Q8_MAX_DEPTH 131071
+int pack_q8_matmul_workspace_size(int64_t rows, int32_t outputs, int32_t depth, int32_t gate, size_t* bytes);
+int pack_q8_matmul(const int8_t* x, int64_t ldx, const float* x_scale, const int8_t* w, int64_t ldw,
+                   const float* w_scale, const float* bias, int32_t gate, int32_t precision, int64_t rows,
+                   int32_t outputs, int32_t depth, void* out, int64_t ldo, void* work, size_t work_bytes,
+                   hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -1,8 +1,10 @@
 // Entry points of the student network's operators (include/tabpack.h):
 // argument checks, then one launch function of the kernels' files.
+#include <algorithm>
 #include <cfloat>
 #include <cstdarg>
 #include <cstdio>
+#include <initializer_list>
 
 #include "../../include/tabpack.h"
 #include "ops_internal.h"
@@ -68,9 +70,189 @@ int norm_rows(RowMode mode, RowArgs& a, int32_t precision, hipStream_t stream) {
   return done("row kernel", launch_rows(precision, mode, a, stream));
 }
 
+constexpr int32_t kMaxWidth = 1 << 24;  // d_in, hidden, d_out, outputs
+
+bool known_act(int32_t act) { return act >= PACK_ACT_SILU && act <= PACK_ACT_RELU; }
+
+MmType type_of(int32_t precision) { return precision == PACK_PREC_BF16 ? MM_BF16 : MM_FP32; }
+
+// The products of a gated block (x [T, D], hidden width F, y [T, O]).
+MmArgs mm_gate(int64_t T, int32_t D, int32_t F) {
+  MmArgs a{};
+  a.M = (int32_t)T, a.N = F, a.K = D, a.epi = MM_GATE;
+  return a;
+}
+MmArgs mm_down(int64_t T, int32_t F, int32_t O) {
+  MmArgs a{};
+  a.M = (int32_t)T, a.N = O, a.K = F, a.epi = MM_PLAIN;
+  return a;
+}
+MmArgs mm_dh(int64_t T, int32_t F, int32_t O) {
+  MmArgs a{};
+  a.M = (int32_t)T, a.N = F, a.K = O, a.b_rmaj = 1, a.epi = MM_GATE_BWD;
+  return a;
+}
+MmArgs mm_dx(int64_t T, int32_t D, int32_t F) {
+  MmArgs a{};
+  a.M = (int32_t)T, a.N = D, a.K = 2 * F, a.b_rmaj = 1, a.epi = MM_PLAIN;
+  return a;
+}
+MmArgs mm_dw(int64_t T, int32_t rows, int32_t cols) {
+  MmArgs a{};
+  a.M = rows, a.N = cols, a.K = (int32_t)T, a.a_rmaj = a.b_rmaj = 1, a.epi = MM_PLAIN;
+  return a;
+}
+MmArgs mm_q8(int64_t rows, int32_t outputs, int32_t depth, int32_t gate) {
+  MmArgs a{};
+  a.M = (int32_t)rows, a.N = outputs, a.K = depth, a.epi = gate < 0 ? MM_Q8 : MM_Q8_GATE, a.act = gate < 0 ? 0 : gate;
+  return a;
+}
+
+int check_ff(int32_t precision, int32_t act, int64_t T, int32_t D, int32_t F, int32_t O) {
+  if (!known(precision)) return bad("unknown precision %d", precision);
+  if (!known_act(act)) return bad("unknown activation %d", act);
+  if (T < 0 || T > kMaxExtent) return bad("tokens=%lld out of [0, 2^31 - 1]", (long long)T);
+  if (D < 1 || F < 1 || O < 1 || D > kMaxWidth || F > kMaxWidth || O > kMaxWidth)
+    return bad("d_in=%d, hidden=%d and d_out=%d must lie in [1, 2^24]", D, F, O);
+  return PACK_OK;
+}
+
+int check_q8(int64_t rows, int32_t outputs, int32_t depth, int32_t gate) {
+  if (gate != -1 && !known_act(gate)) return bad("unknown gate %d", gate);
+  if (rows < 0 || rows > kMaxExtent) return bad("rows=%lld out of [0, 2^31 - 1]", (long long)rows);
+  if (outputs < 1 || outputs > kMaxWidth) return bad("outputs=%d out of [1, 2^24]", outputs);
+  if (depth < 1 || depth > PACK_Q8_MAX_DEPTH) return bad("depth=%d out of [1, %d]", depth, PACK_Q8_MAX_DEPTH);
+  return PACK_OK;
+}
+
+int check_work(const void* work, size_t have, size_t need) {
+  if (need == 0) return PACK_OK;
+  if (!work) return bad("work is NULL");
+  if (have < need) return bad("workspace has %zu bytes, %zu needed", have, need);
+  if (!aligned(work, 16)) return bad("workspace must be 16-byte aligned");
+  return PACK_OK;
+}
+
+size_t largest(std::initializer_list<size_t> v) { return std::max(v); }
+
 }  // namespace
 
 extern "C" {
+
+int pack_gated_ff_workspace_size(int32_t precision, int64_t tokens, int32_t d_in, int32_t hidden, int32_t d_out,
+                                 int32_t backward, size_t* bytes) {
+  if (!bytes) return bad("bytes is NULL");
+  const int rc = check_ff(precision, PACK_ACT_SILU, tokens, d_in, hidden, d_out);
+  if (rc != PACK_OK) return rc;
+  const MmType t = type_of(precision);
+  *bytes = !backward ? largest({mm_workspace(t, mm_gate(tokens, d_in, hidden)), mm_workspace(t, mm_down(tokens, hidden, d_out))})
+                     : largest({mm_workspace(t, mm_dh(tokens, hidden, d_out)), mm_workspace(t, mm_dx(tokens, d_in, hidden)),
+                                mm_workspace(t, mm_dw(tokens, 2 * hidden, d_in)), mm_workspace(t, mm_dw(tokens, d_out, hidden))});
+  return PACK_OK;
+}
+
+int pack_gated_ff_forward(const void* x, int64_t ldx, const void* w_gate_up, int64_t ldwg, const void* w_down,
+                          int64_t ldwd, const void* residual, int64_t ldr, int32_t precision, int32_t act,
+                          int64_t tokens, int32_t d_in, int32_t hidden, int32_t d_out, void* gate_up_out,
+                          void* hidden_out, void* out, int64_t ldo, void* work, size_t work_bytes,
+                          hipStream_t stream) {
+  int rc = check_ff(precision, act, tokens, d_in, hidden, d_out);
+  if (rc != PACK_OK) return rc;
+  if (!ld_ok(ldx, d_in) || !ld_ok(ldwg, d_in) || !ld_ok(ldwd, hidden) || (residual && !ld_ok(ldr, d_out)) ||
+      !ld_ok(ldo, d_out))
+    return bad("a leading dimension is smaller than its matrix's rows or too large");
+  if (tokens == 0) return PACK_OK;
+  if (!x || !w_gate_up || !w_down || !hidden_out || !out) return bad("NULL device pointer");
+  size_t need = 0;
+  rc = pack_gated_ff_workspace_size(precision, tokens, d_in, hidden, d_out, 0, &need);
+  if (rc == PACK_OK) rc = check_work(work, work_bytes, need);
+  if (rc != PACK_OK) return rc;
+  const MmType t = type_of(precision);
+  MmArgs a = mm_gate(tokens, d_in, hidden);
+  a.A = x, a.lda = ldx, a.B = w_gate_up, a.ldb = ldwg, a.act = act;
+  a.pre = gate_up_out, a.ldpre = 2 * (int64_t)hidden, a.out = hidden_out, a.ldo = hidden;
+  a.work = static_cast<float*>(work), a.work_bytes = work_bytes;
+  rc = done("gate and up projections", launch_mm(t, a, stream));
+  if (rc != PACK_OK) return rc;
+  MmArgs d = mm_down(tokens, hidden, d_out);
+  d.A = hidden_out, d.lda = hidden, d.B = w_down, d.ldb = ldwd, d.add = residual, d.ldadd = ldr;
+  d.out = out, d.ldo = ldo, d.work = a.work, d.work_bytes = work_bytes;
+  return done("down projection", launch_mm(t, d, stream));
+}
+
+int pack_gated_ff_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* w_gate_up,
+                           int64_t ldwg, const void* w_down, int64_t ldwd, const void* gate_up, const void* hidden_in,
+                           int32_t precision, int32_t act, int64_t tokens, int32_t d_in, int32_t hidden,
+                           int32_t d_out, void* dgate_up, void* dx_out, int64_t lddx, void* dw_gate_up_out,
+                           void* dw_down_out, void* work, size_t work_bytes, hipStream_t stream) {
+  int rc = check_ff(precision, act, tokens, d_in, hidden, d_out);
+  if (rc != PACK_OK) return rc;
+  if (!ld_ok(lddy, d_out) || !ld_ok(ldx, d_in) || !ld_ok(ldwg, d_in) || !ld_ok(ldwd, hidden) ||
+      (dx_out && !ld_ok(lddx, d_in)))
+    return bad("a leading dimension is smaller than its matrix's rows or too large");
+  if (tokens > 0 && (!dy || !x || !w_gate_up || !w_down || !gate_up || !hidden_in || !dgate_up))
+    return bad("NULL device pointer");
+  size_t need = 0;
+  rc = pack_gated_ff_workspace_size(precision, tokens, d_in, hidden, d_out, 1, &need);
+  if (rc == PACK_OK) rc = check_work(work, work_bytes, need);
+  if (rc != PACK_OK) return rc;
+  const MmType t = type_of(precision);
+  const int64_t ldg = 2 * (int64_t)hidden;
+  float* const w = static_cast<float*>(work);
+  if (tokens > 0 && (dx_out || dw_gate_up_out)) {
+    MmArgs a = mm_dh(tokens, hidden, d_out);
+    a.A = dy, a.lda = lddy, a.B = w_down, a.ldb = ldwd, a.act = act, a.pre = const_cast<void*>(gate_up), a.ldpre = ldg;
+    a.out = dgate_up, a.ldo = ldg, a.work = w, a.work_bytes = work_bytes;
+    rc = done("gradients of gate and up", launch_mm(t, a, stream));
+    if (rc != PACK_OK) return rc;
+  }
+  if (tokens > 0 && dx_out) {
+    MmArgs a = mm_dx(tokens, d_in, hidden);
+    a.A = dgate_up, a.lda = ldg, a.B = w_gate_up, a.ldb = ldwg, a.out = dx_out, a.ldo = lddx, a.work = w, a.work_bytes = work_bytes;
+    rc = done("gradient of x", launch_mm(t, a, stream));
+    if (rc != PACK_OK) return rc;
+  }
+  if (dw_gate_up_out) {
+    MmArgs a = mm_dw(tokens, 2 * hidden, d_in);
+    a.A = dgate_up, a.lda = ldg, a.B = x, a.ldb = ldx, a.out = dw_gate_up_out, a.ldo = d_in, a.work = w, a.work_bytes = work_bytes;
+    rc = done("gradient of w_gate_up", launch_mm(t, a, stream));
+    if (rc != PACK_OK) return rc;
+  }
+  if (dw_down_out) {
+    MmArgs a = mm_dw(tokens, d_out, hidden);
+    a.A = dy, a.lda = lddy, a.B = hidden_in, a.ldb = hidden, a.out = dw_down_out, a.ldo = hidden, a.work = w, a.work_bytes = work_bytes;
+    rc = done("gradient of w_down", launch_mm(t, a, stream));
+  }
+  return rc;
+}
+
+int pack_q8_matmul_workspace_size(int64_t rows, int32_t outputs, int32_t depth, int32_t gate, size_t* bytes) {
+  if (!bytes) return bad("bytes is NULL");
+  const int rc = check_q8(rows, outputs, depth, gate);
+  if (rc != PACK_OK) return rc;
+  *bytes = mm_workspace(MM_I8, mm_q8(rows, outputs, depth, gate));
+  return PACK_OK;
+}
+
+int pack_q8_matmul(const int8_t* x, int64_t ldx, const float* x_scale, const int8_t* w, int64_t ldw,
+                   const float* w_scale, const float* bias, int32_t gate, int32_t precision, int64_t rows,
+                   int32_t outputs, int32_t depth, void* out, int64_t ldo, void* work, size_t work_bytes,
+                   hipStream_t stream) {
+  if (!known(precision)) return bad("unknown precision %d", precision);
+  int rc = check_q8(rows, outputs, depth, gate);
+  if (rc != PACK_OK) return rc;
+  if (!ld_ok(ldx, depth) || !ld_ok(ldw, depth) || !ld_ok(ldo, outputs))
+    return bad("a leading dimension is smaller than its matrix's rows or too large");
+  if (rows == 0) return PACK_OK;
+  if (!x || !x_scale || !w || !w_scale || !out) return bad("NULL device pointer");
+  MmArgs a = mm_q8(rows, outputs, depth, gate);
+  rc = check_work(work, work_bytes, mm_workspace(MM_I8, a));
+  if (rc != PACK_OK) return rc;
+  a.A = x, a.lda = ldx, a.B = w, a.ldb = ldw, a.row_scale = x_scale, a.col_scale = w_scale, a.bias = bias;
+  a.out = out, a.ldo = ldo, a.out_f32 = precision == PACK_PREC_FP32;
+  a.work = static_cast<float*>(work), a.work_bytes = work_bytes;
+  return done("8-bit product", launch_mm(MM_I8, a, stream));
+}
 
 int pack_add_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, const float* weight,
                       int32_t precision, int64_t rows, int32_t cols, float eps, void* sum_out, int64_t lds,

@@ -59,4 +59,39 @@ struct DistillArgs {
 };
 hipError_t launch_distill(int prec, const DistillArgs& a, hipStream_t s);
 
+// A matrix product C[m, n] = sum_k A(m, k) B(n, k) with an epilogue per element.
+enum MmType { MM_BF16 = 0, MM_FP32 = 1, MM_I8 = 2 };
+// How an operand lies in memory: depth-contiguous (element (r, k) at P[r * ld + k])
+// or rows-contiguous (at P[k * ld + r]).
+enum MmEpi {
+  MM_PLAIN = 0,     // out = C (+ add)
+  MM_GATE = 1,      // B holds n gate rows, then n up rows: out = act(C_gate) C_up; both to `pre` if given
+  MM_GATE_BWD = 2,  // C = dh: out = [dh u act'(g) | dh act(g)], g and u from `pre`
+  MM_Q8 = 3,        // out = C row_scale col_scale (+ bias)
+  MM_Q8_GATE = 4,   // the same for 2 n columns, then act(gate) up
+};
+struct MmArgs {
+  const void* A;
+  const void* B;
+  int64_t lda, ldb;
+  int32_t M, N, K;        // N: output columns (gated: of each half)
+  int32_t a_rmaj, b_rmaj; // 1: rows-contiguous
+  int32_t epi, act;
+  const void* add;        // MM_PLAIN: or NULL
+  void* pre;              // [M, 2N] gate and up values (MM_GATE: or NULL)
+  void* out;
+  int64_t ldadd, ldpre, ldo;
+  const float* row_scale;
+  const float* col_scale; // [N] or [2N]
+  const float* bias;      // [N] or [2N], or NULL
+  int32_t out_f32;        // MM_Q8*: type of out (elsewhere the operands')
+  float* work;            // partial sums of a split depth
+  size_t work_bytes;
+  // filled in by launch_mm
+  int32_t tiles_m, tiles_n, splits, steps_per_split, vec_out;
+};
+// Bytes of `work` that the product needs (0: none).
+size_t mm_workspace(MmType type, const MmArgs& a);
+hipError_t launch_mm(MmType type, const MmArgs& a, hipStream_t s);
+
 }  // namespace tabpack

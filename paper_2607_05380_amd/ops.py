@@ -5,6 +5,8 @@ class probabilities and served in 8 bits.  Its parts:
 
   distill_topk                        the loss against a teacher's top logits and its gradient
   add_rms_norm, rms_norm_backward     root-mean-square norm of x + residual, and its gradients
+  gated_ff, gated_ff_backward         y = (act(x Wg^T) * (x Wu^T)) Wd^T (+ residual), and its gradients
+  q8_matmul                           product of 8-bit codes with scales per row and output, optionally gated
   add_rms_norm_q8, quantize_rows      the norm, or plain rows, as 8-bit codes with a scale per row
 
 Matrices are 2-D device tensors in bfloat16 or float32 whose rows are contiguous (any row stride and alignment).
@@ -158,3 +160,90 @@ def distill_topk(logits, idx, teacher, temperature=1.0, row_weight=None, grad=Tr
           float(temperature), wp, loss.data_ptr(), g.data_ptr() if grad else None, classes, like=logits,
           others=(idx, teacher, row_weight))
     return loss, g
+
+
+def _act(act):
+    if act not in tabpack.ACTIVATIONS:
+        _fail(f"unknown activation {act!r}")
+    return tabpack.ACTIVATIONS[act]
+
+
+def _work(like, fn, *args):
+    n = _bytes(fn, *args)
+    return _empty(like, n, dtype=torch.uint8) if n else None
+
+
+def _ff_inputs(x, w_gate_up, w_down):
+    prec = _prec(x, "x")
+    xp, ldx = _matrix(x, "x")
+    tokens, d_in = x.shape
+    wdp, ldwd = _matrix(w_down, "w_down", x.dtype)
+    d_out, hidden = w_down.shape
+    wgp, ldwg = _matrix(w_gate_up, "w_gate_up", x.dtype, (2 * hidden, d_in))
+    return prec, (tokens, d_in, hidden, d_out), (xp, ldx, wgp, ldwg, wdp, ldwd)
+
+
+def gated_ff(x, w_gate_up, w_down, act="silu", residual=None, save=False):
+    """y = h w_down^T (+ residual) with [g | u] = x w_gate_up^T and h = act(g) u: x [tokens, d_in], w_gate_up
+    [2 hidden, d_in] (gate rows, then up rows), w_down [d_out, hidden], all in one type; act "silu", "gelu" or
+    "relu".  save=True: (y, saved), saved = ([g | u], h) for gated_ff_backward."""
+    prec, dims, ptrs = _ff_inputs(x, w_gate_up, w_down)
+    tokens, _, hidden, d_out = dims
+    rp, ldr = (None, 0) if residual is None else _matrix(residual, "residual", x.dtype, (tokens, d_out))
+    code = _act(act)
+    gu = _empty(x, tokens, 2 * hidden) if save else None
+    h, y = _empty(x, tokens, hidden), _empty(x, tokens, d_out)
+    work = _work(x, "pack_gated_ff_workspace_size", prec, *dims, 0)
+    _call("pack_gated_ff_forward", *ptrs, rp, ldr, prec, code, *dims, gu.data_ptr() if save else None, h.data_ptr(),
+          y.data_ptr(), d_out, None if work is None else work.data_ptr(), 0 if work is None else work.numel(),
+          like=x, others=(w_gate_up, w_down, residual))
+    return (y, (gu, h)) if save else y
+
+
+def gated_ff_backward(dy, x, w_gate_up, w_down, saved, act="silu", need_dx=True):
+    """(dx, dw_gate_up, dw_down) of gated_ff from dy [tokens, d_out] and what it saved (the residual's gradient is
+    dy itself), in x's type; dx is None with need_dx=False."""
+    prec, dims, ptrs = _ff_inputs(x, w_gate_up, w_down)
+    tokens, d_in, hidden, d_out = dims
+    gp, ldg = _matrix(dy, "dy", x.dtype, (tokens, d_out))
+    gu, h = saved
+    for t, name, cols in ((gu, "saved gate and up values", 2 * hidden), (h, "saved hidden values", hidden)):
+        _matrix(t, name, x.dtype, (tokens, cols))
+        if not t.is_contiguous():
+            _fail(f"{name} must be contiguous")
+    code = _act(act)
+    dgu = _empty(x, tokens, 2 * hidden)
+    dx = _empty(x, tokens, d_in) if need_dx else None
+    dwg, dwd = _empty(x, 2 * hidden, d_in), _empty(x, d_out, hidden)
+    work = _work(x, "pack_gated_ff_workspace_size", prec, *dims, 1)
+    _call("pack_gated_ff_backward", gp, ldg, *ptrs, gu.data_ptr(), h.data_ptr(), prec, code, *dims, dgu.data_ptr(),
+          dx.data_ptr() if need_dx else None, d_in, dwg.data_ptr(), dwd.data_ptr(),
+          None if work is None else work.data_ptr(), 0 if work is None else work.numel(), like=x,
+          others=(dy, w_gate_up, w_down, gu, h))
+    return dx, dwg, dwd
+
+
+def q8_matmul(q, scale, w, w_scale, bias=None, gate=None, dtype=torch.bfloat16):
+    """(q * scale[:, None]) (w * w_scale[:, None])^T (+ bias) of 8-bit codes q int8 [rows, depth] and w int8
+    [outputs, depth], scales and bias fp32, summed exactly in int32; [rows, outputs] in ``dtype``.  gate: an activation
+    name; w, w_scale and bias then hold the gate rows and the up rows, and the result is act(gate) * up."""
+    qp, ldq = _matrix(q, "q", torch.int8)
+    rows, depth = q.shape
+    wp, ldw = _matrix(w, "w", torch.int8)
+    n = w.shape[0]
+    if w.shape[1] != depth:
+        _fail(f"w must have {depth} columns, not {w.shape[1]}")
+    code = -1 if gate is None else _act(gate)
+    if gate is not None and n % 2:
+        _fail("a gated w holds as many gate rows as up rows")
+    if dtype not in _PREC:
+        _fail("dtype must be bfloat16 or float32")
+    sp, wsp = _vector(scale, "scale", rows), _vector(w_scale, "w_scale", n)
+    bp = None if bias is None else _vector(bias, "bias", n)
+    outputs = n if gate is None else n // 2
+    out = _empty(q, rows, outputs, dtype=dtype)
+    work = _work(q, "pack_q8_matmul_workspace_size", rows, outputs, depth, code)
+    _call("pack_q8_matmul", qp, ldq, sp, wp, ldw, wsp, bp, code, _PREC[dtype], rows, outputs, depth, out.data_ptr(),
+          outputs, None if work is None else work.data_ptr(), 0 if work is None else work.numel(), like=q,
+          others=(scale, w, w_scale, bias))
+    return out

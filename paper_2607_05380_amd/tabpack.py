@@ -21,6 +21,7 @@ PREDICT_MEMBERS, PREDICT_ENSEMBLE = 0, 1
 STATUS_IDX_RANGE = 1
 BIND_DATA_MAX_B = 2048  # PACK_BIND_DATA_MAX_B
 OPTIMIZERS = {"adamw": 0, "muon": 1}
+ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2}
 
 SYMBOLS = ["pack_last_error", "pack_init", "pack_destroy", "pack_get_hparams", "pack_workspace_size",
            "pack_bind", "pack_train_step", "pack_eval_members", "pack_select_workspace_size",
@@ -30,7 +31,9 @@ SYMBOLS = ["pack_last_error", "pack_init", "pack_destroy", "pack_get_hparams", "
            "pack_stream_copy", "pack_select_static", "pack_bind_data", "pack_debug_plan",
            # operators of a student network (``ops``)
            "pack_add_rms_norm", "pack_add_rms_norm_q8", "pack_quantize_rows",
-           "pack_rms_norm_backward_workspace_size", "pack_rms_norm_backward", "pack_distill_topk"]
+           "pack_rms_norm_backward_workspace_size", "pack_rms_norm_backward", "pack_distill_topk",
+           "pack_gated_ff_workspace_size", "pack_gated_ff_forward", "pack_gated_ff_backward",
+           "pack_q8_matmul_workspace_size", "pack_q8_matmul"]
 
 
 class MemberHP(ctypes.Structure):
@@ -126,6 +129,13 @@ def load_library(path=LIB_PATH):
         "pack_rms_norm_backward_workspace_size": ([i64, i32, ctypes.POINTER(sz)], ctypes.c_int),
         "pack_rms_norm_backward": ([vp, i64, vp, i64, vp, vp, vp, i64, i32, i64, i32, vp, i64, vp, vp, sz, vp],
                                    ctypes.c_int),
+        "pack_gated_ff_workspace_size": ([i32, i64, i32, i32, i32, i32, ctypes.POINTER(sz)], ctypes.c_int),
+        "pack_gated_ff_forward": ([vp, i64, vp, i64, vp, i64, vp, i64, i32, i32, i64, i32, i32, i32, vp, vp, vp, i64,
+                                   vp, sz, vp], ctypes.c_int),
+        "pack_gated_ff_backward": ([vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, i32, i32, i64, i32, i32, i32, vp, vp,
+                                    i64, vp, vp, vp, sz, vp], ctypes.c_int),
+        "pack_q8_matmul_workspace_size": ([i64, i32, i32, i32, ctypes.POINTER(sz)], ctypes.c_int),
+        "pack_q8_matmul": ([vp, i64, vp, vp, i64, vp, vp, i32, i32, i64, i32, i32, vp, i64, vp, sz, vp], ctypes.c_int),
         "pack_distill_topk": ([vp, i64, i32, i64, i32, vp, vp, i32, f32, vp, vp, vp, i64, vp], ctypes.c_int),
     }
     for name, (args, res) in sig.items():

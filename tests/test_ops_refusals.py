@@ -79,10 +79,74 @@ def test_distill_refuses(kw, part):
                                                   "g", "ldg")] + [None], part)
 
 
+FF = dict(x=P, ldx=16, wg=P, ldwg=16, wd=P, ldwd=24, r=P, ldr=8, prec=BF16, act=0, T=4, D=16, F=24, O=8, gu=P, h=P,
+          out=P, ldo=8, work=P, nbytes=1 << 40)
+
+
+@pytest.mark.parametrize("kw,part", [
+    (dict(x=None), "NULL"), (dict(wg=None), "NULL"), (dict(wd=None), "NULL"), (dict(h=None), "NULL"),
+    (dict(out=None), "NULL"), (dict(ldx=15), "leading"), (dict(ldwg=15), "leading"), (dict(ldwd=23), "leading"),
+    (dict(ldr=7), "leading"), (dict(ldo=7), "leading"), (dict(prec=2), "precision"), (dict(act=3), "activation"),
+    (dict(act=-1), "activation"), (dict(T=-1), "tokens"), (dict(T=1 << 31), "tokens"), (dict(D=0), "d_in"),
+    (dict(F=0), "d_in"), (dict(O=0), "d_in"), (dict(F=(1 << 24) + 1), "d_in"),
+    (dict(D=1 << 20, ldx=1 << 20, ldwg=1 << 20, work=None), "work"),
+    (dict(D=1 << 20, ldx=1 << 20, ldwg=1 << 20, nbytes=16), "workspace"),
+    (dict(D=1 << 20, ldx=1 << 20, ldwg=1 << 20, work=P + 8), "aligned")])
+def test_gated_ff_refuses(kw, part):
+    a = dict(FF, **kw)
+    _refused("pack_gated_ff_forward", [a[k] for k in ("x", "ldx", "wg", "ldwg", "wd", "ldwd", "r", "ldr", "prec", "act",
+                                                      "T", "D", "F", "O", "gu", "h", "out", "ldo", "work", "nbytes")]
+             + [None], part)
+
+
+@pytest.mark.parametrize("kw,part", [
+    (dict(dy=None), "NULL"), (dict(x=None), "NULL"), (dict(gu=None), "NULL"), (dict(h=None), "NULL"),
+    (dict(dgu=None), "NULL"), (dict(wd=None), "NULL"), (dict(wg=None), "NULL"), (dict(lddy=7), "leading"),
+    (dict(lddx=15), "leading"), (dict(prec=9), "precision"), (dict(act=5), "activation"), (dict(T=-3), "tokens"),
+    (dict(T=1 << 20, nbytes=0), "workspace"), (dict(T=1 << 20, work=P + 4), "aligned")])
+def test_gated_ff_backward_refuses(kw, part):
+    a = dict(FF, dy=P, lddy=8, dgu=P, dx=P, lddx=16, dwg=P, dwd=P)
+    a.update(kw)
+    _refused("pack_gated_ff_backward", [a[k] for k in ("dy", "lddy", "x", "ldx", "wg", "ldwg", "wd", "ldwd", "gu", "h",
+                                                       "prec", "act", "T", "D", "F", "O", "dgu", "dx", "lddx", "dwg",
+                                                       "dwd", "work", "nbytes")] + [None], part)
+
+
+@pytest.mark.parametrize("kw,part", [
+    (dict(x=None), "NULL"), (dict(xs=None), "NULL"), (dict(w=None), "NULL"), (dict(ws=None), "NULL"),
+    (dict(out=None), "NULL"), (dict(gate=3), "gate"), (dict(gate=-2), "gate"), (dict(prec=3), "precision"),
+    (dict(M=-1), "rows"), (dict(N=0), "outputs"), (dict(K=0), "depth"), (dict(K=131072), "depth"),
+    (dict(ldx=31), "leading"), (dict(ldw=31), "leading"), (dict(ldo=7), "leading"),
+    (dict(M=100, K=131071, ldx=131071, ldw=131071, work=None), "work"),
+    (dict(M=100, K=131071, ldx=131071, ldw=131071, nbytes=8), "workspace")])
+def test_q8_matmul_refuses(kw, part):
+    a = dict(x=P, ldx=32, xs=P, w=P, ldw=32, ws=P, b=P, gate=-1, prec=BF16, M=100, N=8, K=32, out=P, ldo=8, work=P,
+             nbytes=1 << 40)
+    a.update(kw)
+    _refused("pack_q8_matmul", [a[k] for k in ("x", "ldx", "xs", "w", "ldw", "ws", "b", "gate", "prec", "M", "N", "K",
+                                               "out", "ldo", "work", "nbytes")] + [None], part)
+
+
+def test_workspace_sizes():
+    lib = tabpack.load_library()
+    n = ctypes.c_size_t()
+    for T in (0, 1, 17, 4096, (1 << 31) - 1):
+        for backward in (0, 1):
+            assert lib.pack_gated_ff_workspace_size(BF16, T, 24, 40, 8, backward, ctypes.byref(n)) == 0
+        assert lib.pack_q8_matmul_workspace_size(T, 24, 40, -1, ctypes.byref(n)) == 0
+        assert lib.pack_rms_norm_backward_workspace_size(T, 24, ctypes.byref(n)) == 0
+    assert lib.pack_gated_ff_workspace_size(BF16, 1, 24, 40, 8, 0, None) == -1
+    assert lib.pack_gated_ff_workspace_size(2, 1, 24, 40, 8, 0, ctypes.byref(n)) == -1
+    assert lib.pack_q8_matmul_workspace_size(1, 24, 40, -1, None) == -1
+    assert lib.pack_q8_matmul_workspace_size(1, 0, 40, -1, ctypes.byref(n)) == -1
+
+
 def test_binding_refuses_host_tensors_and_types():
     h = torch.zeros(2, 8)
     for call in (lambda: ops.add_rms_norm(h, torch.ones(8)), lambda: ops.add_rms_norm_q8(h, torch.ones(8)),
                  lambda: ops.quantize_rows(h), lambda: ops.quantize_rows(h.double()), lambda: ops.quantize_rows([1]),
+                 lambda: ops.gated_ff(h, torch.zeros(4, 8), torch.zeros(8, 2)),
+                 lambda: ops.q8_matmul(h.char(), torch.ones(2), h.char(), torch.ones(2)),
                  lambda: ops.rms_norm_backward(h, h, torch.ones(8), torch.ones(2)),
                  lambda: ops.distill_topk(h, torch.zeros(2, 1, dtype=torch.int32), torch.zeros(2, 1))):
         with pytest.raises(tabpack.PackError):
