@@ -24,7 +24,9 @@
 //          rest go straight to LDS.
 //   huge   256 x 256, 8 waves of 128 x 64, two steps in LDS (128 KB), one
 //          workgroup per CU (see huge_kernel).
-//   thin   up to 64 rows of A, 16 columns, no LDS for operands: each weight
+//   mini   64 x 64, 4 waves of 32 x 32, four steps in LDS (64 KB); for products
+//          whose larger tiles would leave CUs idle.
+//   thin   up to 16 rows of A, 16 columns, no LDS for operands: each weight
 //          byte is read once (see thin_kernel).
 // MFMAs: v_mfma_f32_32x32x16_bf16, v_mfma_i32_32x32x32_i8,
 // v_mfma_f32_32x32x2_f32, with B as the first operand, so that a lane holds 4
@@ -104,125 +106,174 @@ __device__ __forceinline__ void act_value_grad(int act, float g, float& v, float
 }
 
 // ---------------------------------------------------------------- epilogues --
-// 8 consecutive elements of a row, or the `n` of them that exist; vec: they
-// all do and lie at 16 bytes.
-__device__ __forceinline__ void load8(const __bf16* p, float* v, int n, bool vec) {
-  if (vec) {
-    const u32x4 u = *reinterpret_cast<const u32x4*>(p);
+// 8 consecutive elements at 16 bytes, as they lie in memory
+template <typename T>
+struct Raw8 {
+  u32x4 v[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[2 * i] = __builtin_bit_cast(float, u[i] << 16);
-      v[2 * i + 1] = __builtin_bit_cast(float, u[i] & 0xffff0000u);
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) v[i] = *reinterpret_cast<const u32x4*>(p + i * (16 / sizeof(T)));
+  }
+  __device__ __forceinline__ void get(float* f) const {
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        f[2 * i] = __builtin_bit_cast(float, v[0][i] << 16);
+        f[2 * i + 1] = __builtin_bit_cast(float, v[0][i] & 0xffff0000u);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const f32x4 x = __builtin_bit_cast(f32x4, v[i]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) f[4 * i + j] = x[j];
+      }
     }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < n ? (float)p[i] : 0.0f;
   }
+};
+__device__ __forceinline__ void store8(__bf16* p, const float* v) {
+  bf16x8 o;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) o[i] = (__bf16)v[i];
+  *reinterpret_cast<bf16x8*>(p) = o;
 }
-__device__ __forceinline__ void load8(const float* p, float* v, int n, bool vec) {
-  if (vec) {
+__device__ __forceinline__ void store8(float* p, const float* v) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const f32x4 u = *reinterpret_cast<const f32x4*>(p + 4 * i);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) v[4 * i + j] = u[j];
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.0f;
-  }
-}
-__device__ __forceinline__ void store8(__bf16* p, const float* v, int n, bool vec) {
-  if (vec) {
-    bf16x8 o;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = (__bf16)v[i];
-    *reinterpret_cast<bf16x8*>(p) = o;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < n) p[i] = (__bf16)v[i];
-  }
-}
-__device__ __forceinline__ void store8(float* p, const float* v, int n, bool vec) {
-  if (vec) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      *reinterpret_cast<f32x4*>(p + 4 * i) = f32x4{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < n) p[i] = v[i];
-  }
+  for (int i = 0; i < 2; ++i)
+    *reinterpret_cast<f32x4*>(p + 4 * i) = f32x4{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
 }
 
-// The outputs n .. n + 7 (n < N) of row m from the sums c (gated: gate sums c,
-// up sums u), which are consumed.
+// What an epilogue reads besides the sums, for 8 columns at 16 bytes: per
+// column (8-bit products), and per row and column.
+struct Q8Cols {
+  Raw8<float> scale, bias;
+  __device__ __forceinline__ void load(const MmArgs& a, int n) {
+    scale.load(a.col_scale + n);
+    if (a.bias) {
+      bias.load(a.bias + n);
+    } else {
+      bias.v[0] = bias.v[1] = u32x4{0, 0, 0, 0};
+    }
+  }
+  // sums in int32 -> values
+  __device__ __forceinline__ void apply(float* c, float row_scale) const {
+    float s[8], b[8];
+    scale.get(s);
+    bias.get(b);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] = (float)__builtin_bit_cast(int32_t, c[i]) * (row_scale * s[i]) + b[i];
+  }
+};
 template <int EPI, typename T>
-__device__ __forceinline__ void finish8(const MmArgs& a, int64_t m, int n, float* c, float* u) {
-  const int cnt = a.N - n;
-  const bool vec = a.vec_out && cnt >= 8;
+struct Cols {
+  Q8Cols gate, up;
+  __device__ __forceinline__ void load(const MmArgs& a, int n) {
+    if constexpr (is_q8(EPI)) gate.load(a, n);
+    if constexpr (EPI == MM_Q8_GATE) up.load(a, a.N + n);
+  }
+};
+template <int EPI, typename T>
+struct Extra {
+  Raw8<T> g, u;
+  float row_scale;
+  __device__ __forceinline__ void load(const MmArgs& a, int64_t m, int n) {
+    if constexpr (is_q8(EPI)) row_scale = a.row_scale[m];
+    if constexpr (EPI == MM_PLAIN) {
+      if (a.add) g.load(static_cast<const T*>(a.add) + m * a.ldadd + n);
+    }
+    if constexpr (EPI == MM_GATE_BWD) {
+      const T* p = static_cast<const T*>(a.pre) + m * a.ldpre + n;
+      g.load(p);
+      u.load(p + a.N);
+    }
+  }
+};
+
+// The outputs n .. n + 7 of row m from the sums c (gated: gate sums c, up sums
+// u), which are consumed; everything at 16 bytes.
+template <int EPI, typename T>
+__device__ __forceinline__ void finish8(const MmArgs& a, int64_t m, int n, float* c, float* u,
+                                        const Cols<EPI, T>& cols, const Extra<EPI, T>& x) {
   constexpr bool FAST = sizeof(T) == 2;
   if constexpr (is_q8(EPI)) {
-    const float sx = a.row_scale[m];
-    float sw[8], b[8];
-    load8(a.col_scale + n, sw, cnt, vec);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) c[i] = (float)__builtin_bit_cast(int32_t, c[i]) * (sx * sw[i]);
-    if (a.bias) {
-      load8(a.bias + n, b, cnt, vec);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) c[i] += b[i];
-    }
+    cols.gate.apply(c, x.row_scale);
     if constexpr (EPI == MM_Q8_GATE) {
-      load8(a.col_scale + a.N + n, sw, cnt, vec);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) u[i] = (float)__builtin_bit_cast(int32_t, u[i]) * (sx * sw[i]);
-      if (a.bias) {
-        load8(a.bias + a.N + n, b, cnt, vec);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) u[i] += b[i];
-      }
+      cols.up.apply(u, x.row_scale);
 #pragma unroll
       for (int i = 0; i < 8; ++i) c[i] = act_value<false>(a.act, c[i]) * u[i];
     }
     if (a.out_f32)
-      store8(static_cast<float*>(a.out) + m * a.ldo + n, c, cnt, vec);
+      store8(static_cast<float*>(a.out) + m * a.ldo + n, c);
     else
-      store8(static_cast<__bf16*>(a.out) + m * a.ldo + n, c, cnt, vec);
+      store8(static_cast<__bf16*>(a.out) + m * a.ldo + n, c);
   } else if constexpr (EPI == MM_PLAIN) {
     if (a.add) {
       float r[8];
-      load8(static_cast<const T*>(a.add) + m * a.ldadd + n, r, cnt, vec);
+      x.g.get(r);
 #pragma unroll
       for (int i = 0; i < 8; ++i) c[i] += r[i];
     }
-    store8(static_cast<T*>(a.out) + m * a.ldo + n, c, cnt, vec);
+    store8(static_cast<T*>(a.out) + m * a.ldo + n, c);
   } else if constexpr (EPI == MM_GATE) {
     if (a.pre) {
       T* p = static_cast<T*>(a.pre) + m * a.ldpre + n;
-      store8(p, c, cnt, vec);
-      store8(p + a.N, u, cnt, vec);
+      store8(p, c);
+      store8(p + a.N, u);
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) c[i] = act_value<FAST>(a.act, c[i]) * u[i];
-    store8(static_cast<T*>(a.out) + m * a.ldo + n, c, cnt, vec);
+    store8(static_cast<T*>(a.out) + m * a.ldo + n, c);
   } else {
     static_assert(EPI == MM_GATE_BWD);
-    float g[8], w[8], dg[8], du[8];
-    const T* p = static_cast<const T*>(a.pre) + m * a.ldpre + n;
-    load8(p, g, cnt, vec);
-    load8(p + a.N, w, cnt, vec);
+    float g[8], w[8];
+    x.g.get(g);
+    x.u.get(w);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       float v, d;
       act_value_grad<FAST>(a.act, g[i], v, d);
-      dg[i] = c[i] * w[i] * d;
-      du[i] = c[i] * v;
+      g[i] = c[i] * w[i] * d;
+      w[i] = c[i] * v;
     }
     T* o = static_cast<T*>(a.out) + m * a.ldo + n;
-    store8(o, dg, cnt, vec);
-    store8(o + a.N, du, cnt, vec);
+    store8(o, g);
+    store8(o + a.N, w);
+  }
+}
+
+// The same for one element n < N, at any alignment.
+template <int EPI, typename T>
+__device__ __forceinline__ void finish1(const MmArgs& a, int64_t m, int n, float c, float u) {
+  constexpr bool FAST = sizeof(T) == 2;
+  if constexpr (is_q8(EPI)) {
+    const float sx = a.row_scale[m];
+    c = (float)__builtin_bit_cast(int32_t, c) * (sx * a.col_scale[n]) + (a.bias ? a.bias[n] : 0.0f);
+    if constexpr (EPI == MM_Q8_GATE) {
+      u = (float)__builtin_bit_cast(int32_t, u) * (sx * a.col_scale[a.N + n]) + (a.bias ? a.bias[a.N + n] : 0.0f);
+      c = act_value<false>(a.act, c) * u;
+    }
+    if (a.out_f32)
+      static_cast<float*>(a.out)[m * a.ldo + n] = c;
+    else
+      static_cast<__bf16*>(a.out)[m * a.ldo + n] = (__bf16)c;
+  } else if constexpr (EPI == MM_PLAIN) {
+    if (a.add) c += (float)static_cast<const T*>(a.add)[m * a.ldadd + n];
+    static_cast<T*>(a.out)[m * a.ldo + n] = (T)c;
+  } else if constexpr (EPI == MM_GATE) {
+    if (a.pre) {
+      T* p = static_cast<T*>(a.pre) + m * a.ldpre + n;
+      p[0] = (T)c;
+      p[a.N] = (T)u;
+    }
+    static_cast<T*>(a.out)[m * a.ldo + n] = (T)(act_value<FAST>(a.act, c) * u);
+  } else {
+    const T* p = static_cast<const T*>(a.pre) + m * a.ldpre + n;
+    const float g = (float)p[0], w = (float)p[a.N];
+    float v, d;
+    act_value_grad<FAST>(a.act, g, v, d);
+    T* o = static_cast<T*>(a.out) + m * a.ldo + n;
+    o[0] = (T)(c * w * d);
+    o[a.N] = (T)(c * v);
   }
 }
 
@@ -234,60 +285,98 @@ __host__ __device__ __forceinline__ int64_t partial_ld(int N) {
   return is_gate(EPI) ? 2 * partial_half(N) : partial_half(N);
 }
 
-// One wave's 64 x 64 block of sums acc[i][j] (rows 32 i + lane % 32, columns
-// 32 j + ...) to the outputs: through 16 KB of LDS, so that a wave reads and
-// writes whole 64-byte (or longer) pieces of rows.  16-byte chunk c of row r
-// is stored at c ^ (r & 15).  Gated: columns 0..31 are gate sums, 32..63 the
-// up sums of the same outputs.  m0, n0: first row and first output column.
-template <int EPI, typename T, typename A16>
-__device__ __forceinline__ void store_block(const MmArgs& a, const A16& a00, const A16& a01, const A16& a10,
-                                            const A16& a11, char* stage, int m0, int n0, int split, int lane) {
-  typedef typename Ty<T>::acc_t acc_t;
+// One wave's sums acc[i][j], NB x NB blocks of 32 x 32 (rows 32 i + lane % 32,
+// columns 32 j + ...), to the outputs: through 4 NB^2 KB of LDS, so that a wave
+// reads and writes whole pieces of rows.  A stage row is 8 NB chunks of 16
+// bytes, chunk c of row r stored at c ^ (r & (8 NB - 1)).  Gated: the first
+// half of the columns are gate sums, the second the up sums of the same
+// outputs.
+template <int NB>
+__device__ __forceinline__ const char* chunk_at(const char* stage, int row, int c) {
+  return stage + row * (128 * NB) + ((c ^ (row & (8 * NB - 1))) << 4);
+}
+template <typename acc_t, int NB, typename A16>
+__device__ __forceinline__ void stage_block(const A16 (&acc)[NB][NB], char* stage, int lane) {
+  typedef acc_t acc4 __attribute__((ext_vector_type(4)));
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < NB; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const A16& b = i == 0 ? (j == 0 ? a00 : a01) : (j == 0 ? a10 : a11);
-      const int row = 32 * i + (lane & 31);
+    for (int j = 0; j < NB; ++j)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int c = 8 * j + 2 * q + (lane >> 5);
-        typedef acc_t acc4 __attribute__((ext_vector_type(4)));
-        *reinterpret_cast<acc4*>(stage + row * 256 + ((c ^ (row & 15)) << 4)) =
+        const A16& b = acc[i][j];
+        *reinterpret_cast<acc4*>(
+            const_cast<char*>(chunk_at<NB>(stage, 32 * i + (lane & 31), 8 * j + 2 * q + (lane >> 5)))) =
             acc4{b[4 * q], b[4 * q + 1], b[4 * q + 2], b[4 * q + 3]};
       }
-    }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
-  constexpr int CH = is_gate(EPI) ? 4 : 8;  // 8-column chunks a row
-  constexpr int RP = 64 / CH;               // rows a pass
-  const int ch = lane % CH;
+}
+// 8 sums of a row from the stage, from chunk c on
+template <int NB>
+__device__ __forceinline__ void unstage8(const char* stage, int row, int c, float* v) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const f32x4 x = *reinterpret_cast<const f32x4*>(chunk_at<NB>(stage, row, c + h));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[4 * h + e] = x[e];
+  }
+}
+template <int NB>
+__device__ __forceinline__ float unstage1(const char* stage, int row, int col) {
+  return *reinterpret_cast<const float*>(chunk_at<NB>(stage, row, col / 4) + (col % 4) * 4);
+}
+// The staged block to the outputs; m0, n0: its first row and output column.
+template <int EPI, typename T, int NB>
+__device__ __forceinline__ void write_block(const MmArgs& a, const char* stage, int m0, int n0, int split, int lane) {
+  constexpr int ROWS = 32 * NB, COLS = is_gate(EPI) ? 16 * NB : 32 * NB;
+  constexpr int CH = COLS / 8, RP = 64 / CH, NP = ROWS / RP;  // chunks of 8 columns, rows a pass, passes
+  const int ch = lane % CH, r0 = lane / CH;
   const int n = n0 + 8 * ch;
-  if (n < a.N) {
+  if (a.splits > 1) {
+#pragma unroll 1
+    for (int it = 0; it < NP; ++it) {
+      const int row = it * RP + r0;
+      if (n < a.N && m0 + row < a.M) {
+        float c[8];
+        float* p = a.work + ((int64_t)split * a.M + m0 + row) * partial_ld<EPI>(a.N) + n;
+        unstage8<NB>(stage, row, 2 * ch, c);
+        store8(p, c);
+        if constexpr (is_gate(EPI)) {
+          unstage8<NB>(stage, row, COLS / 4 + 2 * ch, c);
+          store8(p + partial_half(a.N), c);
+        }
+      }
+    }
+  } else if (a.vec_out) {
+    // what the rows read besides the sums is asked for all passes of a turn together
+    constexpr int NT = NP < 4 ? NP : 4;
+    const int nc = min(n, a.N - 8);  // columns past the end read others and write nothing
+    Cols<EPI, T> cols;
+    cols.load(a, nc);
+#pragma unroll 1
+    for (int it = 0; it < NP; it += NT) {
+      Extra<EPI, T> x[NT];
 #pragma unroll
-    for (int it = 0; it < 64 / RP; ++it) {
-      const int row = it * RP + lane / CH;
-      const int m = m0 + row;
-      if (m < a.M) {
+      for (int b = 0; b < NT; ++b) x[b].load(a, min(m0 + (it + b) * RP + r0, a.M - 1), nc);
+#pragma unroll
+      for (int b = 0; b < NT; ++b) {
+        const int row = (it + b) * RP + r0;
         float c[8], u[8];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const f32x4 v = *reinterpret_cast<const f32x4*>(stage + row * 256 + (((2 * ch + h) ^ (row & 15)) << 4));
-#pragma unroll
-          for (int e = 0; e < 4; ++e) c[4 * h + e] = v[e];
-          if constexpr (is_gate(EPI)) {
-            const f32x4 w = *reinterpret_cast<const f32x4*>(stage + row * 256 + (((8 + 2 * ch + h) ^ (row & 15)) << 4));
-#pragma unroll
-            for (int e = 0; e < 4; ++e) u[4 * h + e] = w[e];
-          }
-        }
-        if (a.splits > 1) {
-          float* p = a.work + ((int64_t)split * a.M + m) * partial_ld<EPI>(a.N) + n;
-          store8(p, c, 8, true);
-          if constexpr (is_gate(EPI)) store8(p + partial_half(a.N), u, 8, true);
-        } else {
-          finish8<EPI, T>(a, m, n, c, u);
-        }
+        unstage8<NB>(stage, row, 2 * ch, c);
+        if constexpr (is_gate(EPI)) unstage8<NB>(stage, row, COLS / 4 + 2 * ch, u);
+        if (n < a.N && m0 + row < a.M) finish8<EPI, T>(a, m0 + row, n, c, u, cols, x[b]);
+      }
+    }
+  } else {
+    // a lane takes one output column
+    const int col = lane % COLS;
+    if (n0 + col < a.N) {
+#pragma unroll 1
+      for (int row = lane / COLS; row < ROWS && m0 + row < a.M; row += 64 / COLS) {
+        const float c = unstage1<NB>(stage, row, col);
+        const float u = is_gate(EPI) ? unstage1<NB>(stage, row, COLS + col) : 0.0f;
+        finish1<EPI, T>(a, m0 + row, n0 + col, c, u);
       }
     }
   }
@@ -298,50 +387,63 @@ __device__ __forceinline__ void store_block(const MmArgs& a, const A16& a00, con
 // The sums of a split depth, joined in order of the splits.
 template <int EPI, typename T>
 __global__ __launch_bounds__(256) void join_kernel(MmArgs a) {
-  const int64_t chunks = partial_half(a.N) / 8, total = a.M * chunks;
+  const int64_t half = partial_half(a.N), chunks = half / 8, total = a.M * chunks;
   const int64_t ldp = partial_ld<EPI>(a.N);
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
     const int64_t m = i / chunks;
     const int n = (int)(i % chunks) * 8;
-    float c[8], u[8], v[8];
     const float* p = a.work + m * ldp + n;
-    load8(p, c, 8, true);
-    if constexpr (is_gate(EPI)) load8(p + partial_half(a.N), u, 8, true);
-    for (int s = 1; s < a.splits; ++s) {
-      p += (int64_t)a.M * ldp;
-      load8(p, v, 8, true);
+    Cols<EPI, T> cols;
+    Extra<EPI, T> x;
+    if (a.vec_out) {
+      cols.load(a, n);
+      x.load(a, m, n);
+    }
+    float c[8], u[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c[e] = u[e] = 0.0f;
+#pragma unroll 4
+    for (int s = 0; s < a.splits; ++s, p += (int64_t)a.M * ldp) {
+      Raw8<float> v, w;
+      float f[8], g[8];
+      v.load(p);
+      v.get(f);
+      if constexpr (is_gate(EPI)) {
+        w.load(p + half);
+        w.get(g);
+      }
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        if constexpr (is_q8(EPI))
-          c[e] = __builtin_bit_cast(float, __builtin_bit_cast(int32_t, c[e]) + __builtin_bit_cast(int32_t, v[e]));
-        else
-          c[e] += v[e];
-      }
-      if constexpr (is_gate(EPI)) {
-        load8(p + partial_half(a.N), v, 8, true);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          if constexpr (is_q8(EPI))
-            u[e] = __builtin_bit_cast(float, __builtin_bit_cast(int32_t, u[e]) + __builtin_bit_cast(int32_t, v[e]));
-          else
-            u[e] += v[e];
+        if constexpr (is_q8(EPI)) {
+          c[e] = __builtin_bit_cast(float, __builtin_bit_cast(int32_t, c[e]) + __builtin_bit_cast(int32_t, f[e]));
+          if constexpr (is_gate(EPI))
+            u[e] = __builtin_bit_cast(float, __builtin_bit_cast(int32_t, u[e]) + __builtin_bit_cast(int32_t, g[e]));
+        } else {
+          c[e] += f[e];
+          if constexpr (is_gate(EPI)) u[e] += g[e];
         }
       }
     }
-    finish8<EPI, T>(a, m, n, c, u);
+    if (a.vec_out) {
+      finish8<EPI, T>(a, m, n, c, u, cols, x);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (n + e < a.N) finish1<EPI, T>(a, m, n + e, c[e], u[e]);
+    }
   }
 }
 
 // ------------------------------------------------------------------ loaders --
 // Straight to LDS (base and rows at 16 bytes, the contiguous extent a multiple
-// of 16 bytes): a region is 16 blocks of 1 KB, one load instruction each; wave
-// w of NW issues blocks w PER .. w PER + PER - 1.  grow(r): the operand's row
+// of 16 bytes): a region of R rows is R / 8 blocks of 1 KB, one load instruction
+// each; wave w of NW issues blocks w PER .. w PER + PER - 1.  grow(r): the operand's row
 // (rows-contiguous: element) that region row r holds, relative to P, or -1.
 // Lanes outside the operand have an offset past the descriptor's range and
 // read zeros, so depth past the end adds nothing.
-template <int NW, int ES, bool RM>
+template <int NW, int ES, bool RM, int R = 128>
 struct Dma {
-  static constexpr int PER = 16 / NW;
+  static constexpr int PER = R / 8 / NW;
   const char* base;
   __amdgpu_buffer_rsrc_t rsrc;
   int64_t ldb;
@@ -364,8 +466,9 @@ struct Dma {
         kofs[p] = c * (16 / ES);
         voff[p] = g < 0 ? kOob : (uint32_t)(g * ldb + c * 16);
       } else {
-        const int k = b * 4 + lane / 16;
-        const int col = ((((lane % 16) >> 1) ^ rmaj_x<128>(k)) << 4) + (lane & 1) * 8;
+        constexpr int LPK = R / 8;  // lanes a depth row
+        const int k = b * (64 / LPK) + lane / LPK;
+        const int col = ((((lane % LPK) >> 1) ^ rmaj_x<R>(k)) << 4) + (lane & 1) * 8;
         const int64_t g = grow(col);
         kofs[p] = k;
         voff[p] = g < 0 ? kOob : (uint32_t)(k * ldb + g * ES);
@@ -382,31 +485,37 @@ struct Dma {
   }
 };
 
-// Through registers (any alignment and extent): 4 vectors of 16 bytes per
+// 16 bytes of global memory at any alignment
+__device__ __forceinline__ u32x4 load16(const void* p) {
+  typedef u32x4 u32x4_any __attribute__((aligned(1)));
+  return *(const TABPACK_GLOBAL u32x4_any*)p;
+}
+
+// Through registers (any alignment and extent): R / 32 vectors of 16 bytes per
 // thread of 256 and region.  rbound: rows-contiguous operands end there.
-template <typename T, bool RM>
+template <typename T, bool RM, int R = 128>
 struct Reg {
-  static constexpr int VE = Ty<T>::VE;
-  static constexpr int VPR = RM ? 128 / VE : 8;  // vectors per line of the region
+  static constexpr int VE = Ty<T>::VE, NV = R / 32;
+  static constexpr int VPR = RM ? R / VE : 8;  // vectors per line of the region
   const T* base;
   int64_t ld;
-  int64_t row[4];  // operand row (rows-contiguous: element) of the vector, or -1
+  int64_t row[NV];  // operand row (rows-contiguous: element) of the vector, or -1
   int64_t rbound;
-  u32x4 v[4];
+  u32x4 v[NV];
   template <typename F>
   __device__ __forceinline__ void init(const void* P, int64_t ld_, int64_t rbound_, int tid, F grow) {
     base = static_cast<const T*>(P);
     ld = ld_;
     rbound = rbound_;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < NV; ++i) {
       const int q = tid + i * 256;
       row[i] = RM ? grow((q % VPR) * VE) : grow(q / VPR);
     }
   }
   __device__ __forceinline__ void load(int64_t k0, int64_t kend, int tid) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < NV; ++i) {
       const int q = tid + i * 256;
       v[i] = u32x4{0, 0, 0, 0};
       int64_t left;  // elements of the vector that exist
@@ -421,7 +530,7 @@ struct Reg {
         p = base + row[i] * ld + k;
       }
       if (left >= VE) {
-        __builtin_memcpy(&v[i], p, 16);
+        v[i] = load16(p);
       } else if (left > 0) {
         T e[VE];
 #pragma unroll
@@ -432,15 +541,15 @@ struct Reg {
   }
   __device__ __forceinline__ void store(char* lds, int tid) const {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < NV; ++i) {
       const int q = tid + i * 256;
       int off;
       if constexpr (!RM)
         off = kmaj16_off<4>(q / VPR, q % VPR);
       else if constexpr (sizeof(T) == 2)
-        off = rmaj_off<128>(q / VPR, (q % VPR) * VE);
+        off = rmaj_off<R>(q / VPR, (q % VPR) * VE);
       else
-        off = (q / VPR) * 512 + (q % VPR) * 16;
+        off = (q / VPR) * (4 * R) + (q % VPR) * 16;
       *reinterpret_cast<u32x4*>(lds + off) = v[i];
     }
   }
@@ -463,15 +572,15 @@ __device__ __forceinline__ void mma(bf16x8 b, bf16x8 a, f32x16& acc, float) {
 
 // The 16 bytes that lane needs of rows row .. row + 31 of a region for MFMA
 // step ks of 4, in inline assembly (see gemm_tiles.h): the caller waits.
-template <bool RM>
+template <bool RM, int R>
 __device__ __forceinline__ bf16x8 frag_asm(const char* lds, int row, int ks, int lane) {
   if constexpr (RM)
-    return frag_tr_asm<128>(lds, row, ks, lane);
+    return frag_tr_asm<R>(lds, row, ks, lane);
   else
     return frag_kmaj_asm<4>(lds, row, ks, lane);
 }
 // The same as ordinary reads, for regions that were written through registers.
-template <typename T, bool RM>
+template <typename T, bool RM, int R>
 __device__ __forceinline__ bf16x8 frag_reg(const char* lds, int row, int ks, int lane) {
   if constexpr (!RM) {
     return *reinterpret_cast<const bf16x8*>(lds + kmaj16_off<4>(row + (lane & 31), 2 * ks + (lane >> 5)));
@@ -480,24 +589,27 @@ __device__ __forceinline__ bf16x8 frag_reg(const char* lds, int row, int ks, int
     const int k = 16 * ks + 8 * (g >> 1) + (s >> 2);
     const int col = row + 16 * (g & 1) + 4 * (s & 3);
     typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
-    const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(lds + rmaj_off<128>(k, col)));
-    const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(lds + rmaj_off<128>(k + 4, col)));
+    const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(lds + rmaj_off<R>(k, col)));
+    const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(lds + rmaj_off<R>(k + 4, col)));
     const u32x2 x = __builtin_bit_cast(u32x2, lo), y = __builtin_bit_cast(u32x2, hi);
     return __builtin_bit_cast(bf16x8, u32x4{x[0], x[1], y[0], y[1]});
-  } else {  // fp32 [32 depth rows][128]
+  } else {  // fp32 [32 depth rows][R]
     f32x4 f;
     const int k = 8 * ks + 4 * (lane >> 5);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) f[e] = *reinterpret_cast<const float*>(lds + (k + e) * 512 + (row + (lane & 31)) * 4);
+    for (int e = 0; e < 4; ++e) f[e] = *reinterpret_cast<const float*>(lds + (k + e) * (4 * R) + (row + (lane & 31)) * 4);
     return __builtin_bit_cast(bf16x8, f);
   }
 }
 
 // Every LDS read of this wave but the last N is done; the fragments named are
 // tied to the wait, so no use of them moves before it.
-template <int N>
-__device__ __forceinline__ void wait_lds(bf16x8& a, bf16x8& b, bf16x8& c, bf16x8& d) {
-  asm volatile("s_waitcnt lgkmcnt(%4)" : "+v"(a), "+v"(b), "+v"(c), "+v"(d) : "n"(N < 15 ? N : 15));
+template <int N, int NB>
+__device__ __forceinline__ void wait_lds(bf16x8 (&a)[NB], bf16x8 (&b)[NB]) {
+  if constexpr (NB == 2)
+    asm volatile("s_waitcnt lgkmcnt(%4)" : "+v"(a[0]), "+v"(a[1]), "+v"(b[0]), "+v"(b[1]) : "n"(N < 15 ? N : 15));
+  else
+    asm volatile("s_waitcnt lgkmcnt(%2)" : "+v"(a[0]), "+v"(b[0]) : "n"(N < 15 ? N : 15));
 }
 
 template <typename A16>
@@ -525,60 +637,74 @@ __device__ __forceinline__ Where where(const MmArgs& a) {
   return w;
 }
 
-// ------------------------------------------------------------- small tiles --
-template <typename T, bool RA, bool RB, int EPI, bool DMA>
-__global__ __launch_bounds__(256, 2) void small_kernel(MmArgs a) {
-  constexpr int ES = sizeof(T), KE = kStep / ES;
-  __shared__ __attribute__((aligned(16))) char smem[4 * kRegion];
+// ---------------------------------------------------- small and mini tiles --
+// 64 NB x 64 NB tiles on 4 waves (2 x 2) of NB x NB 32 x 32 blocks.
+template <typename T, bool RA, bool RB, int EPI, bool DMA, int NB, int NS>
+__global__ __launch_bounds__(256, NB * NS == 8 ? 1 : NB * NS == 4 ? 2 : 4) void small_kernel(MmArgs a) {
+  constexpr int ES = sizeof(T), KE = kStep / ES, R = 64 * NB, REGION = R * kStep, W = 32 * NB;
+  static_assert(DMA || NS == 2, "two stages through registers");
+  __shared__ __attribute__((aligned(16))) char smem[2 * NS * REGION];
   typedef typename Ty<T>::acc16 acc16;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave >> 1, wn = wave & 1;
   const Where w = where(a);
-  const int m0 = w.tm * 128, n0 = w.tn * (is_gate(EPI) ? 64 : 128);
+  const int m0 = w.tm * R, n0 = w.tn * (is_gate(EPI) ? R / 2 : R);
   const int64_t kbeg = (int64_t)w.split * a.steps_per_split * KE;
   const int64_t kend = min((int64_t)a.K, kbeg + (int64_t)a.steps_per_split * KE);
   const int nk = (int)((kend - kbeg + KE - 1) / KE);
   auto grow_a = [&](int r) -> int64_t { return m0 + r < a.M ? r : -1; };
-  // region row wn 64 + j 32 + x: plain column n0 + that; gated: gate (j = 0) or
-  // up (j = 1) row of output n0 + wn 32 + x
+  // region row of B wn W + x: plain column n0 + that; gated: x < W / 2 the gate
+  // row of output n0 + wn W / 2 + x, the others the up rows of the same outputs
   auto grow_b = [&](int r) -> int64_t {
     if constexpr (!is_gate(EPI)) return n0 + r < a.N ? r : -1;
-    const int x = (r >> 6) * 32 + (r & 31);
-    return n0 + x < a.N ? x + ((r >> 5) & 1 ? (int64_t)a.N : 0) : -1;
+    const int x = (r / W) * (W / 2) + r % (W / 2);
+    return n0 + x < a.N ? x + ((r % W) >= W / 2 ? (int64_t)a.N : 0) : -1;
   };
   const T* A = static_cast<const T*>(a.A) + (RA ? (int64_t)m0 : m0 * a.lda);
   const T* B = static_cast<const T*>(a.B) + (RB ? (int64_t)n0 : n0 * a.ldb);
-  acc16 acc[2][2];
+  acc16 acc[NB][NB];
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < NB; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) clear(acc[i][j]);
+    for (int j = 0; j < NB; ++j) clear(acc[i][j]);
   if constexpr (DMA) {
-    Dma<4, ES, RA> la;
-    Dma<4, ES, RB> lb;
+    Dma<4, ES, RA, R> la;
+    Dma<4, ES, RB, R> lb;
     la.init(A, a.lda, wave, lane, grow_a);
     lb.init(B, a.ldb, wave, lane, grow_b);
-    auto issue = [&](char* st, int64_t k0) {
+    auto issue = [&](char* st, int64_t k0, int q) {  // quarter q of a step's loads
 #pragma unroll
-      for (int p = 0; p < 4; ++p) la.issue(st, k0, kend, p);
-#pragma unroll
-      for (int p = 0; p < 4; ++p) lb.issue(st + kRegion, k0, kend, p);
+      for (int p = 0; p < NB; ++p) {
+        if (q < 2)
+          la.issue(st, k0, kend, q * NB + p);
+        else
+          lb.issue(st + REGION, k0, kend, (q - 2) * NB + p);
+      }
     };
-    constexpr int NRD = (RA ? 4 : 2) + (RB ? 4 : 2);  // LDS reads per MFMA step
-    issue(smem, kbeg);
+    constexpr int NRD = (RA ? 2 * NB : NB) + (RB ? 2 * NB : NB);  // LDS reads per MFMA step
+#pragma unroll
+    for (int st = 0; st < NS - 1; ++st)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) issue(smem + st * 2 * REGION, kbeg + (int64_t)st * KE, q);
+    int at = 0;  // this step's stage
 #pragma unroll 1
     for (int kt = 0; kt < nk; ++kt) {
-      char* const cur = smem + (kt & 1) * 2 * kRegion;
-      wait_vm<0, true>();
-      bar();  // this step has landed, and every wave is done with the last one
-      if (kt + 1 < nk) issue(smem + ((kt + 1) & 1) * 2 * kRegion, kbeg + (int64_t)(kt + 1) * KE);
-      bf16x8 fa[4][2], fb[4][2];
+      char* const cur = smem + at * 2 * REGION;
+      wait_vm<(NS - 2) * 4 * NB, true>();
+      bar();  // this step has landed, and every wave is done with the last one, whose stage is asked for again
+      char* const ahead = smem + (at ? at - 1 : NS - 1) * 2 * REGION;
+      at = at + 1 < NS ? at + 1 : 0;
+      if constexpr (NS == 2) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) issue(ahead, kbeg + (int64_t)(kt + 1) * KE, q);
+      }
+      bf16x8 fa[4][NB], fb[4][NB];
       auto rd = [&](int ks) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) fa[ks][i] = frag_asm<RA>(cur, wm * 64 + i * 32, ks, lane);
+        for (int i = 0; i < NB; ++i) fa[ks][i] = frag_asm<RA, R>(cur, wm * W + i * 32, ks, lane);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) fb[ks][j] = frag_asm<RB>(cur + kRegion, wn * 64 + j * 32, ks, lane);
+        for (int j = 0; j < NB; ++j) fb[ks][j] = frag_asm<RB, R>(cur + REGION, wn * W + j * 32, ks, lane);
       };
       rd(0);
       rd(1);
@@ -587,31 +713,37 @@ __global__ __launch_bounds__(256, 2) void small_kernel(MmArgs a) {
         if (ks + 2 < 4) rd(ks + 2);
         __builtin_amdgcn_sched_barrier(0);
         if (ks < 2)
-          wait_lds<2 * NRD>(fa[ks][0], fa[ks][1], fb[ks][0], fb[ks][1]);
+          wait_lds<2 * NRD>(fa[ks], fb[ks]);
         else if (ks == 2)
-          wait_lds<NRD>(fa[ks][0], fa[ks][1], fb[ks][0], fb[ks][1]);
+          wait_lds<NRD>(fa[ks], fb[ks]);
         else
-          wait_lds<0>(fa[ks][0], fa[ks][1], fb[ks][0], fb[ks][1]);
+          wait_lds<0>(fa[ks], fb[ks]);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < NB; ++i)
 #pragma unroll
-          for (int j = 0; j < 2; ++j) mma(fb[ks][j], fa[ks][i], acc[i][j], T());
+          for (int j = 0; j < NB; ++j) mma(fb[ks][j], fa[ks][i], acc[i][j], T());
         __builtin_amdgcn_sched_barrier(0);
+        if constexpr (NS > 2) {
+          // (with steps to spare the loads go between the products: in one burst
+          // they fill the address unit's queue and hold the reads up)
+          issue(ahead, kbeg + (int64_t)(kt + NS - 1) * KE, ks);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
     }
   } else {
-    Reg<T, RA> la;
-    Reg<T, RB> lb;
+    Reg<T, RA, R> la;
+    Reg<T, RB, R> lb;
     la.init(A, a.lda, a.M - m0, tid, grow_a);
     lb.init(B, a.ldb, a.N - n0, tid, grow_b);
     la.load(kbeg, kend, tid);
     lb.load(kbeg, kend, tid);
 #pragma unroll 1
     for (int kt = 0; kt < nk; ++kt) {
-      char* const cur = smem + (kt & 1) * 2 * kRegion;
+      char* const cur = smem + (kt & 1) * 2 * REGION;
       la.store(cur, tid);
-      lb.store(cur + kRegion, tid);
+      lb.store(cur + REGION, tid);
       __syncthreads();  // the other stage was read before the barrier of the step before this one's stores
       if (kt + 1 < nk) {
         la.load(kbeg + (int64_t)(kt + 1) * KE, kend, tid);
@@ -619,47 +751,384 @@ __global__ __launch_bounds__(256, 2) void small_kernel(MmArgs a) {
       }
 #pragma unroll
       for (int ks = 0; ks < 4; ++ks) {
-        bf16x8 fa[2], fb[2];
+        bf16x8 fa[NB], fb[NB];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) fa[i] = frag_reg<T, RA>(cur, wm * 64 + i * 32, ks, lane);
+        for (int i = 0; i < NB; ++i) fa[i] = frag_reg<T, RA, R>(cur, wm * W + i * 32, ks, lane);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) fb[j] = frag_reg<T, RB>(cur + kRegion, wn * 64 + j * 32, ks, lane);
+        for (int j = 0; j < NB; ++j) fb[j] = frag_reg<T, RB, R>(cur + REGION, wn * W + j * 32, ks, lane);
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < NB; ++i)
 #pragma unroll
-          for (int j = 0; j < 2; ++j) mma(fb[j], fa[i], acc[i][j], T());
+          for (int j = 0; j < NB; ++j) mma(fb[j], fa[i], acc[i][j], T());
       }
     }
   }
   wait_vm<0, true>();
   bar();  // the sums are staged in the operand regions
-  store_block<EPI, T>(a, acc[0][0], acc[0][1], acc[1][0], acc[1][1], smem + wave * 16384, m0 + wm * 64,
-                      n0 + wn * (is_gate(EPI) ? 32 : 64), w.split, lane);
+  char* const stage = smem + wave * (4096 * NB * NB);
+  stage_block<typename Ty<T>::acc_t, NB>(acc, stage, lane);
+  write_block<EPI, T, NB>(a, stage, m0 + wm * W, n0 + wn * (is_gate(EPI) ? W / 2 : W), w.split, lane);
+}
+
+// -------------------------------------------------------------- huge tiles --
+// LDS addresses of a wave's fragments of one operand inside a region; what is
+// a constant distance goes into the instruction's offset.  Depth-contiguous:
+// v[ks], row block i 4 KB on (32 rows do not change the swizzle).
+// Rows-contiguous: v[i], MFMA step ks 4 KB on.
+template <bool RM, int NI>
+struct FragAddr {
+  uint32_t v[RM ? NI : 4];
+  __device__ __forceinline__ void init(const char* lds, int row0, int lane) {
+    typedef __attribute__((address_space(3))) const char* lds_cptr;
+    const uint32_t base = (uint32_t)(uintptr_t)(lds_cptr)lds;
+    if constexpr (!RM) {
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) v[ks] = base + kmaj16_off<4>(row0 + (lane & 31), 2 * ks + (lane >> 5));
+    } else {
+      const int s = lane & 15, g = lane >> 4;
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+        v[i] = base + rmaj_off<128>(8 * (g >> 1) + (s >> 2), row0 + 32 * i + 16 * (g & 1) + 4 * (s & 3));
+    }
+  }
+  template <int I, int KS>
+  __device__ __forceinline__ void read(bf16x8& f, uint32_t region) const {
+    if constexpr (!RM) {
+      u32x4 r;
+      asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(r) : "v"(v[KS] + region), "n"(I * 4096));
+      f = __builtin_bit_cast(bf16x8, r);
+    } else {
+      u32x2 x, y;
+      asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(x) : "v"(v[I] + region), "n"(KS * 4096));
+      asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(y) : "v"(v[I] + region), "n"(KS * 4096 + 1024));
+      f = __builtin_bit_cast(bf16x8, u32x4{x[0], x[1], y[0], y[1]});
+    }
+  }
+  // the fragments of row block I of the region at byte `region`
+  template <int I>
+  __device__ __forceinline__ void read4(bf16x8 (&f)[4], uint32_t region) const {
+    read<I, 0>(f[0], region);
+    read<I, 1>(f[1], region);
+    read<I, 2>(f[2], region);
+    read<I, 3>(f[3], region);
+  }
+};
+__device__ __forceinline__ void tie(bf16x8 (&f)[4]) {
+  asm volatile("" : "+v"(f[0]), "+v"(f[1]), "+v"(f[2]), "+v"(f[3]));
+}
+
+// 256 x 256 tiles on 8 waves (2 x 4, two to a SIMD), each 128 x 64.  A K step
+// is two phases, one half (64 x 64) of the wave's sums each; a phase is a read
+// part (the half's fragments from LDS) and a product part (16 MFMAs, with the
+// loads of later steps between them), with a barrier after each.  The waves of
+// the tile's lower half run one part behind those of the upper half, so on
+// every SIMD one wave's products run beside the other's reads; the wave with
+// products has priority.
+// The 16 KB regions are numbered A half 0, B half 0, B half 1, A half 1 of step
+// 0, of step 1, ...: region n lies in slot n % 10 of LDS; phase g asks for the
+// regions 2 g + 8 and 2 g + 9.  When the reads of phase g end, those up to 2 g +
+// 7 have been asked for and the next phase needs region 2 g + 3 (g even) or
+// 2 g + 4: the newest 4 or 3 may be in flight, vmcnt(8) or (6) (two loads a
+// region and wave) before the barrier.  A slot is asked for again in the phase
+// after its last reads at the earliest, in the product part, when the lagging
+// waves have finished theirs.
+template <typename T, bool RA, bool RB, int EPI>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void huge_kernel(MmArgs a) {
+  constexpr int ES = sizeof(T), KE = kStep / ES, SLOTS = 10;
+  __shared__ __attribute__((aligned(16))) char smem[SLOTS * kRegion];
+  typedef typename Ty<T>::acc16 acc16;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave >> 2, wn = wave & 3;
+  const Where w = where(a);
+  const int m0 = w.tm * 256, n0 = w.tn * (is_gate(EPI) ? 128 : 256);
+  const int64_t kbeg = (int64_t)w.split * a.steps_per_split * KE;
+  const int64_t kend = min((int64_t)a.K, kbeg + (int64_t)a.steps_per_split * KE);
+  const int nk = (int)((kend - kbeg + KE - 1) / KE);
+  const T* A = static_cast<const T*>(a.A) + (RA ? (int64_t)m0 : m0 * a.lda);
+  const T* B = static_cast<const T*>(a.B) + (RB ? (int64_t)n0 : n0 * a.ldb);
+  Dma<8, ES, RA> la[2];
+  Dma<8, ES, RB> lb[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    // A half h: the rows of phases 2h, 2h + 1 of both wave rows; B half h: the
+    // columns of two phases of every wave column (gated: gate rows, up rows)
+    la[h].init(A, a.lda, wave, lane, [&](int r) -> int64_t {
+      const int x = (r >> 6) * 128 + h * 64 + (r & 63);
+      return m0 + x < a.M ? x : -1;
+    });
+    lb[h].init(B, a.ldb, wave, lane, [&](int r) -> int64_t {
+      if constexpr (is_gate(EPI)) return n0 + r < a.N ? r + (h ? (int64_t)a.N : 0) : -1;
+      const int x = (r >> 5) * 64 + h * 32 + (r & 31);
+      return n0 + x < a.N ? x : -1;
+    });
+  }
+  auto ask_a = [&](int h, int step, int slot, int p) {
+    la[h].issue(smem + slot * kRegion, kbeg + (int64_t)step * KE, kend, p);
+  };
+  auto ask_b = [&](int h, int step, int slot, int p) {
+    lb[h].issue(smem + slot * kRegion, kbeg + (int64_t)step * KE, kend, p);
+  };
+  FragAddr<RA, 2> fa;
+  FragAddr<RB, 1> fb;
+  fa.init(smem, wm * 64, lane);
+  fb.init(smem, wn * 32, lane);
+  acc16 acc[2][2][2];  // [A half][32-row block][B half]
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) clear(acc[h][i][j]);
+#pragma unroll
+  for (int n = 0; n < 8; ++n)
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      if (n % 4 == 0 || n % 4 == 3)
+        ask_a(n % 4 == 3, n / 4, n, p);
+      else
+        ask_b(n % 4 == 2, n / 4, n, p);
+    }
+  wait_vm<10, false>();
+  bar();
+  if (wm == 1) bar();
+  bf16x8 x0[4], x1[4], y0[4], y1[4];  // A row blocks 0 and 1 of the half; B halves
+  // end of a phase's reads, and its products
+  auto products = [&](acc16 (&c)[2][2], auto vm, auto ask) {
+    __builtin_amdgcn_sched_barrier(0);
+    wait_vm<decltype(vm)::value, false>();
+    bar();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    tie(x0);
+    tie(x1);
+    tie(y0);
+    tie(y1);
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+      mma(y0[ks], x0[ks], c[0][0], T());
+      mma(y0[ks], x1[ks], c[1][0], T());
+      mma(y1[ks], x0[ks], c[0][1], T());
+      __builtin_amdgcn_sched_barrier(0);
+      ask(ks);
+      __builtin_amdgcn_sched_barrier(0);
+      mma(y1[ks], x1[ks], c[1][1], T());
+    }
+    __builtin_amdgcn_s_setprio(0);
+    __builtin_amdgcn_sched_barrier(0);
+    bar();
+  };
+  int slot = 0;  // of the step's first region
+  auto after = [](int sl, int n) { return sl + n < SLOTS ? sl + n : sl + n - SLOTS; };
+#pragma unroll 1
+  for (int kt = 0; kt < nk; ++kt) {
+    fa.template read4<0>(x0, slot * kRegion);
+    fa.template read4<1>(x1, slot * kRegion);
+    fb.template read4<0>(y0, after(slot, 1) * kRegion);
+    fb.template read4<0>(y1, after(slot, 2) * kRegion);
+    products(acc[0], std::integral_constant<int, 8>{}, [&](int q) {
+      if (q < 2)
+        ask_a(0, kt + 2, after(slot, 8), q);
+      else
+        ask_b(0, kt + 2, after(slot, 9), q - 2);
+    });
+    fa.template read4<0>(x0, after(slot, 3) * kRegion);
+    fa.template read4<1>(x1, after(slot, 3) * kRegion);
+    products(acc[1], std::integral_constant<int, 6>{}, [&](int q) {
+      if (q < 2)
+        ask_b(1, kt + 2, slot, q);
+      else
+        ask_a(1, kt + 2, after(slot, 1), q - 2);
+    });
+    slot = after(slot, 4);
+  }
+  if (wm == 0) bar();
+  wait_vm<0, true>();
+  bar();  // the sums are staged in the operand regions
+  char* const stage = smem + wave * 16384;
+#pragma unroll 1
+  for (int h = 0; h < 2; ++h) {
+    if (h == 0)
+      stage_block<typename Ty<T>::acc_t, 2>(acc[0], stage, lane);
+    else
+      stage_block<typename Ty<T>::acc_t, 2>(acc[1], stage, lane);
+    write_block<EPI, T, 2>(a, stage, m0 + wm * 128 + h * 64, n0 + wn * (is_gate(EPI) ? 32 : 64), w.split, lane);
+  }
+}
+
+// -------------------------------------------------------------- thin tiles --
+// Up to 16 rows of A (depth-contiguous operands, bf16 and int8): a workgroup
+// owns 16 columns (gated: 16 gate and 16 up rows of B), its NW waves share the
+// depth in strips of 256 bytes, and every weight byte is read once, straight
+// into MFMA operands (16 x 16 blocks; lane l holds 16 bytes of depth of row
+// l % 16).  The loads bound it: a strip's are all issued before its products,
+// at any alignment.  The waves' sums meet in LDS, added in order.
+__device__ __forceinline__ void mma16(u32x4 b, u32x4 a, f32x4& acc, __bf16) {
+  acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a), acc, 0, 0, 0);
+}
+__device__ __forceinline__ void mma16(u32x4 b, u32x4 a, i32x4& acc, int8_t) {
+  acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, b), __builtin_bit_cast(i32x4, a), acc, 0, 0, 0);
+}
+// 16 bytes of a row from element k on, zeros from kend on
+template <typename T>
+__device__ __forceinline__ u32x4 row16(const T* row, int64_t k, int64_t kend) {
+  constexpr int VE = Ty<T>::VE;
+  u32x4 v{0, 0, 0, 0};
+  if (k + VE <= kend) {
+    v = load16(row + k);
+  } else if (k < kend) {
+    T e[VE];
+#pragma unroll
+    for (int j = 0; j < VE; ++j) e[j] = k + j < kend ? row[k + j] : (T)0;
+    __builtin_memcpy(&v, e, 16);
+  }
+  return v;
+}
+template <typename T, int EPI, int NW>
+__global__ __launch_bounds__(NW * 64) void thin_kernel(MmArgs a) {
+  constexpr int G = is_gate(EPI) ? 2 : 1, ES = sizeof(T), STRIP = 256 / ES, UNIT = 64 / ES;
+  typedef typename Ty<T>::acc_t acc_t;
+  typedef acc_t acc4 __attribute__((ext_vector_type(4)));
+  __shared__ acc4 sums[NW][G][64];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n0 = blockIdx.x * 16;
+  const int64_t K = a.K;
+  // rows and columns past the end read the last one; their sums are not used
+  const T* wrow[G];
+  const T* const xrow = static_cast<const T*>(a.A) + min(lane % 16, a.M - 1) * a.lda;
+  const int64_t kl = (lane / 16) * (16 / ES);  // the lane's depth inside a unit
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+    wrow[g] = static_cast<const T*>(a.B) + (min(n0 + lane % 16, a.N - 1) + (int64_t)g * a.N) * a.ldb;
+  acc4 acc[G];
+#pragma unroll
+  for (int g = 0; g < G; ++g) acc[g] = acc4{0, 0, 0, 0};
+  struct Strip {
+    u32x4 w[G][4], x[4];
+  };
+  const int64_t strips = (K + STRIP - 1) / STRIP;
+  auto load = [&](Strip& f, int64_t st) {
+    const int64_t k0 = st * STRIP + kl;
+    if ((st + 1) * STRIP <= K) {  // the same for the whole wave
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+#pragma unroll
+        for (int g = 0; g < G; ++g) f.w[g][u] = load16(wrow[g] + k0 + u * UNIT);
+        f.x[u] = load16(xrow + k0 + u * UNIT);
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+#pragma unroll
+        for (int g = 0; g < G; ++g) f.w[g][u] = row16(wrow[g], k0 + u * UNIT, K);
+        f.x[u] = row16(xrow, k0 + u * UNIT, K);
+      }
+    }
+  };
+  auto products = [&](const Strip& f) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int g = 0; g < G; ++g) mma16(f.w[g][u], f.x[u], acc[g], T());
+  };
+  // the next strip is asked for before the products of the present one
+  if (wave < strips) {
+    Strip f, next;
+    load(f, wave);
+    for (int64_t st = wave; st < strips; st += NW) {
+      const bool more = st + NW < strips;
+      if (more) load(next, st + NW);
+      products(f);
+      if (more) f = next;
+    }
+  }
+#pragma unroll
+  for (int g = 0; g < G; ++g) sums[wave][g][lane] = acc[g];
+  __syncthreads();
+  // lane of the first wave: row lane % 16, columns n0 + 4 (lane / 16) ..  + 3
+  const int m = lane % 16, n = n0 + 4 * (lane / 16);
+  if (tid >= 64 || m >= a.M) return;
+  acc4 c = sums[0][0][lane], u = sums[0][G - 1][lane];
+#pragma unroll
+  for (int q = 1; q < NW; ++q) {
+    c += sums[q][0][lane];
+    if constexpr (G == 2) u += sums[q][1][lane];
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const acc_t ce = c[e], ue = u[e];
+    if (n + e < a.N) finish1<EPI, T>(a, m, n + e, __builtin_bit_cast(float, ce), __builtin_bit_cast(float, ue));
+  }
 }
 
 // ------------------------------------------------------------------- host --
+enum Tiles { TILES_THIN, TILES_MINI, TILES_SMALL, TILES_HUGE };
+// How a product is laid out over workgroups.
 struct Plan {
-  int tm, tn, splits, steps;
+  Tiles tiles;
+  int64_t tm, tn;
+  int splits, steps;  // workgroups that share a tile's depth, K steps of each
 };
 
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 int elem_bytes(MmType t) { return t == MM_BF16 ? 2 : t == MM_FP32 ? 4 : 1; }
 
-// Tiles of a product and how many workgroups share each tile's depth: as many
-// as fill the chip's 512 small-tile places, at least 8 steps each.
-Plan plan_small(MmType type, const MmArgs& a) {
+int64_t depth_steps(MmType type, const MmArgs& a) {
+  return a.K > 0 ? cdiv((int64_t)a.K * elem_bytes(type), kStep) : 1;
+}
+
+Plan plan_with(MmType type, const MmArgs& a, Tiles t, int64_t splits) {
+  const int side = t == TILES_HUGE ? 256 : t == TILES_SMALL ? 128 : 64;
   Plan p;
-  p.tm = (int)cdiv(a.M, 128);
-  p.tn = (int)cdiv(a.N, is_gate(a.epi) ? 64 : 128);
-  const int64_t steps = a.K > 0 ? cdiv((int64_t)a.K * elem_bytes(type), kStep) : 1;
-  const int64_t tiles = std::max((int64_t)p.tm * p.tn, (int64_t)1);  // (no rows: a workspace query)
-  int64_t s = tiles >= 256 ? 1 : 512 / tiles;
-  s = s < steps / 8 ? s : steps / 8;
-  if (s < 1) s = 1;
-  p.steps = (int)cdiv(steps, s);
+  p.tiles = t;
+  p.tm = t == TILES_THIN ? 1 : cdiv(a.M, side);
+  p.tn = t == TILES_THIN ? cdiv(a.N, 16) : cdiv(a.N, is_gate(a.epi) ? side / 2 : side);
+  const int64_t steps = depth_steps(type, a);
+  splits = std::max((int64_t)1, std::min(splits, steps));
+  p.steps = (int)cdiv(steps, splits);
   p.splits = (int)cdiv(steps, p.steps);
   return p;
+}
+
+// The layout that should be fastest.  Up to 16 rows the thin kernel (at depth
+// 1024 and 1024..4096 columns 3.8-5.1 us against 5.6-6.8 on mini tiles; at 32
+// rows it no longer gains: 7.0 / 6.6, depth 4096 13.4 / 9.9 split).  The
+// others by a model of the time in us, fitted to measurements of products of
+// 128..16384 rows, 256..4096 columns and depths 1024..16384: a start, a time per
+// K step that grows with the tiles a CU holds, and the join's traffic.  Mini
+// tiles step in 0.2 us a tile, small ones in 0.6, huge ones in 1.05 on a few
+// CUs and 1.6 where all of them run (the clock falls under their power);
+// operands through registers take 0.37 and 0.8, fp32 0.7 and 2.45.
+Plan choose(MmType type, const MmArgs& a, bool dma) {
+  if (type != MM_FP32 && !a.a_rmaj && !a.b_rmaj && a.M <= 16) return plan_with(type, a, TILES_THIN, 1);
+  Plan best = plan_with(type, a, TILES_MINI, 1);
+  double best_us = 1e30;
+  for (Tiles t : {TILES_MINI, TILES_SMALL, TILES_HUGE}) {
+    if (t == TILES_HUGE && !dma) continue;
+    int64_t last = 0;
+    for (int64_t s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+      const Plan p = plan_with(type, a, t, s);
+      if (p.splits == last || (p.splits > 1 && p.steps < 2)) continue;
+      last = p.splits;
+      const double wgs = (double)p.tm * p.tn * p.splits, held = (double)cdiv((int64_t)wgs, 256);
+      double step;
+      if (t == TILES_HUGE)
+        step = wgs < 256 ? 1.05 + 0.55 * wgs / 256 : 1.6 * held;
+      else if (type == MM_FP32)
+        step = t == TILES_MINI ? std::max(0.85, 0.7 * held) : 2.45 * held;
+      else if (!dma)
+        step = t == TILES_MINI ? std::max(0.5, 0.37 * held) : std::max(0.95, 0.8 * held);
+      else
+        step = (t == TILES_MINI ? 0.2 : 0.6) * held;
+      double us = (t == TILES_HUGE ? 7 : 3.3) + p.steps * step;
+      if (p.splits > 1) us += 2.5 + p.splits * (double)a.M * partial_half(a.N) * (is_gate(a.epi) ? 16 : 8) / 3.5e6;
+      if (us < best_us) best_us = us, best = p;
+    }
+  }
+  return best;
 }
 
 size_t partial_bytes(const MmArgs& a, const Plan& p) {
@@ -682,19 +1151,49 @@ bool can_dma(MmType type, const MmArgs& a) {
   return a.lda * es * 256 < lim && a.ldb * es * brows < lim && (int64_t)a.K * es < lim / 2;
 }
 
+template <typename T, int EPI>
+void launch_thin(const MmArgs& a, dim3 grid, hipStream_t s) {
+  // a wave per 256-byte strip of depth, 4 to 16 of them (gated 8: two strips of
+  // two weight rows do not fit the registers of 16)
+  constexpr int MOST = is_gate(EPI) ? 8 : 16;
+  const int64_t strips = cdiv((int64_t)a.K * (int)sizeof(T), 256);
+  if (strips > 8)
+    hipLaunchKernelGGL((thin_kernel<T, EPI, MOST>), grid, dim3(MOST * 64), 0, s, a);
+  else if (strips > 4)
+    hipLaunchKernelGGL((thin_kernel<T, EPI, 8>), grid, dim3(512), 0, s, a);
+  else
+    hipLaunchKernelGGL((thin_kernel<T, EPI, 4>), grid, dim3(256), 0, s, a);
+}
+
 template <typename T, bool RA, bool RB, int EPI>
 hipError_t launch_tiles(MmType type, MmArgs a, hipStream_t s) {
-  const Plan p = plan_small(type, a);
-  a.tiles_m = p.tm, a.tiles_n = p.tn, a.splits = p.splits, a.steps_per_split = p.steps;
-  const int64_t blocks = (int64_t)p.tm * p.tn * p.splits;
-  if (blocks > (1 << 23)) return hipErrorInvalidConfiguration;  // a launch is limited to 2^32 threads
+  const bool dma = can_dma(type, a);
+  const Plan p = choose(type, a, dma);
+  const int64_t blocks = p.tm * p.tn * p.splits;
+  if (blocks > (1 << 22)) return hipErrorInvalidConfiguration;  // a launch is limited to 2^32 threads
+  if (p.splits > 1 && a.work_bytes < partial_bytes(a, p)) return hipErrorInvalidValue;
+  a.tiles_m = (int)p.tm, a.tiles_n = (int)p.tn, a.splits = p.splits, a.steps_per_split = p.steps;
   const dim3 grid((uint32_t)blocks);
-  bool dma = false;
-  if constexpr (sizeof(T) != 4) {
-    dma = can_dma(type, a);
-    if (dma) hipLaunchKernelGGL((small_kernel<T, RA, RB, EPI, true>), grid, dim3(256), 0, s, a);
+  if constexpr (sizeof(T) != 4 && !RA && !RB) {
+    if (p.tiles == TILES_THIN) {
+      launch_thin<T, EPI>(a, grid, s);
+      return hipGetLastError();
+    }
   }
-  if (!dma) hipLaunchKernelGGL((small_kernel<T, RA, RB, EPI, false>), grid, dim3(256), 0, s, a);
+  if constexpr (sizeof(T) != 4) {
+    if (p.tiles == TILES_HUGE)
+      hipLaunchKernelGGL((huge_kernel<T, RA, RB, EPI>), grid, dim3(512), 0, s, a);
+    else if (dma && p.tiles == TILES_SMALL)
+      hipLaunchKernelGGL((small_kernel<T, RA, RB, EPI, true, 2, 2>), grid, dim3(256), 0, s, a);
+    else if (dma)
+      hipLaunchKernelGGL((small_kernel<T, RA, RB, EPI, true, 1, 4>), grid, dim3(256), 0, s, a);
+  }
+  if (!dma) {
+    if (p.tiles == TILES_SMALL)
+      hipLaunchKernelGGL((small_kernel<T, RA, RB, EPI, false, 2, 2>), grid, dim3(256), 0, s, a);
+    else
+      hipLaunchKernelGGL((small_kernel<T, RA, RB, EPI, false, 1, 2>), grid, dim3(256), 0, s, a);
+  }
   if (p.splits > 1) {
     const int64_t n = cdiv((int64_t)a.M * (partial_half(a.N) / 8), 256);
     hipLaunchKernelGGL((join_kernel<EPI, T>), dim3((uint32_t)(n < 4096 ? n : 4096)), dim3(256), 0, s, a);
@@ -716,7 +1215,10 @@ hipError_t launch_float(MmType type, const MmArgs& a, hipStream_t s) {
 
 }  // namespace
 
-size_t mm_workspace(MmType type, const MmArgs& a) { return partial_bytes(a, plan_small(type, a)); }
+// (whatever the operands' alignment turns out to be)
+size_t mm_workspace(MmType type, const MmArgs& a) {
+  return std::max(partial_bytes(a, choose(type, a, true)), partial_bytes(a, choose(type, a, false)));
+}
 
 hipError_t launch_mm(MmType type, const MmArgs& args, hipStream_t s) {
   MmArgs a = args;
