@@ -370,8 +370,8 @@ int pack_profile_read(pack_handle* h, pack_kernel_stat* out, int32_t max, int32_
  *
  * Matrices are row-major with a leading dimension (elements from one row to
  * the next) of at least the row's length; elements of a row are contiguous.
- * Any alignment of the element type is accepted; where every row starts at a
- * multiple of 16 bytes and its length is one too, 16-byte accesses are used.
+ * Any alignment of the element type is accepted; matrix products are faster
+ * where every row starts at a multiple of 16 bytes and its length is one too.
  * precision is that of the matrices (PACK_PREC_BF16 or PACK_PREC_FP32); sums
  * are held in fp32 (8-bit products in int32).  Outputs must not overlap inputs
  * unless a call allows it.  Sizes of 0 rows are accepted and do nothing more

@@ -1102,7 +1102,7 @@ Plan plan_with(MmType type, const MmArgs& a, Tiles t, int64_t splits) {
 // tiles step in 0.2 us a tile, small ones in 0.6, huge ones in 1.05 on a few
 // CUs and 1.6 where all of them run (the clock falls under their power);
 // operands through registers take 0.37 and 0.8, fp32 0.7 and 2.45.
-Plan choose(MmType type, const MmArgs& a, bool dma) {
+Plan search(MmType type, const MmArgs& a, bool dma) {
   if (type != MM_FP32 && !a.a_rmaj && !a.b_rmaj && a.M <= 16) return plan_with(type, a, TILES_THIN, 1);
   Plan best = plan_with(type, a, TILES_MINI, 1);
   double best_us = 1e30;
@@ -1129,6 +1129,23 @@ Plan choose(MmType type, const MmArgs& a, bool dma) {
     }
   }
   return best;
+}
+
+// search(), whose result depends on the sizes alone, with its last answers kept
+// (it costs about a microsecond, a block's calls ask for up to 20 plans).
+Plan choose(MmType type, const MmArgs& a, bool dma) {
+  struct Memo {
+    int32_t M, N, K, kind;
+    Plan plan;
+  };
+  static thread_local Memo memo[64];
+  const int32_t kind = 1 + (int)type + 4 * a.epi + 32 * a.a_rmaj + 64 * a.b_rmaj + 128 * (int)dma;  // 0: empty
+  const uint32_t at = ((uint32_t)a.M * 0x9E3779B1u ^ (uint32_t)a.N * 0x85EBCA77u ^ (uint32_t)a.K * 0xC2B2AE3Du ^
+                       (uint32_t)kind * 0x27D4EB2Fu) >> 26;
+  Memo& e = memo[at];
+  if (e.M != a.M || e.N != a.N || e.K != a.K || e.kind != kind)
+    e = Memo{a.M, a.N, a.K, kind, search(type, a, dma)};
+  return e.plan;
 }
 
 size_t partial_bytes(const MmArgs& a, const Plan& p) {

@@ -34,17 +34,11 @@ int done(const char* what, hipError_t e) {
 constexpr int64_t kMaxExtent = 0x7fffffff;  // rows, leading dimensions
 
 bool known(int32_t precision) { return precision == PACK_PREC_BF16 || precision == PACK_PREC_FP32; }
-int elem_size(int32_t precision) { return precision == PACK_PREC_BF16 ? 2 : 4; }
 
 // A leading dimension that fits rows of `cols` elements.
 bool ld_ok(int64_t ld, int64_t cols) { return ld >= cols && ld <= kMaxExtent; }
 
 bool aligned(const void* p, int64_t bytes) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)bytes == 0; }
-
-// Every row of the matrix starts at a multiple of `bytes`.
-bool rows_aligned(const void* p, int64_t ld, int size, int bytes) {
-  return aligned(p, bytes) && ld * size % bytes == 0;
-}
 
 int check_rows(int32_t precision, int64_t rows, int32_t cols) {
   if (!known(precision)) return bad("unknown precision %d", precision);
@@ -63,10 +57,6 @@ int norm_rows(RowMode mode, RowArgs& a, int32_t precision, hipStream_t stream) {
   if (a.rows == 0) return PACK_OK;
   if (!a.x || (mode != ROW_Q8 && !a.weight) || (mode == ROW_NORM ? !a.out : !a.q || !a.scale))
     return bad("NULL device pointer");
-  const int es = elem_size(precision), ve = 16 / es;
-  a.vec = a.cols % ve == 0 && rows_aligned(a.x, a.ldx, es, 16) && (!a.residual || rows_aligned(a.residual, a.ldr, es, 16)) &&
-          (!a.sum || rows_aligned(a.sum, a.lds, es, 16)) && (!a.weight || aligned(a.weight, 16)) &&
-          (mode == ROW_NORM ? rows_aligned(a.out, a.ldo, es, 16) : rows_aligned(a.q, a.ldo, 1, ve));
   return done("row kernel", launch_rows(precision, mode, a, stream));
 }
 
@@ -304,13 +294,10 @@ int pack_rms_norm_backward(const void* dy, int64_t ldy, const void* sum, int64_t
     return bad("NULL device pointer");
   if (work_bytes < need) return bad("workspace has %zu bytes, %zu needed", work_bytes, need);
   if (!aligned(work, 4)) return bad("workspace must be 4-byte aligned");
-  const int es = elem_size(precision);
   NormBwdArgs a{};
   a.sum = sum, a.lds = lds, a.dy = dy, a.ldy = ldy, a.dsum = dsum, a.ldd = ldd;
   a.weight = weight, a.rstd = rstd, a.dx = dx_out, a.ldx = ldx, a.dweight = dweight_out;
   a.partial = static_cast<float*>(work), a.rows = rows, a.cols = cols;
-  a.vec = cols % (16 / es) == 0 && rows_aligned(dy, ldy, es, 16) && rows_aligned(sum, lds, es, 16) &&
-          (!dsum || rows_aligned(dsum, ldd, es, 16)) && rows_aligned(dx_out, ldx, es, 16) && aligned(weight, 16);
   return done("norm backward", launch_norm_bwd(precision, a, stream));
 }
 
@@ -327,12 +314,9 @@ int pack_distill_topk(const void* logits, int64_t ldz, int32_t precision, int64_
     return bad("a leading dimension is smaller than classes=%d or too large", classes);
   if (rows == 0) return PACK_OK;
   if (!logits || !idx || !teacher || !loss_out) return bad("NULL device pointer");
-  const int es = elem_size(precision);
   DistillArgs a{};
   a.logits = logits, a.ldz = ldz, a.idx = idx, a.teacher = teacher, a.weight = row_weight;
   a.loss = loss_out, a.grad = grad_out, a.ldg = ldg, a.rows = rows, a.classes = classes, a.k = k, a.tau = temperature;
-  a.vec = classes % (16 / es) == 0 && rows_aligned(logits, ldz, es, 16) &&
-          (!grad_out || rows_aligned(grad_out, ldg, es, 16));
   return done("distillation", launch_distill(precision, a, stream));
 }
 

@@ -25,7 +25,6 @@ struct RowArgs {
   int64_t rows, ldx, ldr, lds, ldo;
   int32_t cols;
   float eps;
-  int32_t vec;            // 1: every row starts at 16 bytes and cols is a multiple of the 16-byte vector
 };
 enum RowMode { ROW_NORM = 0, ROW_NORM_Q8 = 1, ROW_Q8 = 2 };
 hipError_t launch_rows(int prec, RowMode mode, const RowArgs& a, hipStream_t s);
@@ -40,7 +39,7 @@ struct NormBwdArgs {
   float* dweight;         // [cols]
   float* partial;         // [norm_bwd_blocks(rows, cols), cols]
   int64_t rows, lds, ldy, ldd, ldx;
-  int32_t cols, vec;
+  int32_t cols;
 };
 int norm_bwd_blocks(int64_t rows, int32_t cols);
 hipError_t launch_norm_bwd(int prec, const NormBwdArgs& a, hipStream_t s);
@@ -55,7 +54,6 @@ struct DistillArgs {
   int64_t rows, ldz, ldg;
   int32_t classes, k;
   float tau;
-  int32_t vec;
 };
 hipError_t launch_distill(int prec, const DistillArgs& a, hipStream_t s);
 

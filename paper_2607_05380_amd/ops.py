@@ -13,6 +13,9 @@ Matrices are 2-D device tensors in bfloat16 or float32 whose rows are contiguous
 Every call runs HIP kernels on the current stream of the tensors' device; ``PackError`` says what an argument
 breaks.  Formulas and rules for empty, masked and non-finite rows are in ``include/tabpack.h``.
 """
+import ctypes
+import functools
+
 import torch
 
 from . import tabpack
@@ -61,17 +64,20 @@ def _call(fn, *args, like, others=()):
     for t in others:
         if t is not None and t.device != like.device:
             _fail("all tensors must be on one device")
-    lib = tabpack.load_library()
+    call = getattr(tabpack.load_library(), fn)
     dev = like.device.index
     if dev == torch.cuda.current_device():
-        tabpack._check(getattr(lib, fn)(*args, torch.cuda.current_stream(dev).cuda_stream))
+        rc = call(*args, torch.cuda.current_stream(dev).cuda_stream)
     else:
         with torch.cuda.device(dev):
-            tabpack._check(getattr(lib, fn)(*args, torch.cuda.current_stream(dev).cuda_stream))
+            rc = call(*args, torch.cuda.current_stream(dev).cuda_stream)
+    if rc:
+        tabpack._check(rc)
 
 
+@functools.lru_cache(maxsize=256)
 def _bytes(fn, *args):
-    import ctypes
+    """A workspace size (it depends on the sizes alone)."""
     n = ctypes.c_size_t()
     tabpack._check(getattr(tabpack.load_library(), fn)(*args, ctypes.byref(n)))
     return n.value

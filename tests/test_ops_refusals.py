@@ -89,9 +89,9 @@ FF = dict(x=P, ldx=16, wg=P, ldwg=16, wd=P, ldwd=24, r=P, ldr=8, prec=BF16, act=
     (dict(ldr=7), "leading"), (dict(ldo=7), "leading"), (dict(prec=2), "precision"), (dict(act=3), "activation"),
     (dict(act=-1), "activation"), (dict(T=-1), "tokens"), (dict(T=1 << 31), "tokens"), (dict(D=0), "d_in"),
     (dict(F=0), "d_in"), (dict(O=0), "d_in"), (dict(F=(1 << 24) + 1), "d_in"),
-    (dict(D=1 << 20, ldx=1 << 20, ldwg=1 << 20, work=None), "work"),
-    (dict(D=1 << 20, ldx=1 << 20, ldwg=1 << 20, nbytes=16), "workspace"),
-    (dict(D=1 << 20, ldx=1 << 20, ldwg=1 << 20, work=P + 8), "aligned")])
+    (dict(T=100, D=1 << 20, ldx=1 << 20, ldwg=1 << 20, work=None), "work"),
+    (dict(T=100, D=1 << 20, ldx=1 << 20, ldwg=1 << 20, nbytes=16), "workspace"),
+    (dict(T=100, D=1 << 20, ldx=1 << 20, ldwg=1 << 20, work=P + 8), "aligned")])
 def test_gated_ff_refuses(kw, part):
     a = dict(FF, **kw)
     _refused("pack_gated_ff_forward", [a[k] for k in ("x", "ldx", "wg", "ldwg", "wd", "ldwd", "r", "ldr", "prec", "act",
