@@ -467,8 +467,7 @@ int pack_gated_ff_forward(const void* x, int64_t ldx, const void* w_gate_up, int
  * wrote them (the residual's gradient is dy itself):
  *   dh = dy w_down,  dg = dh u act'(g),  du = dh act(g),
  *   dx = [dg | du] w_gate_up,  dw_gate_up = [dg | du]^T x,  dw_down = dy^T h
- *   dgate_up     device [tokens, 2 hidden], dense: dg and du (scratch of the
- *                call; may be gate_up itself)
+ *   dgate_up     device [tokens, 2 hidden], dense: dg and du (scratch of the call)
  *   dx_out       device [tokens, d_in]; dw_gate_up_out [2 hidden, d_in] and
  *                dw_down_out [d_out, hidden], dense; each may be NULL
  * relu'(0) is 0. */

@@ -81,38 +81,90 @@ __device__ __forceinline__ float logistic(float x) {
   const float d = 1.0f + exp_neg(x);
   return FAST ? __builtin_amdgcn_rcpf(d) : 1.0f / d;
 }
-constexpr float kSqrtHalf = 0.70710678118654752f, kInvSqrt2Pi = 0.39894228040143268f;
-
-template <bool FAST>
-__device__ __forceinline__ float act_value(int act, float g) {
-  if (act == PACK_ACT_SILU) return g * logistic<FAST>(g);
-  if (act == PACK_ACT_GELU) return 0.5f * g * (1.0f + erff(g * kSqrtHalf));
-  return g > 0.0f ? g : g == g ? 0.0f : g;
+constexpr float kInvSqrt2Pi = 0.39894228040143268f;
+// The normal distribution function at g, with e = exp(-g^2 / 2): Abramowitz and
+// Stegun 7.1.26 (erf to within 1.5e-7) for the tail beyond |g|, so that small
+// values on the negative side are not differences of large ones; no branches.
+__device__ __forceinline__ float normal_cdf(float g, float e) {
+  const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(g), 0.3275911f * 0.70710678118654752f, 1.0f));
+  float p = fmaf(t, 1.061405429f, -1.453152027f);
+  p = fmaf(t, p, 1.421413741f);
+  p = fmaf(t, p, -0.284496736f);
+  p = fmaf(t, p, 0.254829592f);
+  const float tail = 0.5f * t * p * e;
+  return g < 0.0f ? tail : 1.0f - tail;
 }
+__device__ __forceinline__ float exp_half_square(float g) {
+  return __builtin_amdgcn_exp2f(g * g * -0.72134752044448170f);
+}
+
+// c <- act(c) u, 8 values (the choice of the activation outside their loop)
 template <bool FAST>
-__device__ __forceinline__ void act_value_grad(int act, float g, float& v, float& d) {
+__device__ __forceinline__ void gate8(int act, float* c, const float* u) {
   if (act == PACK_ACT_SILU) {
-    const float p = logistic<FAST>(g);
-    v = g * p;
-    d = p * (1.0f + g * (1.0f - p));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] = c[i] * logistic<FAST>(c[i]) * u[i];
   } else if (act == PACK_ACT_GELU) {
-    const float c = 0.5f * (1.0f + erff(g * kSqrtHalf));
-    v = g * c;
-    d = fmaf(g * kInvSqrt2Pi, __builtin_amdgcn_exp2f(g * g * -0.72134752044448170f), c);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] = c[i] * normal_cdf(c[i], exp_half_square(c[i])) * u[i];
   } else {
-    v = g > 0.0f ? g : g == g ? 0.0f : g;
-    d = g > 0.0f ? 1.0f : 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] = (c[i] > 0.0f ? c[i] : c[i] == c[i] ? 0.0f : c[i]) * u[i];
+  }
+}
+// g <- d u act'(g) and u <- d act(g): the gradients of gate and up from d = dh
+template <bool FAST>
+__device__ __forceinline__ void gate8_grad(int act, const float* d, float* g, float* u) {
+  if (act == PACK_ACT_SILU) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float p = logistic<FAST>(g[i]), v = g[i] * p;
+      g[i] = d[i] * u[i] * (p + v * (1.0f - p));
+      u[i] = d[i] * v;
+    }
+  } else if (act == PACK_ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float e = exp_half_square(g[i]), c = normal_cdf(g[i], e), v = g[i] * c;
+      g[i] = d[i] * u[i] * fmaf(g[i] * kInvSqrt2Pi, e, c);
+      u[i] = d[i] * v;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float v = g[i] > 0.0f ? g[i] : g[i] == g[i] ? 0.0f : g[i];
+      g[i] = d[i] * u[i] * (g[i] > 0.0f ? 1.0f : 0.0f);
+      u[i] = d[i] * v;
+    }
   }
 }
 
 // ---------------------------------------------------------------- epilogues --
-// 8 consecutive elements at 16 bytes, as they lie in memory
+// the same at any alignment (the global memory path splits what crosses a line)
+typedef u32x4 u32x4_any __attribute__((aligned(1)));
+
+// 8 consecutive elements as they lie in memory
 template <typename T>
 struct Raw8 {
   u32x4 v[sizeof(T) / 2];
   __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) v[i] = *reinterpret_cast<const u32x4*>(p + i * (16 / sizeof(T)));
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) v[i] = *reinterpret_cast<const u32x4_any*>(p + i * (16 / sizeof(T)));
+  }
+  // n (1 to 8) elements exist: the others repeat the last one (loads without a
+  // branch, so none waits for another)
+  __device__ __forceinline__ void load(const T* p, int n) {
+    T e[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] = p[min(i, n - 1)];
+    __builtin_memcpy(v, e, sizeof v);
+  }
+  template <bool PART>
+  __device__ __forceinline__ void load_some(const T* p, int n) {
+    if constexpr (PART)
+      load(p, n);
+    else
+      load(p);
   }
   __device__ __forceinline__ void get(float* f) const {
     if constexpr (sizeof(T) == 2) {
@@ -135,22 +187,38 @@ __device__ __forceinline__ void store8(__bf16* p, const float* v) {
   bf16x8 o;
 #pragma unroll
   for (int i = 0; i < 8; ++i) o[i] = (__bf16)v[i];
-  *reinterpret_cast<bf16x8*>(p) = o;
+  *reinterpret_cast<u32x4_any*>(p) = __builtin_bit_cast(u32x4, o);
 }
 __device__ __forceinline__ void store8(float* p, const float* v) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
-    *reinterpret_cast<f32x4*>(p + 4 * i) = f32x4{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
+  for (int i = 0; i < 2; ++i) {
+    const f32x4 x{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
+    *reinterpret_cast<u32x4_any*>(p + 4 * i) = __builtin_bit_cast(u32x4, x);
+  }
 }
 
-// What an epilogue reads besides the sums, for 8 columns at 16 bytes: per
-// column (8-bit products), and per row and column.
+// 8 values, or the first n of them
+template <bool PART, typename T>
+__device__ __forceinline__ void store_some(T* p, const float* v, int n) {
+  if constexpr (!PART) {
+    store8(p, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) p[i] = (T)v[i];
+  }
+}
+
+// What an epilogue reads besides the sums, for 8 columns (PART: for the first
+// cnt of them): per column (8-bit
+// products), and per row and column.
+template <bool PART>
 struct Q8Cols {
   Raw8<float> scale, bias;
-  __device__ __forceinline__ void load(const MmArgs& a, int n) {
-    scale.load(a.col_scale + n);
+  __device__ __forceinline__ void load(const MmArgs& a, int n, int cnt) {
+    scale.template load_some<PART>(a.col_scale + n, cnt);
     if (a.bias) {
-      bias.load(a.bias + n);
+      bias.template load_some<PART>(a.bias + n, cnt);
     } else {
       bias.v[0] = bias.v[1] = u32x4{0, 0, 0, 0};
     }
@@ -164,48 +232,47 @@ struct Q8Cols {
     for (int i = 0; i < 8; ++i) c[i] = (float)__builtin_bit_cast(int32_t, c[i]) * (row_scale * s[i]) + b[i];
   }
 };
-template <int EPI, typename T>
+template <int EPI, typename T, bool PART>
 struct Cols {
-  Q8Cols gate, up;
-  __device__ __forceinline__ void load(const MmArgs& a, int n) {
-    if constexpr (is_q8(EPI)) gate.load(a, n);
-    if constexpr (EPI == MM_Q8_GATE) up.load(a, a.N + n);
+  Q8Cols<PART> gate, up;
+  __device__ __forceinline__ void load(const MmArgs& a, int n, int cnt) {
+    if constexpr (is_q8(EPI)) gate.load(a, n, cnt);
+    if constexpr (EPI == MM_Q8_GATE) up.load(a, a.N + n, cnt);
   }
 };
-template <int EPI, typename T>
+template <int EPI, typename T, bool PART>
 struct Extra {
   Raw8<T> g, u;
   float row_scale;
-  __device__ __forceinline__ void load(const MmArgs& a, int64_t m, int n) {
+  __device__ __forceinline__ void load(const MmArgs& a, int64_t m, int n, int cnt) {
     if constexpr (is_q8(EPI)) row_scale = a.row_scale[m];
     if constexpr (EPI == MM_PLAIN) {
-      if (a.add) g.load(static_cast<const T*>(a.add) + m * a.ldadd + n);
+      if (a.add) g.template load_some<PART>(static_cast<const T*>(a.add) + m * a.ldadd + n, cnt);
     }
     if constexpr (EPI == MM_GATE_BWD) {
       const T* p = static_cast<const T*>(a.pre) + m * a.ldpre + n;
-      g.load(p);
-      u.load(p + a.N);
+      g.template load_some<PART>(p, cnt);
+      u.template load_some<PART>(p + a.N, cnt);
     }
   }
 };
 
-// The outputs n .. n + 7 of row m from the sums c (gated: gate sums c, up sums
-// u), which are consumed; everything at 16 bytes.
-template <int EPI, typename T>
+// The outputs n .. n + 7 (PART: the first cnt) of row m from the sums c (gated:
+// gate sums c, up sums u), which are consumed.
+template <int EPI, typename T, bool PART>
 __device__ __forceinline__ void finish8(const MmArgs& a, int64_t m, int n, float* c, float* u,
-                                        const Cols<EPI, T>& cols, const Extra<EPI, T>& x) {
+                                        const Cols<EPI, T, PART>& cols, const Extra<EPI, T, PART>& x, int cnt) {
   constexpr bool FAST = sizeof(T) == 2;
   if constexpr (is_q8(EPI)) {
     cols.gate.apply(c, x.row_scale);
     if constexpr (EPI == MM_Q8_GATE) {
       cols.up.apply(u, x.row_scale);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) c[i] = act_value<false>(a.act, c[i]) * u[i];
+      gate8<false>(a.act, c, u);
     }
     if (a.out_f32)
-      store8(static_cast<float*>(a.out) + m * a.ldo + n, c);
+      store_some<PART>(static_cast<float*>(a.out) + m * a.ldo + n, c, cnt);
     else
-      store8(static_cast<__bf16*>(a.out) + m * a.ldo + n, c);
+      store_some<PART>(static_cast<__bf16*>(a.out) + m * a.ldo + n, c, cnt);
   } else if constexpr (EPI == MM_PLAIN) {
     if (a.add) {
       float r[8];
@@ -213,68 +280,35 @@ __device__ __forceinline__ void finish8(const MmArgs& a, int64_t m, int n, float
 #pragma unroll
       for (int i = 0; i < 8; ++i) c[i] += r[i];
     }
-    store8(static_cast<T*>(a.out) + m * a.ldo + n, c);
+    store_some<PART>(static_cast<T*>(a.out) + m * a.ldo + n, c, cnt);
   } else if constexpr (EPI == MM_GATE) {
     if (a.pre) {
       T* p = static_cast<T*>(a.pre) + m * a.ldpre + n;
-      store8(p, c);
-      store8(p + a.N, u);
+      store_some<PART>(p, c, cnt);
+      store_some<PART>(p + a.N, u, cnt);
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) c[i] = act_value<FAST>(a.act, c[i]) * u[i];
-    store8(static_cast<T*>(a.out) + m * a.ldo + n, c);
+    gate8<FAST>(a.act, c, u);
+    store_some<PART>(static_cast<T*>(a.out) + m * a.ldo + n, c, cnt);
   } else {
     static_assert(EPI == MM_GATE_BWD);
     float g[8], w[8];
     x.g.get(g);
     x.u.get(w);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float v, d;
-      act_value_grad<FAST>(a.act, g[i], v, d);
-      g[i] = c[i] * w[i] * d;
-      w[i] = c[i] * v;
-    }
+    gate8_grad<FAST>(a.act, c, g, w);
     T* o = static_cast<T*>(a.out) + m * a.ldo + n;
-    store8(o, g);
-    store8(o + a.N, w);
+    store_some<PART>(o, g, cnt);
+    store_some<PART>(o + a.N, w, cnt);
   }
 }
 
-// The same for one element n < N, at any alignment.
-template <int EPI, typename T>
-__device__ __forceinline__ void finish1(const MmArgs& a, int64_t m, int n, float c, float u) {
-  constexpr bool FAST = sizeof(T) == 2;
-  if constexpr (is_q8(EPI)) {
-    const float sx = a.row_scale[m];
-    c = (float)__builtin_bit_cast(int32_t, c) * (sx * a.col_scale[n]) + (a.bias ? a.bias[n] : 0.0f);
-    if constexpr (EPI == MM_Q8_GATE) {
-      u = (float)__builtin_bit_cast(int32_t, u) * (sx * a.col_scale[a.N + n]) + (a.bias ? a.bias[a.N + n] : 0.0f);
-      c = act_value<false>(a.act, c) * u;
-    }
-    if (a.out_f32)
-      static_cast<float*>(a.out)[m * a.ldo + n] = c;
-    else
-      static_cast<__bf16*>(a.out)[m * a.ldo + n] = (__bf16)c;
-  } else if constexpr (EPI == MM_PLAIN) {
-    if (a.add) c += (float)static_cast<const T*>(a.add)[m * a.ldadd + n];
-    static_cast<T*>(a.out)[m * a.ldo + n] = (T)c;
-  } else if constexpr (EPI == MM_GATE) {
-    if (a.pre) {
-      T* p = static_cast<T*>(a.pre) + m * a.ldpre + n;
-      p[0] = (T)c;
-      p[a.N] = (T)u;
-    }
-    static_cast<T*>(a.out)[m * a.ldo + n] = (T)(act_value<FAST>(a.act, c) * u);
-  } else {
-    const T* p = static_cast<const T*>(a.pre) + m * a.ldpre + n;
-    const float g = (float)p[0], w = (float)p[a.N];
-    float v, d;
-    act_value_grad<FAST>(a.act, g, v, d);
-    T* o = static_cast<T*>(a.out) + m * a.ldo + n;
-    o[0] = (T)(c * w * d);
-    o[a.N] = (T)(c * v);
-  }
+// finish8 with its reads
+template <int EPI, typename T, bool PART>
+__device__ __forceinline__ void finish_row(const MmArgs& a, int64_t m, int n, float* c, float* u, int cnt) {
+  Cols<EPI, T, PART> cols;
+  Extra<EPI, T, PART> x;
+  cols.load(a, n, cnt);
+  x.load(a, m, n, cnt);
+  finish8<EPI, T, PART>(a, m, n, c, u, cols, x, cnt);
 }
 
 // Partial sums of a split depth: [split][M][ldp], ldp = N rounded up to 8,
@@ -322,9 +356,27 @@ __device__ __forceinline__ void unstage8(const char* stage, int row, int c, floa
     for (int e = 0; e < 4; ++e) v[4 * h + e] = x[e];
   }
 }
-template <int NB>
-__device__ __forceinline__ float unstage1(const char* stage, int row, int col) {
-  return *reinterpret_cast<const float*>(chunk_at<NB>(stage, row, col / 4) + (col % 4) * 4);
+// Chunk ch of a staged block's rows row, row + RP, ...: outputs n .. n + 7
+// (PART: cnt of them) of the rows m, m + RP, ... of C.  What the rows read
+// besides the sums is asked for NT rows together.
+template <int EPI, typename T, int NB, int NT, bool PART>
+__device__ __forceinline__ void write_rows(const MmArgs& a, const char* stage, int m, int row, int n, int ch, int cnt) {
+  constexpr int ROWS = 32 * NB, COLS = is_gate(EPI) ? 16 * NB : 32 * NB, RP = 64 / (COLS / 8);
+  Cols<EPI, T, PART> cols;
+  cols.load(a, n, cnt);
+#pragma unroll 1
+  for (; row < ROWS; row += NT * RP, m += NT * RP) {
+    Extra<EPI, T, PART> x[NT];
+#pragma unroll
+    for (int b = 0; b < NT; ++b) x[b].load(a, min(m + b * RP, a.M - 1), n, cnt);
+#pragma unroll
+    for (int b = 0; b < NT; ++b) {
+      float c[8], u[8];
+      unstage8<NB>(stage, row + b * RP, 2 * ch, c);
+      if constexpr (is_gate(EPI)) unstage8<NB>(stage, row + b * RP, COLS / 4 + 2 * ch, u);
+      if (m + b * RP < a.M) finish8<EPI, T, PART>(a, m + b * RP, n, c, u, cols, x[b], cnt);
+    }
+  }
 }
 // The staged block to the outputs; m0, n0: its first row and output column.
 template <int EPI, typename T, int NB>
@@ -348,37 +400,10 @@ __device__ __forceinline__ void write_block(const MmArgs& a, const char* stage, 
         }
       }
     }
-  } else if (a.vec_out) {
-    // what the rows read besides the sums is asked for all passes of a turn together
-    constexpr int NT = NP < 4 ? NP : 4;
-    const int nc = min(n, a.N - 8);  // columns past the end read others and write nothing
-    Cols<EPI, T> cols;
-    cols.load(a, nc);
-#pragma unroll 1
-    for (int it = 0; it < NP; it += NT) {
-      Extra<EPI, T> x[NT];
-#pragma unroll
-      for (int b = 0; b < NT; ++b) x[b].load(a, min(m0 + (it + b) * RP + r0, a.M - 1), nc);
-#pragma unroll
-      for (int b = 0; b < NT; ++b) {
-        const int row = (it + b) * RP + r0;
-        float c[8], u[8];
-        unstage8<NB>(stage, row, 2 * ch, c);
-        if constexpr (is_gate(EPI)) unstage8<NB>(stage, row, COLS / 4 + 2 * ch, u);
-        if (n < a.N && m0 + row < a.M) finish8<EPI, T>(a, m0 + row, n, c, u, cols, x[b]);
-      }
-    }
-  } else {
-    // a lane takes one output column
-    const int col = lane % COLS;
-    if (n0 + col < a.N) {
-#pragma unroll 1
-      for (int row = lane / COLS; row < ROWS && m0 + row < a.M; row += 64 / COLS) {
-        const float c = unstage1<NB>(stage, row, col);
-        const float u = is_gate(EPI) ? unstage1<NB>(stage, row, COLS + col) : 0.0f;
-        finish1<EPI, T>(a, m0 + row, n0 + col, c, u);
-      }
-    }
+  } else if (n + 8 <= a.N) {
+    write_rows<EPI, T, NB, NP < 4 ? NP : 4, false>(a, stage, m0 + r0, r0, n, ch, 8);
+  } else if (n < a.N) {
+    write_rows<EPI, T, NB, 1, true>(a, stage, m0 + r0, r0, n, ch, a.N - n);
   }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
@@ -393,12 +418,6 @@ __global__ __launch_bounds__(256) void join_kernel(MmArgs a) {
     const int64_t m = i / chunks;
     const int n = (int)(i % chunks) * 8;
     const float* p = a.work + m * ldp + n;
-    Cols<EPI, T> cols;
-    Extra<EPI, T> x;
-    if (a.vec_out) {
-      cols.load(a, n);
-      x.load(a, m, n);
-    }
     float c[8], u[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) c[e] = u[e] = 0.0f;
@@ -424,13 +443,10 @@ __global__ __launch_bounds__(256) void join_kernel(MmArgs a) {
         }
       }
     }
-    if (a.vec_out) {
-      finish8<EPI, T>(a, m, n, c, u, cols, x);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (n + e < a.N) finish1<EPI, T>(a, m, n + e, c[e], u[e]);
-    }
+    if (n + 8 <= a.N)
+      finish_row<EPI, T, false>(a, m, n, c, u, 8);
+    else
+      finish_row<EPI, T, true>(a, m, n, c, u, a.N - n);
   }
 }
 
@@ -487,7 +503,6 @@ struct Dma {
 
 // 16 bytes of global memory at any alignment
 __device__ __forceinline__ u32x4 load16(const void* p) {
-  typedef u32x4 u32x4_any __attribute__((aligned(1)));
   return *(const TABPACK_GLOBAL u32x4_any*)p;
 }
 
@@ -1056,11 +1071,15 @@ __global__ __launch_bounds__(NW * 64) void thin_kernel(MmArgs a) {
     c += sums[q][0][lane];
     if constexpr (G == 2) u += sums[q][1][lane];
   }
+  if (n >= a.N) return;
+  float cs[8], us[8];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const acc_t ce = c[e], ue = u[e];
-    if (n + e < a.N) finish1<EPI, T>(a, m, n + e, __builtin_bit_cast(float, ce), __builtin_bit_cast(float, ue));
+  for (int e = 0; e < 8; ++e) {
+    const acc_t ce = c[e & 3], ue = u[e & 3];
+    cs[e] = __builtin_bit_cast(float, ce);
+    us[e] = __builtin_bit_cast(float, ue);
   }
+  finish_row<EPI, T, true>(a, m, n, cs, us, min(4, a.N - n));
 }
 
 // ------------------------------------------------------------------- host --
@@ -1237,14 +1256,7 @@ size_t mm_workspace(MmType type, const MmArgs& a) {
   return std::max(partial_bytes(a, choose(type, a, true)), partial_bytes(a, choose(type, a, false)));
 }
 
-hipError_t launch_mm(MmType type, const MmArgs& args, hipStream_t s) {
-  MmArgs a = args;
-  // outputs, added and saved matrices in 16-byte pieces where all allow it
-  const int es = type == MM_BF16 || (type == MM_I8 && !a.out_f32) ? 2 : 4;
-  auto ok = [&](const void* p, int64_t ld) { return !p || rows16(p, ld, es, a.N); };
-  auto okv = [&](const float* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
-  a.vec_out = a.N % 8 == 0 && ok(a.out, a.ldo) && ok(a.add, a.ldadd) && ok(a.pre, a.ldpre) && okv(a.col_scale) &&
-              okv(a.bias);
+hipError_t launch_mm(MmType type, const MmArgs& a, hipStream_t s) {
   switch (type) {
     case MM_BF16: return launch_float<__bf16>(type, a, s);
     case MM_FP32: return launch_float<float>(type, a, s);

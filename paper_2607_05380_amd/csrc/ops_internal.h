@@ -86,7 +86,7 @@ struct MmArgs {
   float* work;            // partial sums of a split depth
   size_t work_bytes;
   // filled in by launch_mm
-  int32_t tiles_m, tiles_n, splits, steps_per_split, vec_out;
+  int32_t tiles_m, tiles_n, splits, steps_per_split;
 };
 // Bytes of `work` that the product needs (0: none).
 size_t mm_workspace(MmType type, const MmArgs& a);
