@@ -34,6 +34,7 @@
 // in a fixed order; a depth split over workgroups is joined in a fixed order
 // by a second kernel.
 #include <algorithm>
+#include <cmath>
 
 #include "gemm_tiles.h"
 #include "ops_internal.h"
@@ -639,11 +640,11 @@ __device__ __forceinline__ void clear(A16& a) {
 struct Where {
   int tm, tn, split;
 };
-__device__ __forceinline__ Where where(const MmArgs& a) {
+__device__ __forceinline__ Where where(const MmArgs& a, uint32_t block) {
   const uint32_t per = (uint32_t)a.tiles_m * a.tiles_n;
   Where w;
-  w.split = blockIdx.x / per;
-  const uint32_t b = blockIdx.x % per, q = per / 8, r = per % 8, x = b % 8;
+  w.split = block / per;
+  const uint32_t b = block % per, q = per / 8, r = per % 8, x = b % 8;
   const uint32_t t = x * q + (x < r ? x : r) + b / 8;
   const uint32_t band = t / (4 * a.tiles_n), in = t % (4 * a.tiles_n);
   const uint32_t h = min(4u, (uint32_t)a.tiles_m - 4 * band);
@@ -655,15 +656,14 @@ __device__ __forceinline__ Where where(const MmArgs& a) {
 // ---------------------------------------------------- small and mini tiles --
 // 64 NB x 64 NB tiles on 4 waves (2 x 2) of NB x NB 32 x 32 blocks.
 template <typename T, bool RA, bool RB, int EPI, bool DMA, int NB, int NS>
-__global__ __launch_bounds__(256, NB * NS == 8 ? 1 : NB * NS == 4 ? 2 : 4) void small_kernel(MmArgs a) {
+__device__ __forceinline__ void small_tile(const MmArgs& a, uint32_t block, char* smem) {
   constexpr int ES = sizeof(T), KE = kStep / ES, R = 64 * NB, REGION = R * kStep, W = 32 * NB;
   static_assert(DMA || NS == 2, "two stages through registers");
-  __shared__ __attribute__((aligned(16))) char smem[2 * NS * REGION];
   typedef typename Ty<T>::acc16 acc16;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave >> 1, wn = wave & 1;
-  const Where w = where(a);
+  const Where w = where(a, block);
   const int m0 = w.tm * R, n0 = w.tn * (is_gate(EPI) ? R / 2 : R);
   const int64_t kbeg = (int64_t)w.split * a.steps_per_split * KE;
   const int64_t kend = min((int64_t)a.K, kbeg + (int64_t)a.steps_per_split * KE);
@@ -832,6 +832,53 @@ __device__ __forceinline__ void tie(bf16x8 (&f)[4]) {
   asm volatile("" : "+v"(f[0]), "+v"(f[1]), "+v"(f[2]), "+v"(f[3]));
 }
 
+// A wave's 128 x 64 sums to the outputs, one 64 x 64 half after the other.  No
+// other workgroup on the CU covers the waits, so what a quarter's rows read
+// besides the sums is asked for a quarter ahead.
+template <int EPI, typename T, typename A16>
+__device__ __forceinline__ void huge_out(const MmArgs& a, const A16 (&acc)[2][2][2], char* stage, int m0, int n0,
+                                         int split, int lane) {
+  typedef typename Ty<T>::acc_t acc_t;
+  constexpr int COLS = is_gate(EPI) ? 32 : 64, CH = COLS / 8, RP = 64 / CH, NP = 32 / RP;  // passes a quarter
+  const int ch = lane % CH, r0 = lane / CH, n = n0 + 8 * ch;
+  if (a.splits > 1 || n0 + COLS > a.N) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      stage_block<acc_t, 2>(acc[h], stage, lane);
+      write_block<EPI, T, 2>(a, stage, m0 + h * 64, n0, split, lane);
+    }
+    return;
+  }
+  Cols<EPI, T, false> cols;
+  cols.load(a, n, 8);
+  Extra<EPI, T, false> x[NP], y[NP];
+  auto ask = [&](Extra<EPI, T, false>(&e)[NP], int q) {
+#pragma unroll
+    for (int p = 0; p < NP; ++p) e[p].load(a, min(m0 + q * 32 + p * RP + r0, a.M - 1), n, 8);
+  };
+  ask(x, 0);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {  // (unrolled: the first half's sums give up their registers)
+    stage_block<acc_t, 2>(acc[h], stage, lane);
+#pragma unroll 1
+    for (int q = 0; q < 2; ++q) {
+      if (h + q < 2) ask(y, 2 * h + q + 1);
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        const int row = q * 32 + p * RP + r0, m = m0 + h * 64 + row;
+        float c[8], u[8];
+        unstage8<2>(stage, row, 2 * ch, c);
+        if constexpr (is_gate(EPI)) unstage8<2>(stage, row, 8 + 2 * ch, u);
+        if (m < a.M) finish8<EPI, T, false>(a, m, n, c, u, cols, x[p], 8);
+      }
+#pragma unroll
+      for (int p = 0; p < NP; ++p) x[p] = y[p];
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
 // 256 x 256 tiles on 8 waves (2 x 4, two to a SIMD), each 128 x 64.  A K step
 // is two phases, one half (64 x 64) of the wave's sums each; a phase is a read
 // part (the half's fragments from LDS) and a product part (16 MFMAs, with the
@@ -847,15 +894,15 @@ __device__ __forceinline__ void tie(bf16x8 (&f)[4]) {
 // region and wave) before the barrier.  A slot is asked for again in the phase
 // after its last reads at the earliest, in the product part, when the lagging
 // waves have finished theirs.
+constexpr int kHugeSlots = 10;
 template <typename T, bool RA, bool RB, int EPI>
-__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void huge_kernel(MmArgs a) {
-  constexpr int ES = sizeof(T), KE = kStep / ES, SLOTS = 10;
-  __shared__ __attribute__((aligned(16))) char smem[SLOTS * kRegion];
+__device__ __forceinline__ void huge_tile(const MmArgs& a, uint32_t block, char* smem) {
+  constexpr int ES = sizeof(T), KE = kStep / ES, SLOTS = kHugeSlots;
   typedef typename Ty<T>::acc16 acc16;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave >> 2, wn = wave & 3;
-  const Where w = where(a);
+  const Where w = where(a, block);
   const int m0 = w.tm * 256, n0 = w.tn * (is_gate(EPI) ? 128 : 256);
   const int64_t kbeg = (int64_t)w.split * a.steps_per_split * KE;
   const int64_t kend = min((int64_t)a.K, kbeg + (int64_t)a.steps_per_split * KE);
@@ -961,17 +1008,46 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   if (wm == 0) bar();
   wait_vm<0, true>();
   bar();  // the sums are staged in the operand regions
-  char* const stage = smem + wave * 16384;
-#pragma unroll 1
-  for (int h = 0; h < 2; ++h) {
-    if (h == 0)
-      stage_block<typename Ty<T>::acc_t, 2>(acc[0], stage, lane);
-    else
-      stage_block<typename Ty<T>::acc_t, 2>(acc[1], stage, lane);
-    write_block<EPI, T, 2>(a, stage, m0 + wm * 128 + h * 64, n0 + wn * (is_gate(EPI) ? 32 : 64), w.split, lane);
-  }
+  huge_out<EPI, T>(a, acc, smem + wave * 16384, m0 + wm * 128, n0 + wn * (is_gate(EPI) ? 32 : 64), w.split, lane);
 }
 
+// ----------------------------------------------------------------- kernels --
+// One product, or two independent ones in one launch, which fill the chip
+// together where each alone leaves CUs idle: b's workgroups spread evenly among
+// a's in octets (an octet covers the XCDs).
+struct MmPair {
+  MmArgs a, b;
+  uint32_t na, nb;  // workgroups of each
+};
+// The part of a pair's launch that this workgroup has: product 0 or 1 (2: none).
+__device__ __forceinline__ int part_of(const MmPair& p, uint32_t& block) {
+  const uint32_t oa = (p.na + 7) / 8, ob = (p.nb + 7) / 8, o = blockIdx.x / 8;
+  const uint32_t lo = (uint32_t)((uint64_t)o * ob / (oa + ob)), hi = (uint32_t)(((uint64_t)o + 1) * ob / (oa + ob));
+  const bool second = hi > lo;
+  block = (second ? lo : o - lo) * 8 + blockIdx.x % 8;
+  return second ? (block < p.nb ? 1 : 2) : (block < p.na ? 0 : 2);
+}
+
+template <typename T, bool RA, bool RB, int EPI, bool DMA, int NB, int NS>
+__global__ __launch_bounds__(256, NB * NS == 4 ? 2 : 4) void small_kernel(MmArgs a) {
+  __shared__ __attribute__((aligned(16))) char smem[2 * NS * 64 * NB * kStep];
+  small_tile<T, RA, RB, EPI, DMA, NB, NS>(a, blockIdx.x, smem);
+}
+template <typename T, int EPI, bool DMA, int NB, int NS>
+__global__ __launch_bounds__(256, NB * NS == 4 ? 2 : 4) void small_pair_kernel(MmPair p) {
+  __shared__ __attribute__((aligned(16))) char smem[2 * NS * 64 * NB * kStep];
+  uint32_t block;
+  const int part = part_of(p, block);
+  if (part == 0)
+    small_tile<T, false, true, EPI, DMA, NB, NS>(p.a, block, smem);
+  else if (part == 1)
+    small_tile<T, true, true, MM_PLAIN, DMA, NB, NS>(p.b, block, smem);
+}
+template <typename T, bool RA, bool RB, int EPI>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void huge_kernel(MmArgs a) {
+  __shared__ __attribute__((aligned(16))) char smem[kHugeSlots * kRegion];
+  huge_tile<T, RA, RB, EPI>(a, blockIdx.x, smem);
+}
 // -------------------------------------------------------------- thin tiles --
 // Up to 16 rows of A (depth-contiguous operands, bf16 and int8): a workgroup
 // owns 16 columns (gated: 16 gate and 16 up rows of B), its NW waves share the
@@ -1089,6 +1165,7 @@ struct Plan {
   Tiles tiles;
   int64_t tm, tn;
   int splits, steps;  // workgroups that share a tile's depth, K steps of each
+  double us;          // the model's time
 };
 
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -1109,42 +1186,47 @@ Plan plan_with(MmType type, const MmArgs& a, Tiles t, int64_t splits) {
   splits = std::max((int64_t)1, std::min(splits, steps));
   p.steps = (int)cdiv(steps, splits);
   p.splits = (int)cdiv(steps, p.steps);
+  p.us = 0;
   return p;
 }
 
+// A model of a product's time in us, fitted to measurements of 128..16384 rows,
+// 256..4096 columns and depths 1024..16384: a start, a time per K step that
+// grows with the tiles a CU holds, and the join's traffic.  Mini tiles step in
+// 0.2 us a tile, small ones in 0.6, huge ones in 1.05 on a few CUs and 1.6 where
+// all of them run (the clock falls under their power); operands through
+// registers take 0.37 and 0.8, fp32 0.7 and 2.45.
+double step_us(MmType type, Tiles t, bool dma, double wgs) {
+  const double held = std::ceil(wgs / 256);
+  if (t == TILES_HUGE) return wgs < 256 ? 1.05 + 0.55 * wgs / 256 : 1.6 * held;
+  if (type == MM_FP32) return t == TILES_MINI ? std::max(0.85, 0.7 * held) : 2.45 * held;
+  if (!dma) return t == TILES_MINI ? std::max(0.5, 0.37 * held) : std::max(0.95, 0.8 * held);
+  return (t == TILES_MINI ? 0.2 : 0.6) * held;
+}
+double start_us(Tiles t) { return t == TILES_HUGE ? 7 : 3.3; }
+double join_us(const MmArgs& a, const Plan& p) {
+  if (p.splits < 2) return 0;
+  return 2.5 + p.splits * (double)a.M * ((a.N + 7) / 8 * 8) * (is_gate(a.epi) ? 16 : 8) / 3.5e6;
+}
+constexpr int64_t kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+
 // The layout that should be fastest.  Up to 16 rows the thin kernel (at depth
 // 1024 and 1024..4096 columns 3.8-5.1 us against 5.6-6.8 on mini tiles; at 32
-// rows it no longer gains: 7.0 / 6.6, depth 4096 13.4 / 9.9 split).  The
-// others by a model of the time in us, fitted to measurements of products of
-// 128..16384 rows, 256..4096 columns and depths 1024..16384: a start, a time per
-// K step that grows with the tiles a CU holds, and the join's traffic.  Mini
-// tiles step in 0.2 us a tile, small ones in 0.6, huge ones in 1.05 on a few
-// CUs and 1.6 where all of them run (the clock falls under their power);
-// operands through registers take 0.37 and 0.8, fp32 0.7 and 2.45.
+// rows it no longer gains: 7.0 / 6.6, depth 4096 13.4 / 9.9 split), the others
+// by the model.
 Plan search(MmType type, const MmArgs& a, bool dma) {
-  if (type != MM_FP32 && !a.a_rmaj && !a.b_rmaj && a.M <= 16) return plan_with(type, a, TILES_THIN, 1);
   Plan best = plan_with(type, a, TILES_MINI, 1);
-  double best_us = 1e30;
+  best.us = 1e30;
+  if (type != MM_FP32 && !a.a_rmaj && !a.b_rmaj && a.M <= 16) return plan_with(type, a, TILES_THIN, 1);
   for (Tiles t : {TILES_MINI, TILES_SMALL, TILES_HUGE}) {
     if (t == TILES_HUGE && !dma) continue;
     int64_t last = 0;
-    for (int64_t s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
-      const Plan p = plan_with(type, a, t, s);
+    for (int64_t s : kSplits) {
+      Plan p = plan_with(type, a, t, s);
       if (p.splits == last || (p.splits > 1 && p.steps < 2)) continue;
       last = p.splits;
-      const double wgs = (double)p.tm * p.tn * p.splits, held = (double)cdiv((int64_t)wgs, 256);
-      double step;
-      if (t == TILES_HUGE)
-        step = wgs < 256 ? 1.05 + 0.55 * wgs / 256 : 1.6 * held;
-      else if (type == MM_FP32)
-        step = t == TILES_MINI ? std::max(0.85, 0.7 * held) : 2.45 * held;
-      else if (!dma)
-        step = t == TILES_MINI ? std::max(0.5, 0.37 * held) : std::max(0.95, 0.8 * held);
-      else
-        step = (t == TILES_MINI ? 0.2 : 0.6) * held;
-      double us = (t == TILES_HUGE ? 7 : 3.3) + p.steps * step;
-      if (p.splits > 1) us += 2.5 + p.splits * (double)a.M * partial_half(a.N) * (is_gate(a.epi) ? 16 : 8) / 3.5e6;
-      if (us < best_us) best_us = us, best = p;
+      p.us = start_us(t) + p.steps * step_us(type, t, dma, (double)p.tm * p.tn * p.splits) + join_us(a, p);
+      if (p.us < best.us) best = p;
     }
   }
   return best;
@@ -1201,15 +1283,27 @@ void launch_thin(const MmArgs& a, dim3 grid, hipStream_t s) {
     hipLaunchKernelGGL((thin_kernel<T, EPI, 4>), grid, dim3(256), 0, s, a);
 }
 
+// Fills in the launch's part of the arguments; its workgroups (0: too many for a launch).
+uint32_t apply(MmArgs& a, const Plan& p) {
+  a.tiles_m = (int)p.tm, a.tiles_n = (int)p.tn, a.splits = p.splits, a.steps_per_split = p.steps;
+  const int64_t blocks = p.tm * p.tn * p.splits;
+  return blocks <= (1 << 21) ? (uint32_t)blocks : 0;  // (a launch is limited to 2^32 threads)
+}
+
+template <int EPI, typename T>
+void launch_join(const MmArgs& a, hipStream_t s) {
+  if (a.splits < 2) return;
+  const int64_t n = cdiv((int64_t)a.M * (partial_half(a.N) / 8), 256);
+  hipLaunchKernelGGL((join_kernel<EPI, T>), dim3((uint32_t)(n < 4096 ? n : 4096)), dim3(256), 0, s, a);
+}
+
 template <typename T, bool RA, bool RB, int EPI>
 hipError_t launch_tiles(MmType type, MmArgs a, hipStream_t s) {
   const bool dma = can_dma(type, a);
   const Plan p = choose(type, a, dma);
-  const int64_t blocks = p.tm * p.tn * p.splits;
-  if (blocks > (1 << 22)) return hipErrorInvalidConfiguration;  // a launch is limited to 2^32 threads
-  if (p.splits > 1 && a.work_bytes < partial_bytes(a, p)) return hipErrorInvalidValue;
-  a.tiles_m = (int)p.tm, a.tiles_n = (int)p.tn, a.splits = p.splits, a.steps_per_split = p.steps;
-  const dim3 grid((uint32_t)blocks);
+  const dim3 grid(apply(a, p));
+  if (grid.x == 0) return hipErrorInvalidConfiguration;
+  if (a.work_bytes < partial_bytes(a, p)) return hipErrorInvalidValue;
   if constexpr (sizeof(T) != 4 && !RA && !RB) {
     if (p.tiles == TILES_THIN) {
       launch_thin<T, EPI>(a, grid, s);
@@ -1230,10 +1324,95 @@ hipError_t launch_tiles(MmType type, MmArgs a, hipStream_t s) {
     else
       hipLaunchKernelGGL((small_kernel<T, RA, RB, EPI, false, 1, 2>), grid, dim3(256), 0, s, a);
   }
-  if (p.splits > 1) {
-    const int64_t n = cdiv((int64_t)a.M * (partial_half(a.N) / 8), 256);
-    hipLaunchKernelGGL((join_kernel<EPI, T>), dim3((uint32_t)(n < 4096 ? n : 4096)), dim3(256), 0, s, a);
+  launch_join<EPI, T>(a, s);
+  return hipGetLastError();
+}
+
+// Two products in one launch: the same tiles, and depths split so that the
+// workgroups of both take about the same number of steps.  Not for huge tiles:
+// the gradients of gate and up beside the down weights' (16,384 tokens of 1024,
+// hidden 4096) 365 us together, 222 + 122 apart.
+struct PairPlan {
+  Plan a, b;
+  double us;
+};
+PairPlan search_pair(MmType type, const MmArgs& a, const MmArgs& b, bool dma) {
+  PairPlan best;
+  best.us = 1e30;
+  const int64_t sa = depth_steps(type, a), sb = depth_steps(type, b);
+  for (Tiles t : {TILES_MINI, TILES_SMALL}) {
+    for (int64_t s : kSplits) {
+      const int64_t q = cdiv(std::max(sa, sb), s);  // most steps of a workgroup
+      if (s > 1 && q < 2) break;
+      PairPlan p;
+      p.a = plan_with(type, a, t, cdiv(sa, q));
+      p.b = plan_with(type, b, t, cdiv(sb, q));
+      const double wa = (double)p.a.tm * p.a.tn * p.a.splits, wb = (double)p.b.tm * p.b.tn * p.b.splits;
+      // the workgroups of a CU one after the other, but no less than the longest one
+      const double mean = (wa * p.a.steps + wb * p.b.steps) / (wa + wb);
+      const double longest = std::max(p.a.steps, p.b.steps);
+      p.us = start_us(t) + join_us(a, p.a) + join_us(b, p.b) +
+             std::max(mean * step_us(type, t, dma, wa + wb), longest * step_us(type, t, dma, std::min(wa + wb, 256.0)));
+      if (p.us < best.us) best = p;
+    }
   }
+  return best;
+}
+// Whether the two go together (remembered as choose()'s plans are); their
+// workspace lies one after the other.
+bool pair_up(MmType type, const MmArgs& a, const MmArgs& b, bool dma, PairPlan& p) {
+  if (a.M < 1 || b.K < 1) return false;
+  struct Memo {
+    int32_t size[6], kind;
+    PairPlan plan;
+    bool good;
+  };
+  static thread_local Memo memo[16];
+  const int32_t size[6] = {a.M, a.N, a.K, b.M, b.N, b.K};
+  const int32_t kind = 1 + (int)type + 4 * a.epi + 128 * (int)dma;  // 0: empty
+  uint32_t h = (uint32_t)kind;
+  for (int32_t v : size) h = (h ^ (uint32_t)v) * 0x9E3779B1u;
+  Memo& e = memo[h >> 28];
+  if (e.kind != kind || !std::equal(size, size + 6, e.size)) {
+    std::copy(size, size + 6, e.size);
+    e.kind = kind;
+    e.plan = search_pair(type, a, b, dma);
+    e.good = e.plan.us < choose(type, a, dma).us + choose(type, b, dma).us;
+  }
+  p = e.plan;
+  return e.good;
+}
+size_t pair_bytes(const MmArgs& a, const MmArgs& b, const PairPlan& p) {
+  return (partial_bytes(a, p.a) + 15) / 16 * 16 + partial_bytes(b, p.b);
+}
+
+template <typename T, int EPI>
+hipError_t launch_pair(MmType type, MmArgs a, MmArgs b, const PairPlan& p, bool dma, hipStream_t s) {
+  MmPair m;
+  m.na = apply(a, p.a);
+  m.nb = apply(b, p.b);
+  if (m.na == 0 || m.nb == 0) return hipErrorInvalidConfiguration;
+  if (!a.out) m.na = 0;
+  if (!b.out) m.nb = 0;
+  if (a.work_bytes < pair_bytes(a, b, p)) return hipErrorInvalidValue;
+  b.work += (partial_bytes(a, p.a) + 15) / 16 * 4;
+  m.a = a, m.b = b;
+  const dim3 grid(((m.na + 7) / 8 + (m.nb + 7) / 8) * 8);
+  const Tiles t = p.a.tiles;
+  if constexpr (sizeof(T) != 4) {
+    if (dma && t == TILES_SMALL)
+      hipLaunchKernelGGL((small_pair_kernel<T, EPI, true, 2, 2>), grid, dim3(256), 0, s, m);
+    else if (dma)
+      hipLaunchKernelGGL((small_pair_kernel<T, EPI, true, 1, 4>), grid, dim3(256), 0, s, m);
+  }
+  if (!dma) {
+    if (t == TILES_SMALL)
+      hipLaunchKernelGGL((small_pair_kernel<T, EPI, false, 2, 2>), grid, dim3(256), 0, s, m);
+    else
+      hipLaunchKernelGGL((small_pair_kernel<T, EPI, false, 1, 2>), grid, dim3(256), 0, s, m);
+  }
+  if (a.out) launch_join<EPI, T>(a, s);
+  if (b.out) launch_join<MM_PLAIN, T>(b, s);
   return hipGetLastError();
 }
 
@@ -1256,6 +1435,15 @@ size_t mm_workspace(MmType type, const MmArgs& a) {
   return std::max(partial_bytes(a, choose(type, a, true)), partial_bytes(a, choose(type, a, false)));
 }
 
+size_t mm_pair_workspace(MmType type, const MmArgs& a, const MmArgs& b) {
+  size_t n = std::max(mm_workspace(type, a), mm_workspace(type, b));
+  for (bool dma : {false, true}) {
+    PairPlan p;
+    if (pair_up(type, a, b, dma, p)) n = std::max(n, pair_bytes(a, b, p));
+  }
+  return n;
+}
+
 hipError_t launch_mm(MmType type, const MmArgs& a, hipStream_t s) {
   switch (type) {
     case MM_BF16: return launch_float<__bf16>(type, a, s);
@@ -1264,6 +1452,21 @@ hipError_t launch_mm(MmType type, const MmArgs& a, hipStream_t s) {
       return a.epi == MM_Q8_GATE ? launch_tiles<int8_t, false, false, MM_Q8_GATE>(type, a, s)
                                  : launch_tiles<int8_t, false, false, MM_Q8>(type, a, s);
   }
+}
+
+hipError_t launch_mm_pair(MmType type, const MmArgs& a, const MmArgs& b, hipStream_t s) {
+  if (!a.out && !b.out) return hipSuccess;
+  const bool dma = can_dma(type, a) && can_dma(type, b);
+  PairPlan p;
+  if (pair_up(type, a, b, dma, p)) {
+    if (type == MM_BF16)
+      return a.epi == MM_PLAIN ? launch_pair<__bf16, MM_PLAIN>(type, a, b, p, dma, s)
+                               : launch_pair<__bf16, MM_GATE_BWD>(type, a, b, p, dma, s);
+    return a.epi == MM_PLAIN ? launch_pair<float, MM_PLAIN>(type, a, b, p, dma, s)
+                             : launch_pair<float, MM_GATE_BWD>(type, a, b, p, dma, s);
+  }
+  const hipError_t e = a.out && a.M > 0 ? launch_mm(type, a, s) : hipSuccess;
+  return e == hipSuccess && b.out ? launch_mm(type, b, s) : e;
 }
 
 }  // namespace tabpack

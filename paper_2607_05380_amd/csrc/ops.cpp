@@ -4,7 +4,6 @@
 #include <cfloat>
 #include <cstdarg>
 #include <cstdio>
-#include <initializer_list>
 
 #include "../../include/tabpack.h"
 #include "ops_internal.h"
@@ -123,8 +122,6 @@ int check_work(const void* work, size_t have, size_t need) {
   return PACK_OK;
 }
 
-size_t largest(std::initializer_list<size_t> v) { return std::max(v); }
-
 }  // namespace
 
 extern "C" {
@@ -135,9 +132,11 @@ int pack_gated_ff_workspace_size(int32_t precision, int64_t tokens, int32_t d_in
   const int rc = check_ff(precision, PACK_ACT_SILU, tokens, d_in, hidden, d_out);
   if (rc != PACK_OK) return rc;
   const MmType t = type_of(precision);
-  *bytes = !backward ? largest({mm_workspace(t, mm_gate(tokens, d_in, hidden)), mm_workspace(t, mm_down(tokens, hidden, d_out))})
-                     : largest({mm_workspace(t, mm_dh(tokens, hidden, d_out)), mm_workspace(t, mm_dx(tokens, d_in, hidden)),
-                                mm_workspace(t, mm_dw(tokens, 2 * hidden, d_in)), mm_workspace(t, mm_dw(tokens, d_out, hidden))});
+  if (!backward)
+    *bytes = std::max(mm_workspace(t, mm_gate(tokens, d_in, hidden)), mm_workspace(t, mm_down(tokens, hidden, d_out)));
+  else
+    *bytes = std::max(mm_pair_workspace(t, mm_dh(tokens, hidden, d_out), mm_dw(tokens, d_out, hidden)),
+                      mm_pair_workspace(t, mm_dx(tokens, d_in, hidden), mm_dw(tokens, 2 * hidden, d_in)));
   return PACK_OK;
 }
 
@@ -188,32 +187,19 @@ int pack_gated_ff_backward(const void* dy, int64_t lddy, const void* x, int64_t 
   if (rc != PACK_OK) return rc;
   const MmType t = type_of(precision);
   const int64_t ldg = 2 * (int64_t)hidden;
-  float* const w = static_cast<float*>(work);
-  if (tokens > 0 && (dx_out || dw_gate_up_out)) {
-    MmArgs a = mm_dh(tokens, hidden, d_out);
-    a.A = dy, a.lda = lddy, a.B = w_down, a.ldb = ldwd, a.act = act, a.pre = const_cast<void*>(gate_up), a.ldpre = ldg;
-    a.out = dgate_up, a.ldo = ldg, a.work = w, a.work_bytes = work_bytes;
-    rc = done("gradients of gate and up", launch_mm(t, a, stream));
-    if (rc != PACK_OK) return rc;
-  }
-  if (tokens > 0 && dx_out) {
-    MmArgs a = mm_dx(tokens, d_in, hidden);
-    a.A = dgate_up, a.lda = ldg, a.B = w_gate_up, a.ldb = ldwg, a.out = dx_out, a.ldo = lddx, a.work = w, a.work_bytes = work_bytes;
-    rc = done("gradient of x", launch_mm(t, a, stream));
-    if (rc != PACK_OK) return rc;
-  }
-  if (dw_gate_up_out) {
-    MmArgs a = mm_dw(tokens, 2 * hidden, d_in);
-    a.A = dgate_up, a.lda = ldg, a.B = x, a.ldb = ldx, a.out = dw_gate_up_out, a.ldo = d_in, a.work = w, a.work_bytes = work_bytes;
-    rc = done("gradient of w_gate_up", launch_mm(t, a, stream));
-    if (rc != PACK_OK) return rc;
-  }
-  if (dw_down_out) {
-    MmArgs a = mm_dw(tokens, d_out, hidden);
-    a.A = dy, a.lda = lddy, a.B = hidden_in, a.ldb = hidden, a.out = dw_down_out, a.ldo = hidden, a.work = w, a.work_bytes = work_bytes;
-    rc = done("gradient of w_down", launch_mm(t, a, stream));
-  }
-  return rc;
+  // [dg | du] beside dw_down, then dx beside dw_gate_up
+  MmArgs dh = mm_dh(tokens, hidden, d_out), dwd = mm_dw(tokens, d_out, hidden);
+  MmArgs dx = mm_dx(tokens, d_in, hidden), dwg = mm_dw(tokens, 2 * hidden, d_in);
+  dh.A = dy, dh.lda = lddy, dh.B = w_down, dh.ldb = ldwd, dh.act = act;
+  dh.pre = const_cast<void*>(gate_up), dh.ldpre = ldg, dh.out = dgate_up, dh.ldo = ldg;
+  dwd.A = dy, dwd.lda = lddy, dwd.B = hidden_in, dwd.ldb = hidden, dwd.out = dw_down_out, dwd.ldo = hidden;
+  dx.A = dgate_up, dx.lda = ldg, dx.B = w_gate_up, dx.ldb = ldwg, dx.out = dx_out, dx.ldo = lddx;
+  dwg.A = dgate_up, dwg.lda = ldg, dwg.B = x, dwg.ldb = ldx, dwg.out = dw_gate_up_out, dwg.ldo = d_in;
+  for (MmArgs* a : {&dh, &dwd, &dx, &dwg}) a->work = static_cast<float*>(work), a->work_bytes = work_bytes;
+  if (!dx_out && !dw_gate_up_out) dh.out = nullptr;
+  hipError_t e = launch_mm_pair(t, dh, dwd, stream);
+  if (e == hipSuccess) e = launch_mm_pair(t, dx, dwg, stream);
+  return done("gated block backward", e);
 }
 
 int pack_q8_matmul_workspace_size(int64_t rows, int32_t outputs, int32_t depth, int32_t gate, size_t* bytes) {

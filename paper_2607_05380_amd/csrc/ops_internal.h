@@ -91,5 +91,11 @@ struct MmArgs {
 // Bytes of `work` that the product needs (0: none).
 size_t mm_workspace(MmType type, const MmArgs& a);
 hipError_t launch_mm(MmType type, const MmArgs& a, hipStream_t s);
+// Two independent products of one type, a with depth-contiguous A and
+// rows-contiguous B (MM_PLAIN or MM_GATE_BWD), b with rows-contiguous operands
+// (MM_PLAIN), the same work given to both: in one launch where that is faster.
+// One whose out is NULL is left out; the other's result does not depend on it.
+size_t mm_pair_workspace(MmType type, const MmArgs& a, const MmArgs& b);
+hipError_t launch_mm_pair(MmType type, const MmArgs& a, const MmArgs& b, hipStream_t s);
 
 }  // namespace tabpack
