@@ -23,6 +23,10 @@ from .tabpack import PackError
 
 _PREC = {torch.bfloat16: 0, torch.float32: 1}
 
+# The current stream's handle without a Stream object around it (a microsecond of a call's ten), where torch has it.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+
 
 def _fail(msg):
     raise PackError(msg)
@@ -34,21 +38,21 @@ def _matrix(t, name, dtype=None, shape=None):
         _fail(f"{name} must be a 2-D device tensor")
     if dtype is not None and t.dtype != dtype:
         _fail(f"{name} must be {dtype}, not {t.dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        _fail(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
-    cols, (ld, inner) = t.shape[1], t.stride()
+    rows, cols = t.shape
+    if shape is not None and (rows, cols) != shape:
+        _fail(f"{name} must have shape {shape}, not {(rows, cols)}")
+    ld, inner = t.stride()
     if inner != 1 and cols > 1:
         _fail(f"{name} must have contiguous rows")
-    if t.shape[0] <= 1:
-        ld = max(ld, cols)
     if ld < cols:
-        _fail(f"{name} must not have overlapping rows")
+        if rows > 1:
+            _fail(f"{name} must not have overlapping rows")
+        ld = cols
     return t.data_ptr(), ld
 
 
 def _vector(t, name, n, dtype=torch.float32):
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and tuple(t.shape) == (n,)
-            and t.is_contiguous()):
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.shape == (n,) and t.is_contiguous()):
         _fail(f"{name} must be a contiguous device tensor of {n} {dtype}")
     return t.data_ptr()
 
@@ -59,18 +63,18 @@ def _prec(t, name):
     return _PREC[t.dtype]
 
 
-def _call(fn, *args, like, others=()):
-    """The library call on the current stream of like's device."""
+def _call(fn, like, others, *args):
+    """The library call on the current stream of like's device (where all of others must be)."""
+    dev = like.get_device()
     for t in others:
-        if t is not None and t.device != like.device:
+        if t is not None and t.get_device() != dev:
             _fail("all tensors must be on one device")
     call = getattr(tabpack.load_library(), fn)
-    dev = like.device.index
     if dev == torch.cuda.current_device():
-        rc = call(*args, torch.cuda.current_stream(dev).cuda_stream)
+        rc = call(*args, _raw_stream(dev))
     else:
         with torch.cuda.device(dev):
-            rc = call(*args, torch.cuda.current_stream(dev).cuda_stream)
+            rc = call(*args, _raw_stream(dev))
     if rc:
         tabpack._check(rc)
 
@@ -84,7 +88,7 @@ def _bytes(fn, *args):
 
 
 def _empty(like, *shape, dtype=None):
-    return torch.empty(shape, dtype=dtype or like.dtype, device=like.device)
+    return like.new_empty(shape, dtype=dtype)
 
 
 def _norm_inputs(x, weight, residual):
@@ -101,8 +105,8 @@ def add_rms_norm(x, weight, residual=None, eps=1e-6):
     a = _norm_inputs(x, weight, residual)
     v = x if residual is None else _empty(x, *x.shape)
     y, rstd = _empty(x, *x.shape), _empty(x, x.shape[0], dtype=torch.float32)
-    _call("pack_add_rms_norm", *a, float(eps), None if residual is None else v.data_ptr(), a[7], y.data_ptr(), a[7],
-          rstd.data_ptr(), like=x, others=(weight, residual))
+    _call("pack_add_rms_norm", x, (weight, residual), *a, float(eps), None if residual is None else v.data_ptr(),
+          a[7], y.data_ptr(), a[7], rstd.data_ptr())
     return y, v, rstd
 
 
@@ -112,8 +116,8 @@ def add_rms_norm_q8(x, weight, residual=None, eps=1e-6):
     a = _norm_inputs(x, weight, residual)
     v = x if residual is None else _empty(x, *x.shape)
     q, scale = _empty(x, *x.shape, dtype=torch.int8), _empty(x, x.shape[0], dtype=torch.float32)
-    _call("pack_add_rms_norm_q8", *a, float(eps), None if residual is None else v.data_ptr(), a[7], q.data_ptr(),
-          a[7], scale.data_ptr(), like=x, others=(weight, residual))
+    _call("pack_add_rms_norm_q8", x, (weight, residual), *a, float(eps), None if residual is None else v.data_ptr(),
+          a[7], q.data_ptr(), a[7], scale.data_ptr())
     return q, scale, v
 
 
@@ -128,8 +132,8 @@ def rms_norm_backward(dy, v, weight, rstd, dv=None):
     wp, rp = _vector(weight, "weight", cols), _vector(rstd, "rstd", rows)
     dx, dw = _empty(v, rows, cols), _empty(v, cols, dtype=torch.float32)
     work = _empty(v, _bytes("pack_rms_norm_backward_workspace_size", rows, cols), dtype=torch.uint8)
-    _call("pack_rms_norm_backward", yp, ldy, vp, ldv, wp, rp, dp, ldd, prec, rows, cols, dx.data_ptr(), cols,
-          dw.data_ptr(), work.data_ptr(), work.numel(), like=v, others=(dy, weight, rstd, dv))
+    _call("pack_rms_norm_backward", v, (dy, weight, rstd, dv), yp, ldy, vp, ldv, wp, rp, dp, ldd, prec, rows, cols,
+          dx.data_ptr(), cols, dw.data_ptr(), work.data_ptr(), work.numel())
     return dx, dw
 
 
@@ -139,7 +143,7 @@ def quantize_rows(x):
     xp, ldx = _matrix(x, "x")
     rows, cols = x.shape
     q, scale = _empty(x, rows, cols, dtype=torch.int8), _empty(x, rows, dtype=torch.float32)
-    _call("pack_quantize_rows", xp, ldx, prec, rows, cols, q.data_ptr(), cols, scale.data_ptr(), like=x)
+    _call("pack_quantize_rows", x, (), xp, ldx, prec, rows, cols, q.data_ptr(), cols, scale.data_ptr())
     return q, scale
 
 
@@ -162,9 +166,8 @@ def distill_topk(logits, idx, teacher, temperature=1.0, row_weight=None, grad=Tr
     wp = None if row_weight is None else _vector(row_weight, "row_weight", rows)
     loss = _empty(logits, rows, dtype=torch.float32)
     g = _empty(logits, rows, classes) if grad else None
-    _call("pack_distill_topk", zp, ldz, prec, rows, classes, idx.data_ptr(), teacher.data_ptr(), k,
-          float(temperature), wp, loss.data_ptr(), g.data_ptr() if grad else None, classes, like=logits,
-          others=(idx, teacher, row_weight))
+    _call("pack_distill_topk", logits, (idx, teacher, row_weight), zp, ldz, prec, rows, classes, idx.data_ptr(),
+          teacher.data_ptr(), k, float(temperature), wp, loss.data_ptr(), g.data_ptr() if grad else None, classes)
     return loss, g
 
 
@@ -200,9 +203,9 @@ def gated_ff(x, w_gate_up, w_down, act="silu", residual=None, save=False):
     gu = _empty(x, tokens, 2 * hidden) if save else None
     h, y = _empty(x, tokens, hidden), _empty(x, tokens, d_out)
     work = _work(x, "pack_gated_ff_workspace_size", prec, *dims, 0)
-    _call("pack_gated_ff_forward", *ptrs, rp, ldr, prec, code, *dims, gu.data_ptr() if save else None, h.data_ptr(),
-          y.data_ptr(), d_out, None if work is None else work.data_ptr(), 0 if work is None else work.numel(),
-          like=x, others=(w_gate_up, w_down, residual))
+    _call("pack_gated_ff_forward", x, (w_gate_up, w_down, residual), *ptrs, rp, ldr, prec, code, *dims,
+          gu.data_ptr() if save else None, h.data_ptr(), y.data_ptr(), d_out,
+          None if work is None else work.data_ptr(), 0 if work is None else work.numel())
     return (y, (gu, h)) if save else y
 
 
@@ -222,10 +225,9 @@ def gated_ff_backward(dy, x, w_gate_up, w_down, saved, act="silu", need_dx=True)
     dx = _empty(x, tokens, d_in) if need_dx else None
     dwg, dwd = _empty(x, 2 * hidden, d_in), _empty(x, d_out, hidden)
     work = _work(x, "pack_gated_ff_workspace_size", prec, *dims, 1)
-    _call("pack_gated_ff_backward", gp, ldg, *ptrs, gu.data_ptr(), h.data_ptr(), prec, code, *dims, dgu.data_ptr(),
-          dx.data_ptr() if need_dx else None, d_in, dwg.data_ptr(), dwd.data_ptr(),
-          None if work is None else work.data_ptr(), 0 if work is None else work.numel(), like=x,
-          others=(dy, w_gate_up, w_down, gu, h))
+    _call("pack_gated_ff_backward", x, (dy, w_gate_up, w_down, gu, h), gp, ldg, *ptrs, gu.data_ptr(), h.data_ptr(),
+          prec, code, *dims, dgu.data_ptr(), dx.data_ptr() if need_dx else None, d_in, dwg.data_ptr(), dwd.data_ptr(),
+          None if work is None else work.data_ptr(), 0 if work is None else work.numel())
     return dx, dwg, dwd
 
 
@@ -249,7 +251,7 @@ def q8_matmul(q, scale, w, w_scale, bias=None, gate=None, dtype=torch.bfloat16):
     outputs = n if gate is None else n // 2
     out = _empty(q, rows, outputs, dtype=dtype)
     work = _work(q, "pack_q8_matmul_workspace_size", rows, outputs, depth, code)
-    _call("pack_q8_matmul", qp, ldq, sp, wp, ldw, wsp, bp, code, _PREC[dtype], rows, outputs, depth, out.data_ptr(),
-          outputs, None if work is None else work.data_ptr(), 0 if work is None else work.numel(), like=q,
-          others=(scale, w, w_scale, bias))
+    _call("pack_q8_matmul", q, (scale, w, w_scale, bias), qp, ldq, sp, wp, ldw, wsp, bp, code, _PREC[dtype], rows,
+          outputs, depth, out.data_ptr(), outputs, None if work is None else work.data_ptr(),
+          0 if work is None else work.numel())
     return out
