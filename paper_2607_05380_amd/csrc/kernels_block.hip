@@ -517,7 +517,7 @@ struct Reg {
   int64_t ld;
   int64_t row[NV];  // operand row (rows-contiguous: element) of the vector, or -1
   int64_t rbound;
-  u32x4 v[NV];
+  u32x4 v[2][NV];  // two K steps
   template <typename F>
   __device__ __forceinline__ void init(const void* P, int64_t ld_, int64_t rbound_, int tid, F grow) {
     base = static_cast<const T*>(P);
@@ -529,11 +529,12 @@ struct Reg {
       row[i] = RM ? grow((q % VPR) * VE) : grow(q / VPR);
     }
   }
+  template <int S>
   __device__ __forceinline__ void load(int64_t k0, int64_t kend, int tid) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int q = tid + i * 256;
-      v[i] = u32x4{0, 0, 0, 0};
+      v[S][i] = u32x4{0, 0, 0, 0};
       int64_t left;  // elements of the vector that exist
       const T* p;
       if constexpr (RM) {
@@ -546,15 +547,16 @@ struct Reg {
         p = base + row[i] * ld + k;
       }
       if (left >= VE) {
-        v[i] = load16(p);
+        v[S][i] = load16(p);
       } else if (left > 0) {
         T e[VE];
 #pragma unroll
         for (int j = 0; j < VE; ++j) e[j] = j < left ? p[j] : (T)0;
-        __builtin_memcpy(&v[i], e, 16);
+        __builtin_memcpy(&v[S][i], e, 16);
       }
     }
   }
+  template <int S>
   __device__ __forceinline__ void store(char* lds, int tid) const {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -566,7 +568,7 @@ struct Reg {
         off = rmaj_off<R>(q / VPR, (q % VPR) * VE);
       else
         off = (q / VPR) * (4 * R) + (q % VPR) * 16;
-      *reinterpret_cast<u32x4*>(lds + off) = v[i];
+      *reinterpret_cast<u32x4*>(lds + off) = v[S][i];
     }
   }
 };
@@ -752,18 +754,15 @@ __device__ __forceinline__ void small_tile(const MmArgs& a, uint32_t block, char
     Reg<T, RB, R> lb;
     la.init(A, a.lda, a.M - m0, tid, grow_a);
     lb.init(B, a.ldb, a.N - n0, tid, grow_b);
-    la.load(kbeg, kend, tid);
-    lb.load(kbeg, kend, tid);
-#pragma unroll 1
-    for (int kt = 0; kt < nk; ++kt) {
-      char* const cur = smem + (kt & 1) * 2 * REGION;
-      la.store(cur, tid);
-      lb.store(cur + REGION, tid);
+    // step kt, whose vectors are in register set and LDS stage S; set S takes step kt + 2
+    auto step = [&](auto set, int kt) {
+      constexpr int S = decltype(set)::value;
+      char* const cur = smem + S * 2 * REGION;
+      la.template store<S>(cur, tid);
+      lb.template store<S>(cur + REGION, tid);
       __syncthreads();  // the other stage was read before the barrier of the step before this one's stores
-      if (kt + 1 < nk) {
-        la.load(kbeg + (int64_t)(kt + 1) * KE, kend, tid);
-        lb.load(kbeg + (int64_t)(kt + 1) * KE, kend, tid);
-      }
+      la.template load<S>(kbeg + (int64_t)(kt + 2) * KE, kend, tid);
+      lb.template load<S>(kbeg + (int64_t)(kt + 2) * KE, kend, tid);
 #pragma unroll
       for (int ks = 0; ks < 4; ++ks) {
         bf16x8 fa[NB], fb[NB];
@@ -776,6 +775,17 @@ __device__ __forceinline__ void small_tile(const MmArgs& a, uint32_t block, char
 #pragma unroll
           for (int j = 0; j < NB; ++j) mma(fb[j], fa[i], acc[i][j], T());
       }
+    };
+    using S0 = std::integral_constant<int, 0>;
+    using S1 = std::integral_constant<int, 1>;
+    la.template load<0>(kbeg, kend, tid);
+    lb.template load<0>(kbeg, kend, tid);
+    la.template load<1>(kbeg + KE, kend, tid);
+    lb.template load<1>(kbeg + KE, kend, tid);
+#pragma unroll 1
+    for (int kt = 0; kt < nk; kt += 2) {
+      step(S0{}, kt);
+      if (kt + 1 < nk) step(S1{}, kt + 1);
     }
   }
   wait_vm<0, true>();
@@ -1206,7 +1216,7 @@ double step_us(MmType type, Tiles t, bool dma, double wgs) {
 double start_us(Tiles t) { return t == TILES_HUGE ? 7 : 3.3; }
 double join_us(const MmArgs& a, const Plan& p) {
   if (p.splits < 2) return 0;
-  return 2.5 + p.splits * (double)a.M * ((a.N + 7) / 8 * 8) * (is_gate(a.epi) ? 16 : 8) / 3.5e6;
+  return 4 + p.splits * (double)a.M * ((a.N + 7) / 8 * 8) * (is_gate(a.epi) ? 16 : 8) / 3.5e6;
 }
 constexpr int64_t kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
 
@@ -1287,7 +1297,7 @@ void launch_thin(const MmArgs& a, dim3 grid, hipStream_t s) {
 uint32_t apply(MmArgs& a, const Plan& p) {
   a.tiles_m = (int)p.tm, a.tiles_n = (int)p.tn, a.splits = p.splits, a.steps_per_split = p.steps;
   const int64_t blocks = p.tm * p.tn * p.splits;
-  return blocks <= (1 << 21) ? (uint32_t)blocks : 0;  // (a launch is limited to 2^32 threads)
+  return blocks <= (1 << 22) ? (uint32_t)blocks : 0;  // (a launch is limited to 2^32 threads, m0 to 2^31)
 }
 
 template <int EPI, typename T>

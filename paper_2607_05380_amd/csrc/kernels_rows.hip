@@ -4,7 +4,7 @@
 //
 // Each does a few operations a byte, so the bytes of one read and one write
 // bound it.  A row is read once into the registers of the G threads that own
-// it (16 to 1024, EPT elements each, by the row's length), reduced there, and
+// it (4 to 1024, EPT elements each, by the row's length), reduced there, and
 // written from there.  Thread t of a row owns the vectors t, t + G, t + 2G, ...
 // of VE elements (16 bytes), so a wave's accesses are contiguous.  Vectors are
 // accessed at any alignment of the element (the global memory path splits what
@@ -279,21 +279,24 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void norm_bwd_kernel(NormBwdArgs
         os[i].raw = u32x4{0, 0, 0, 0};
     }
     const float rho = a.rstd[row];
-    float v[EPT], g[EPT];
-    float dot = 0.0f;
+    // bf16 keeps v and g as floats; fp32 multiplies by the weight, read again from
+    // the cache, a second time (16,384 x 4096: bf16 93 us against 99 the other
+    // way, fp32 156 against 183)
+    constexpr bool KEEP = sizeof(T) == 2;
+    float kv[KEEP ? EPT : 1], kg[KEEP ? EPT : 1], dot = 0.0f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (i * G + t) * VE;
-      float w[VE];
+      float w[VE], v[VE], g[VE];
       load_weight<VE>(a.weight + c, w, a.cols - c);
-      vs[i].get(v + i * VE);
-      gs[i].get(g + i * VE);
+      vs[i].get(v);
+      gs[i].get(g);
 #pragma unroll
       for (int e = 0; e < VE; ++e) {
-        float& gg = g[i * VE + e];
-        dw[i * VE + e] = fmaf(gg * v[i * VE + e], rho, dw[i * VE + e]);
-        gg *= w[e];
-        dot = fmaf(gg, v[i * VE + e], dot);
+        dw[i * VE + e] = fmaf(g[e] * v[e], rho, dw[i * VE + e]);
+        g[e] *= w[e];
+        dot = fmaf(g[e], v[e], dot);
+        if constexpr (KEEP) kv[i * VE + e] = v[e], kg[i * VE + e] = g[e];
       }
     }
     dot = reduce_row<G, OpAdd>(dot, red[turn], tid);
@@ -302,10 +305,21 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void norm_bwd_kernel(NormBwdArgs
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (i * G + t) * VE;
-      float o[VE];
+      float v[VE], g[VE], o[VE];
+      if constexpr (KEEP) {
+#pragma unroll
+        for (int e = 0; e < VE; ++e) v[e] = kv[i * VE + e], g[e] = kg[i * VE + e];
+      } else {
+        float w[VE];
+        load_weight<VE>(a.weight + c, w, a.cols - c);
+        vs[i].get(v);
+        gs[i].get(g);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) g[e] *= w[e];
+      }
       os[i].get(o);
 #pragma unroll
-      for (int e = 0; e < VE; ++e) o[e] = fmaf(rho, g[i * VE + e] - v[i * VE + e] * c1, o[e]);
+      for (int e = 0; e < VE; ++e) o[e] = fmaf(rho, g[e] - v[e] * c1, o[e]);
       store_vec(dx + c, o, a.cols - c);
     }
   }
@@ -553,6 +567,8 @@ hipError_t rows_t(const RowArgs& a, hipStream_t s) {
                        dim3(G > 256 ? G : 256), 0, s, a);                                           \
     return hipGetLastError();                                                                       \
   }
+  TABPACK_ROWS(4, 8)
+  TABPACK_ROWS(16, 8)
   TABPACK_ROWS(64, 8)
   TABPACK_ROWS(64, 16)
   TABPACK_ROWS(64, 32)
@@ -582,6 +598,8 @@ hipError_t norm_bwd_t(const NormBwdArgs& a, hipStream_t s) {
                        a.dweight);                                                                           \
     return hipGetLastError();                                                                                \
   }
+  TABPACK_NORM_BWD(4, 8)
+  TABPACK_NORM_BWD(16, 8)
   TABPACK_NORM_BWD(64, 8)
   TABPACK_NORM_BWD(64, 16)
   TABPACK_NORM_BWD(64, 32)
@@ -601,6 +619,9 @@ hipError_t distill_t(const DistillArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((distill_kernel<T, G, EPT, STREAM>), dim3(row_blocks(a.rows, RPB)),     \
                        dim3(G > 256 ? G : 256), RPB * teacher_bytes(a.k), s, a);                               \
     return hipGetLastError();                                                                                  \
+  }
+  if (a.k <= 32) {  // (64 rows' entries in LDS)
+    TABPACK_DISTILL(4, 8, false)
   }
   TABPACK_DISTILL(16, 8, false)
   TABPACK_DISTILL(64, 16, false)
@@ -622,7 +643,7 @@ hipError_t launch_rows(int prec, RowMode mode, const RowArgs& a, hipStream_t s) 
 // rows that share a block's weight sums: enough blocks to fill the chip four
 // times over, few enough that adding up their sums is a small part
 int norm_bwd_blocks(int64_t rows, int32_t cols) {
-  const int64_t per = cols <= 2048 ? 4 : 1;  // rows a block takes at a time
+  const int64_t per = cols <= 32 ? 64 : cols <= 128 ? 16 : cols <= 2048 ? 4 : 1;  // rows a block takes at a time
   const int64_t want = (rows + per - 1) / per;
   return (int)(want < 1024 ? (want > 0 ? want : 1) : 1024);
 }

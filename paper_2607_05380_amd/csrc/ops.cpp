@@ -25,6 +25,7 @@ int bad(const char* fmt, ...) {
 
 int done(const char* what, hipError_t e) {
   if (e == hipSuccess) return PACK_OK;
+  if (e == hipErrorInvalidConfiguration) return bad("%s: more tiles than a launch holds", what);
   char buf[256];
   snprintf(buf, sizeof buf, "%s: %s", what, hipGetErrorString(e));
   return set_error(PACK_EHIP, buf);
