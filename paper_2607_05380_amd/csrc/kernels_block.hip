@@ -75,13 +75,9 @@ constexpr bool is_q8(int epi) { return epi == MM_Q8 || epi == MM_Q8_GATE; }
 
 // -------------------------------------------------------------- activations --
 __device__ __forceinline__ float exp_neg(float x) { return __builtin_amdgcn_exp2f(x * -1.4426950408889634f); }
-// the logistic function; FAST: results that are rounded to bf16 take the
-// hardware reciprocal (1 ulp)
-template <bool FAST>
-__device__ __forceinline__ float logistic(float x) {
-  const float d = 1.0f + exp_neg(x);
-  return FAST ? __builtin_amdgcn_rcpf(d) : 1.0f / d;
-}
+// the logistic function, with the hardware's reciprocal (1 ulp; a division
+// costs ten instructions more)
+__device__ __forceinline__ float logistic(float x) { return __builtin_amdgcn_rcpf(1.0f + exp_neg(x)); }
 constexpr float kInvSqrt2Pi = 0.39894228040143268f;
 // The normal distribution function at g, with e = exp(-g^2 / 2): Abramowitz and
 // Stegun 7.1.26 (erf to within 1.5e-7) for the tail beyond |g|, so that small
@@ -100,11 +96,10 @@ __device__ __forceinline__ float exp_half_square(float g) {
 }
 
 // c <- act(c) u, 8 values (the choice of the activation outside their loop)
-template <bool FAST>
 __device__ __forceinline__ void gate8(int act, float* c, const float* u) {
   if (act == PACK_ACT_SILU) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) c[i] = c[i] * logistic<FAST>(c[i]) * u[i];
+    for (int i = 0; i < 8; ++i) c[i] = c[i] * logistic(c[i]) * u[i];
   } else if (act == PACK_ACT_GELU) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) c[i] = c[i] * normal_cdf(c[i], exp_half_square(c[i])) * u[i];
@@ -114,12 +109,11 @@ __device__ __forceinline__ void gate8(int act, float* c, const float* u) {
   }
 }
 // g <- d u act'(g) and u <- d act(g): the gradients of gate and up from d = dh
-template <bool FAST>
 __device__ __forceinline__ void gate8_grad(int act, const float* d, float* g, float* u) {
   if (act == PACK_ACT_SILU) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float p = logistic<FAST>(g[i]), v = g[i] * p;
+      const float p = logistic(g[i]), v = g[i] * p;
       g[i] = d[i] * u[i] * (p + v * (1.0f - p));
       u[i] = d[i] * v;
     }
@@ -218,19 +212,20 @@ struct Q8Cols {
   Raw8<float> scale, bias;
   __device__ __forceinline__ void load(const MmArgs& a, int n, int cnt) {
     scale.template load_some<PART>(a.col_scale + n, cnt);
-    if (a.bias) {
-      bias.template load_some<PART>(a.bias + n, cnt);
-    } else {
-      bias.v[0] = bias.v[1] = u32x4{0, 0, 0, 0};
-    }
+    if (a.bias) bias.template load_some<PART>(a.bias + n, cnt);
   }
   // sums in int32 -> values
-  __device__ __forceinline__ void apply(float* c, float row_scale) const {
-    float s[8], b[8];
+  __device__ __forceinline__ void apply(const MmArgs& a, float* c, float row_scale) const {
+    float s[8];
     scale.get(s);
-    bias.get(b);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) c[i] = (float)__builtin_bit_cast(int32_t, c[i]) * (row_scale * s[i]) + b[i];
+    for (int i = 0; i < 8; ++i) c[i] = (float)__builtin_bit_cast(int32_t, c[i]) * (row_scale * s[i]);
+    if (a.bias) {
+      float b[8];
+      bias.get(b);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) c[i] += b[i];
+    }
   }
 };
 template <int EPI, typename T, bool PART>
@@ -263,12 +258,11 @@ struct Extra {
 template <int EPI, typename T, bool PART>
 __device__ __forceinline__ void finish8(const MmArgs& a, int64_t m, int n, float* c, float* u,
                                         const Cols<EPI, T, PART>& cols, const Extra<EPI, T, PART>& x, int cnt) {
-  constexpr bool FAST = sizeof(T) == 2;
   if constexpr (is_q8(EPI)) {
-    cols.gate.apply(c, x.row_scale);
+    cols.gate.apply(a, c, x.row_scale);
     if constexpr (EPI == MM_Q8_GATE) {
-      cols.up.apply(u, x.row_scale);
-      gate8<false>(a.act, c, u);
+      cols.up.apply(a, u, x.row_scale);
+      gate8(a.act, c, u);
     }
     if (a.out_f32)
       store_some<PART>(static_cast<float*>(a.out) + m * a.ldo + n, c, cnt);
@@ -288,14 +282,14 @@ __device__ __forceinline__ void finish8(const MmArgs& a, int64_t m, int n, float
       store_some<PART>(p, c, cnt);
       store_some<PART>(p + a.N, u, cnt);
     }
-    gate8<FAST>(a.act, c, u);
+    gate8(a.act, c, u);
     store_some<PART>(static_cast<T*>(a.out) + m * a.ldo + n, c, cnt);
   } else {
     static_assert(EPI == MM_GATE_BWD);
     float g[8], w[8];
     x.g.get(g);
     x.u.get(w);
-    gate8_grad<FAST>(a.act, c, g, w);
+    gate8_grad(a.act, c, g, w);
     T* o = static_cast<T*>(a.out) + m * a.ldo + n;
     store_some<PART>(o, g, cnt);
     store_some<PART>(o + a.N, w, cnt);

@@ -36,7 +36,10 @@ EPIS = ["fwd", "fwd_eval", "dx", "dw", "ns", "de"]
 SIMPLE = ["dropout_words", "grad_sums", "head_fwd", "head_bwd", "head_train", "gather", "rows_to_bf16", "to_shadow",
           "eval_score", "dropout_mask", "select_partial", "select_pick", "select_update", "select_init", "select_final",
           "ensemble_mean", "muon_prep", "muon_norm", "muon_convert", "muon_update", "embed_table", "embed_grad",
-          "idx_check", "stream_copy"]
+          "idx_check", "stream_copy", "norm_bwd", "norm_dw", "rows", "distill"]
+# kernels of the student's operators: matrix products by tiles, operand kinds and epilogue, row kernels by mode
+MM_EPIS = ["plain", "gate", "gate_bwd", "q8", "q8_gate"]
+ROW_MODES = ["norm", "norm_q8", "quantize"]
 
 
 def source_digest():
@@ -83,6 +86,15 @@ def short_name(kernel):
         if epi >= len(EPIS) or ak >= len(OPS) or bk >= len(OPS):
             return None
         return f"gemm_{t}_{OPS[ak]}_{OPS[bk]}_{EPIS[epi]}"
+    m = re.search(r"\d(small|small_pair|huge|thin|join)_kernelI(DF16b|f|a)?((?:Lb\dE)*)Li(\d)E(DF16b|f|a)?", kernel)
+    if m:
+        t = {"DF16b": "bf16", "f": "f32", "a": "i8"}[m.group(2) or m.group(5)]
+        ops = "" if m.group(1) != "small" and m.group(1) != "huge" else "_" + "".join(
+            "kr"[int(b)] for b in re.findall(r"Lb(\d)E", m.group(3))[:2])
+        return f"mm_{m.group(1)}_{t}{ops}_{MM_EPIS[int(m.group(4))]}"
+    m = re.search(r"\drows_kernelI(DF16b|f)Li\d+ELi\d+ELi(\d)E", kernel)
+    if m:
+        return f"rows_{'f32' if m.group(1) == 'f' else 'bf16'}_{ROW_MODES[int(m.group(2))]}"
     for s in sorted(SIMPLE, key=len, reverse=True):
         if s + "_kernel" in kernel:
             return s
