@@ -16,18 +16,24 @@
 // lane's accumulators hold both values of an output: the activation and the
 // product cost no pass over memory.
 //
-// A K step is 128 bytes of depth (64 bf16, 128 int8, 32 fp32) of 128-row
-// regions of 16 KB.  Tiles:
+// A K step is 128 bytes of depth (64 bf16, 128 int8, 32 fp32).  Tiles (times:
+// bf16 products of M x N x K):
 //   small  128 x 128, 4 waves of 64 x 64, two steps in LDS (64 KB), two
 //          workgroups per CU.  Operands that do not start rows at 16 bytes or
-//          end inside a 16-byte vector, and fp32, pass through registers; the
-//          rest go straight to LDS.
-//   huge   256 x 256, 8 waves of 128 x 64, two steps in LDS (128 KB), one
-//          workgroup per CU (see huge_kernel).
+//          end inside a 16-byte vector, and fp32, pass through registers, two
+//          steps ahead; the rest go straight to LDS.  2048 x 4096 x 1024 22 us
+//          (0.8 PFLOP/s; huge 30, mini 31), through registers 31.
+//   huge   256 x 256, 8 waves of 128 x 64, 160 KB of LDS, one workgroup per CU
+//          (see huge_tile).  16,384 x 1024 x 4096 107 us (1.29 PFLOP/s; small
+//          128), where a large library product reaches 1.42.
 //   mini   64 x 64, 4 waves of 32 x 32, four steps in LDS (64 KB); for products
-//          whose larger tiles would leave CUs idle.
+//          whose larger tiles would leave CUs idle.  2048 x 1024 x 1024 10 us
+//          (small 13.5, huge 24).
 //   thin   up to 16 rows of A, 16 columns, no LDS for operands: each weight
 //          byte is read once (see thin_kernel).
+// What bounds the large tiles is power: with random operands the MFMAs alone,
+// without loads or LDS reads, take 0.82 of the time of the whole loop, and with
+// zeros the loop is 1.4 times faster.
 // MFMAs: v_mfma_f32_32x32x16_bf16, v_mfma_i32_32x32x32_i8,
 // v_mfma_f32_32x32x2_f32, with B as the first operand, so that a lane holds 4
 // consecutive columns of one row of C.  Accumulators are fp32 or int32, added
@@ -609,7 +615,8 @@ __device__ __forceinline__ bf16x8 frag_reg(const char* lds, int row, int ks, int
     f32x4 f;
     const int k = 8 * ks + 4 * (lane >> 5);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) f[e] = *reinterpret_cast<const float*>(lds + (k + e) * (4 * R) + (row + (lane & 31)) * 4);
+    for (int e = 0; e < 4; ++e)
+      f[e] = *reinterpret_cast<const float*>(lds + (k + e) * (4 * R) + (row + (lane & 31)) * 4);
     return __builtin_bit_cast(bf16x8, f);
   }
 }
@@ -1058,9 +1065,12 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 // depth in strips of 256 bytes, and every weight byte is read once, straight
 // into MFMA operands (16 x 16 blocks; lane l holds 16 bytes of depth of row
 // l % 16).  The loads bound it: a strip's are all issued before its products,
-// at any alignment.  The waves' sums meet in LDS, added in order.
+// at any alignment.  The waves' sums meet in LDS, added in order.  One row, 4096
+// gated outputs, depth 1024: int8 4.0 us (2.1 TB/s of weights, a third of it the
+// launch), bf16 5.3; 4096 gated outputs at depth 4096 bf16 14 us (4.7 TB/s).
 __device__ __forceinline__ void mma16(u32x4 b, u32x4 a, f32x4& acc, __bf16) {
-  acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a), acc, 0, 0, 0);
+  acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a), acc, 0,
+                                                0, 0);
 }
 __device__ __forceinline__ void mma16(u32x4 b, u32x4 a, i32x4& acc, int8_t) {
   acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, b), __builtin_bit_cast(i32x4, a), acc, 0, 0, 0);

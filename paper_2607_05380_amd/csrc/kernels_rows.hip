@@ -10,6 +10,15 @@
 // accessed at any alignment of the element (the global memory path splits what
 // crosses a line); the one that the row's end cuts is accessed by elements.
 // Sums are held in fp32 and added in a fixed order.
+//
+// Measured on tensors larger than the caches, against 5.1 TB/s of a device copy:
+// norm with residual 65,536 x 1024 bf16 93 us (5.8 TB/s of reads and writes),
+// with 8-bit output 88 us, its backward with both gradients 106 us (5.1 TB/s),
+// quantising 35 us (5.8 TB/s); 500,000 x 64 bf16 norm 52 us (4 and 16 threads a
+// row: a wave a row takes 181); distillation 4096 x 32,000 bf16 with 32 entries
+// a row 120 us (4.4 TB/s).  Odd lengths (4095) cost up to 1.3 times the time in
+// bf16, whose stores then share their lines; rows of 32,768 in the backward pass
+// 4 times, whose column sums no longer fit the registers.
 #include "ops_internal.h"
 #include "../../include/tabpack.h"
 
@@ -376,7 +385,9 @@ __global__ __launch_bounds__(1024) void norm_dw_kernel(const float* partial, int
 // threads take the teacher's entries meanwhile.  The gradient is written as
 // weight tau q first and the classes of the teacher's entries are then written
 // again by their threads; a class that several entries name is written by the
-// first of them with all their p.
+// first of them with all their p.  512 threads hold up to 32,768 classes, so two
+// rows share a CU and one's reads run beside the other's exponentials (1024
+// threads with one row a CU: 233 us for the case above).
 struct Teacher {  // LDS of one row: k entries of each, and the sum
   int32_t* idx;  // class, or -1
   float* p;      // logit, then p
@@ -507,7 +518,8 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void distill_kernel(DistillArgs 
       }
 #pragma unroll
       for (int m = W / 2; m >= 1; m >>= 1) loss += __shfl_xor(loss, m, 64);
-      if (in && t == 0) a.loss[row] = zero ? 0.0f : tsum != tsum || total != total ? __builtin_nanf("") : wt * a.tau * loss;
+      if (in && t == 0)
+        a.loss[row] = zero ? 0.0f : tsum != tsum || total != total ? __builtin_nanf("") : wt * a.tau * loss;
     }
     if (a.grad) {
       T* g = static_cast<T*>(a.grad) + row * a.ldg;

@@ -57,7 +57,8 @@ class Student:
         keep, branch, v = [], None, x
         for b in range(self.blocks):
             norm, wg, wd = self.w[3 * b:3 * b + 3]
-            n, v, rstd = ops.add_rms_norm(v if branch is None else branch, norm, None if branch is None else v, self.eps)
+            new, stream = (v, None) if branch is None else (branch, v)
+            n, v, rstd = ops.add_rms_norm(new, norm, stream, self.eps)
             branch, saved = ops.gated_ff(n, wg, wd, act=self.act, save=True)
             keep.append((n, v, rstd, saved))
         n, v, rstd = ops.add_rms_norm(branch, self.w[-2], v, self.eps)
@@ -109,7 +110,8 @@ class Student:
         branch, v = None, X.to(torch.bfloat16)
         for b in range(self.blocks):
             norm, (wg, sg), (wd, sd) = self.served[3 * b:3 * b + 3]
-            q, s, v = ops.add_rms_norm_q8(v if branch is None else branch, norm, None if branch is None else v, self.eps)
+            new, stream = (v, None) if branch is None else (branch, v)
+            q, s, v = ops.add_rms_norm_q8(new, norm, stream, self.eps)
             q, s = ops.quantize_rows(ops.q8_matmul(q, s, wg, sg, gate=self.act))
             branch = ops.q8_matmul(q, s, wd, sd)
         q, s, _ = ops.add_rms_norm_q8(branch, self.served[-2], v, self.eps)
