@@ -449,12 +449,16 @@ int pack_distill_topk(const void* logits, int64_t ldz, int32_t precision, int64_
  *   residual     device [tokens, d_out] or NULL
  *   gate_up_out  device [tokens, 2 hidden], dense: g and u for the backward
  *                pass, or NULL
- *   hidden_out   device [tokens, hidden], dense: h
+ *   hidden_out   device [tokens, hidden]: h, rows PACK_FF_LD(precision, hidden)
+ *                apart (the product with w_down then reads it at 16 bytes), zeros
+ *                behind their ends
  *   out          device [tokens, d_out]
  *   work         device scratch, 16-byte aligned, of
  *                pack_gated_ff_workspace_size(..., backward = 0) bytes
  * All matrices are in the precision; h and the saved g and u are rounded to it
- * (h is formed from the unrounded ones). */
+ * (h is formed from the unrounded ones): h feeds matrix instructions, and the
+ * saved values in fp32 would double the largest traffic of a training step. */
+#define PACK_FF_LD(precision, cols) ((precision) == PACK_PREC_BF16 ? ((cols) + 7) / 8 * 8 : (cols))
 int pack_gated_ff_workspace_size(int32_t precision, int64_t tokens, int32_t d_in, int32_t hidden, int32_t d_out,
                                  int32_t backward, size_t* bytes);
 int pack_gated_ff_forward(const void* x, int64_t ldx, const void* w_gate_up, int64_t ldwg, const void* w_down,
@@ -467,10 +471,12 @@ int pack_gated_ff_forward(const void* x, int64_t ldx, const void* w_gate_up, int
  * wrote them (the residual's gradient is dy itself):
  *   dh = dy w_down,  dg = dh u act'(g),  du = dh act(g),
  *   dx = [dg | du] w_gate_up,  dw_gate_up = [dg | du]^T x,  dw_down = dy^T h
- *   dgate_up     device [tokens, 2 hidden], dense: dg and du (scratch of the call)
+ *   dgate_up     device [tokens, 2 hidden], rows PACK_FF_LD(precision, 2 hidden)
+ *                apart: dg and du (scratch of the call)
  *   dx_out       device [tokens, d_in]; dw_gate_up_out [2 hidden, d_in] and
  *                dw_down_out [d_out, hidden], dense; each may be NULL
- * relu'(0) is 0. */
+ * dg and du, formed in fp32 from the saved values, are rounded to the precision
+ * once: the matrix instructions take their operands in it.  relu'(0) is 0. */
 int pack_gated_ff_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* w_gate_up,
                            int64_t ldwg, const void* w_down, int64_t ldwd, const void* gate_up, const void* hidden_in,
                            int32_t precision, int32_t act, int64_t tokens, int32_t d_in, int32_t hidden,

@@ -19,9 +19,10 @@
 // A K step is 128 bytes of depth (64 bf16, 128 int8, 32 fp32).  Tiles (times:
 // bf16 products of M x N x K):
 //   small  128 x 128, 4 waves of 64 x 64, two steps in LDS (64 KB), two
-//          workgroups per CU.  Operands that do not start rows at 16 bytes or
-//          end inside a 16-byte vector, and fp32, pass through registers, two
-//          steps ahead; the rest go straight to LDS.  2048 x 4096 x 1024 22 us
+//          workgroups per CU.  Operands go straight to LDS; fp32, and operands
+//          whose rows do not start at 16 bytes or end inside a 16-byte vector
+//          where copying them first takes longer (see copies()), pass through
+//          registers, two steps ahead.  2048 x 4096 x 1024 22 us
 //          (0.8 PFLOP/s; huge 30, mini 31), through registers 31.
 //   huge   256 x 256, 8 waves of 128 x 64, 160 KB of LDS, one workgroup per CU
 //          (see huge_tile).  16,384 x 1024 x 4096 107 us (1.29 PFLOP/s; small
@@ -38,7 +39,11 @@
 // v_mfma_f32_32x32x2_f32, with B as the first operand, so that a lane holds 4
 // consecutive columns of one row of C.  Accumulators are fp32 or int32, added
 // in a fixed order; a depth split over workgroups is joined in a fixed order
-// by a second kernel.
+// by a second kernel.  What is rounded to bf16 between two products (h, the saved
+// g and u, dg and du) is rounded once, from fp32: the next product's
+// instructions take bf16, and fp32 copies would double the bytes of the gate
+// epilogues, which already are a third of those kernels' time (16,384 x 4096 x
+// 1024, backward 205 us, 670 MB).
 #include <algorithm>
 #include <cmath>
 
@@ -259,6 +264,14 @@ struct Extra {
   }
 };
 
+// The columns behind a row of an output whose rows are padded to 16 bytes
+// (there are some only if the row ends in a partial piece of 8 columns).
+template <typename T>
+__device__ __forceinline__ void zero_pad(const MmArgs& a, T* p) {
+#pragma unroll 1
+  for (int i = 0; i < a.pad; ++i) p[i] = (T)0;
+}
+
 // The outputs n .. n + 7 (PART: the first cnt) of row m from the sums c (gated:
 // gate sums c, up sums u), which are consumed.
 template <int EPI, typename T, bool PART>
@@ -290,6 +303,7 @@ __device__ __forceinline__ void finish8(const MmArgs& a, int64_t m, int n, float
     }
     gate8(a.act, c, u);
     store_some<PART>(static_cast<T*>(a.out) + m * a.ldo + n, c, cnt);
+    if (PART && n + cnt == a.N) zero_pad(a, static_cast<T*>(a.out) + m * a.ldo + a.N);
   } else {
     static_assert(EPI == MM_GATE_BWD);
     float g[8], w[8];
@@ -299,6 +313,7 @@ __device__ __forceinline__ void finish8(const MmArgs& a, int64_t m, int n, float
     T* o = static_cast<T*>(a.out) + m * a.ldo + n;
     store_some<PART>(o, g, cnt);
     store_some<PART>(o + a.N, w, cnt);
+    if (PART && n + cnt == a.N) zero_pad(a, static_cast<T*>(a.out) + m * a.ldo + 2 * (int64_t)a.N);
   }
 }
 
@@ -1172,6 +1187,52 @@ __global__ __launch_bounds__(NW * 64) void thin_kernel(MmArgs a) {
   finish_row<EPI, T, true>(a, m, n, cs, us, min(4, a.N - n));
 }
 
+// ------------------------------------------------------------ aligned copies --
+// Matrices whose rows cannot start at 16 bytes or end inside a vector, copied
+// to rows of whole 128-byte lines with zeros behind their ends.  G = 1 << g
+// lanes a row, four vectors of each lane in flight.  Bandwidth bounds it.
+struct CopyArgs {
+  const char* src[3];
+  char* dst[3];
+  int64_t lds[3], ldd[3], width[3];  // bytes between rows, and of a row
+  int64_t rows[3];
+  uint32_t blocks[3];
+  int32_t g[3];
+};
+__global__ __launch_bounds__(256) void copy_rows_kernel(CopyArgs c) {
+  uint32_t block = blockIdx.x;
+  int i = 0;
+  while (i < 2 && block >= c.blocks[i]) block -= c.blocks[i++];
+  const char* const src = c.src[i];
+  char* const dst = c.dst[i];
+  const int64_t width = c.width[i], rows = c.rows[i], nv = c.ldd[i] / 16;
+  const int g = c.g[i], lane = threadIdx.x & ((1 << g) - 1);
+  const int64_t step = (int64_t)c.blocks[i] * (256 >> g);
+  for (int64_t r = (int64_t)block * (256 >> g) + (threadIdx.x >> g); r < rows; r += step) {
+    const char* const p = src + r * c.lds[i];
+    u32x4* const q = reinterpret_cast<u32x4*>(dst + r * c.ldd[i]);
+    for (int64_t v0 = lane; v0 < nv; v0 += 4 << g) {
+      u32x4 x[4];
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const int64_t at = (v0 + ((int64_t)b << g)) * 16;
+        x[b] = u32x4{0, 0, 0, 0};
+        if (at + 16 <= width) {
+          x[b] = load16(p + at);
+        } else if (at < width) {
+          char e[16];
+#pragma unroll
+          for (int j = 0; j < 16; ++j) e[j] = at + j < width ? p[at + j] : 0;
+          __builtin_memcpy(&x[b], e, 16);
+        }
+      }
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+        if (v0 + ((int64_t)b << g) < nv) q[v0 + ((int64_t)b << g)] = x[b];
+    }
+  }
+}
+
 // ------------------------------------------------------------------- host --
 enum Tiles { TILES_THIN, TILES_MINI, TILES_SMALL, TILES_HUGE };
 // How a product is laid out over workgroups.
@@ -1209,12 +1270,15 @@ Plan plan_with(MmType type, const MmArgs& a, Tiles t, int64_t splits) {
 // grows with the tiles a CU holds, and the join's traffic.  Mini tiles step in
 // 0.2 us a tile, small ones in 0.6, huge ones in 1.05 on a few CUs and 1.6 where
 // all of them run (the clock falls under their power); operands through
-// registers take 0.37 and 0.8, fp32 0.7 and 2.45.
-double step_us(MmType type, Tiles t, bool dma, double wgs) {
+// registers take 0.42 and 0.9, half as much again for each that is
+// rows-contiguous, fp32 0.7 and 2.45.
+double step_us(MmType type, const MmArgs& a, Tiles t, bool dma, double wgs) {
   const double held = std::ceil(wgs / 256);
   if (t == TILES_HUGE) return wgs < 256 ? 1.05 + 0.55 * wgs / 256 : 1.6 * held;
   if (type == MM_FP32) return t == TILES_MINI ? std::max(0.85, 0.7 * held) : 2.45 * held;
-  if (!dma) return t == TILES_MINI ? std::max(0.5, 0.37 * held) : std::max(0.95, 0.8 * held);
+  if (!dma)
+    return (1 + 0.5 * (a.a_rmaj + a.b_rmaj)) *
+           (t == TILES_MINI ? std::max(0.55, 0.42 * held) : std::max(1.05, 0.9 * held));
   return (t == TILES_MINI ? 0.2 : 0.6) * held;
 }
 double start_us(Tiles t) { return t == TILES_HUGE ? 7 : 3.3; }
@@ -1239,7 +1303,7 @@ Plan search(MmType type, const MmArgs& a, bool dma) {
       Plan p = plan_with(type, a, t, s);
       if (p.splits == last || (p.splits > 1 && p.steps < 2)) continue;
       last = p.splits;
-      p.us = start_us(t) + p.steps * step_us(type, t, dma, (double)p.tm * p.tn * p.splits) + join_us(a, p);
+      p.us = start_us(t) + p.steps * step_us(type, a, t, dma, (double)p.tm * p.tn * p.splits) + join_us(a, p);
       if (p.us < best.us) best = p;
     }
   }
@@ -1268,8 +1332,17 @@ size_t partial_bytes(const MmArgs& a, const Plan& p) {
   return (size_t)p.splits * (size_t)a.M * (size_t)partial_half(a.N) * (is_gate(a.epi) ? 8 : 4);
 }
 
-bool rows16(const void* p, int64_t ld, int es, int64_t extent) {
-  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * es % 16 == 0 && extent * es % 16 == 0;
+bool rows16(const void* p, int64_t ld, int es) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * es % 16 == 0;
+}
+
+// Whether an operand's rows in memory end inside a 16-byte vector, with what is
+// not a zero behind them.
+bool odd_a(MmType type, const MmArgs& a) {
+  return !a.a_zero && (int64_t)(a.a_rmaj ? a.M : a.K) * elem_bytes(type) % 16 != 0;
+}
+bool odd_b(MmType type, const MmArgs& a) {
+  return !a.b_zero && (int64_t)(a.b_rmaj ? a.N : a.K) * elem_bytes(type) % 16 != 0;
 }
 
 // Whether both operands can go straight to LDS: rows at 16 bytes, whole 16-byte
@@ -1277,7 +1350,7 @@ bool rows16(const void* p, int64_t ld, int es, int64_t extent) {
 bool can_dma(MmType type, const MmArgs& a) {
   if (type == MM_FP32) return false;
   const int es = elem_bytes(type);
-  if (!rows16(a.A, a.lda, es, a.a_rmaj ? a.M : a.K) || !rows16(a.B, a.ldb, es, a.b_rmaj ? a.N : a.K)) return false;
+  if (odd_a(type, a) || odd_b(type, a) || !rows16(a.A, a.lda, es) || !rows16(a.B, a.ldb, es)) return false;
   const int64_t lim = (int64_t)1 << 31;
   const int64_t brows = is_gate(a.epi) ? (int64_t)a.N + 256 : 256;
   return a.lda * es * 256 < lim && a.ldb * es * brows < lim && (int64_t)a.K * es < lim / 2;
@@ -1366,7 +1439,8 @@ PairPlan search_pair(MmType type, const MmArgs& a, const MmArgs& b, bool dma) {
       const double mean = (wa * p.a.steps + wb * p.b.steps) / (wa + wb);
       const double longest = std::max(p.a.steps, p.b.steps);
       p.us = start_us(t) + join_us(a, p.a) + join_us(b, p.b) +
-             std::max(mean * step_us(type, t, dma, wa + wb), longest * step_us(type, t, dma, std::min(wa + wb, 256.0)));
+             std::max(mean * step_us(type, b, t, dma, wa + wb),
+                      longest * step_us(type, b, t, dma, std::min(wa + wb, 256.0)));
       if (p.us < best.us) best = p;
     }
   }
@@ -1442,23 +1516,94 @@ hipError_t launch_float(MmType type, const MmArgs& a, hipStream_t s) {
   }
 }
 
-}  // namespace
-
-// (whatever the operands' alignment turns out to be)
-size_t mm_workspace(MmType type, const MmArgs& a) {
-  return std::max(partial_bytes(a, choose(type, a, true)), partial_bytes(a, choose(type, a, false)));
+// Operands whose rows end inside a 16-byte vector (by their extents: what a
+// workspace is asked for cannot depend on pointers) are first copied to aligned
+// rows where that and the product straight to LDS take less time than the
+// product through registers, by the model (10,000 tokens of 1023,
+// hidden 4095: forward 430 -> 262 us, backward 1856 -> 653; 3000 rows, 1023
+// columns, depth 4095 in 8 bits 49 -> 40).
+struct Copy {
+  const void* src;
+  int64_t ld, rows, extent;  // elements
+};
+int64_t copy_ld(MmType type, int64_t extent) {  // bytes
+  return (extent * elem_bytes(type) + 127) / 128 * 128;
+}
+size_t copy_bytes(MmType type, const Copy& c) { return (size_t)c.rows * (size_t)copy_ld(type, c.extent); }
+Copy copy_of_a(const MmArgs& a) { return {a.A, a.lda, a.a_rmaj ? a.K : a.M, a.a_rmaj ? a.M : a.K}; }
+Copy copy_of_b(const MmArgs& a) {
+  return {a.B, a.ldb, a.b_rmaj ? a.K : is_gate(a.epi) ? 2 * (int64_t)a.N : a.N, a.b_rmaj ? a.N : a.K};
 }
 
-size_t mm_pair_workspace(MmType type, const MmArgs& a, const MmArgs& b) {
-  size_t n = std::max(mm_workspace(type, a), mm_workspace(type, b));
-  for (bool dma : {false, true}) {
-    PairPlan p;
-    if (pair_up(type, a, b, dma, p)) n = std::max(n, pair_bytes(a, b, p));
+double time_of(MmType type, const MmArgs& a, const MmArgs* b, bool dma_a, bool dma_b) {
+  const double apart = choose(type, a, dma_a).us + (b ? choose(type, *b, dma_b).us : 0);
+  PairPlan p;
+  return b && pair_up(type, a, *b, dma_a && dma_b, p) ? p.us : apart;
+}
+
+// The operands of a product (or of a pair, whose A is one matrix) that are
+// copied, A first; their number.  It depends on the sizes alone.
+int copies(MmType type, const MmArgs& a, const MmArgs* b, Copy (&c)[3]) {
+  if (type == MM_FP32 || a.M < 1 || (b && b->K < 1)) return 0;
+  const bool aa = odd_a(type, a) || (b && odd_a(type, *b)), ab = odd_b(type, a), bb = b && odd_b(type, *b);
+  if (!aa && !ab && !bb) return 0;
+  int n = 0;
+  if (aa) c[n++] = copy_of_a(a);
+  if (ab) c[n++] = copy_of_b(a);
+  if (bb) c[n++] = copy_of_b(*b);
+  double us = 5;
+  for (int i = 0; i < n; ++i) us += 2.0 * (double)copy_bytes(type, c[i]) / 4e6;
+  const double straight = time_of(type, a, b, true, true);
+  return us + straight < time_of(type, a, b, !aa && !ab, !aa && !bb) ? n : 0;
+}
+
+size_t copies_bytes(MmType type, const Copy* c, int n) {
+  size_t bytes = 0;
+  for (int i = 0; i < n; ++i) bytes += copy_bytes(type, c[i]);
+  return bytes;
+}
+
+// Copies the operands that are to be, where the others can go straight to LDS
+// as they lie, and points the products to the copies.
+hipError_t copy_operands(MmType type, MmArgs& a, MmArgs* b, hipStream_t s) {
+  Copy c[3];
+  const int n = copies(type, a, b, c);
+  if (n == 0) return hipSuccess;
+  const size_t bytes = copies_bytes(type, c, n);
+  if (a.work_bytes < bytes) return hipErrorInvalidValue;
+  const int es = elem_bytes(type);
+  MmArgs x = a, y = b ? *b : a;
+  CopyArgs k{};
+  uint32_t blocks = 0;
+  char* dst = reinterpret_cast<char*>(a.work);
+  int at = 0;
+  auto take = [&](const void*& P, int64_t& ld, int32_t& zero) {
+    const int64_t ldd = copy_ld(type, c[at].extent);
+    int g = 0;
+    while (g < 6 && (16 << g) < ldd) ++g;
+    k.src[at] = static_cast<const char*>(c[at].src), k.dst[at] = dst, k.lds[at] = c[at].ld * es, k.ldd[at] = ldd;
+    k.width[at] = c[at].extent * es, k.rows[at] = c[at].rows, k.g[at] = g;
+    k.blocks[at] = (uint32_t)std::min(cdiv(c[at].rows, 256 >> g), (int64_t)4096);
+    blocks += k.blocks[at];
+    P = dst, ld = ldd / es, zero = 1;
+    dst += copy_bytes(type, c[at++]);
+  };
+  const bool aa = odd_a(type, a) || (b && odd_a(type, *b));
+  if (aa) {
+    take(x.A, x.lda, x.a_zero);
+    if (b) y.A = x.A, y.lda = x.lda, y.a_zero = 1;
   }
-  return n;
+  if (odd_b(type, a)) take(x.B, x.ldb, x.b_zero);
+  if (b && odd_b(type, *b)) take(y.B, y.ldb, y.b_zero);
+  if (!can_dma(type, x) || (b && !can_dma(type, y))) return hipSuccess;
+  for (MmArgs* m : {&x, &y}) m->work = reinterpret_cast<float*>(dst), m->work_bytes = a.work_bytes - bytes;
+  hipLaunchKernelGGL(copy_rows_kernel, dim3(blocks), dim3(256), 0, s, k);
+  a = x;
+  if (b) *b = y;
+  return hipGetLastError();
 }
 
-hipError_t launch_mm(MmType type, const MmArgs& a, hipStream_t s) {
+hipError_t launch_one(MmType type, const MmArgs& a, hipStream_t s) {
   switch (type) {
     case MM_BF16: return launch_float<__bf16>(type, a, s);
     case MM_FP32: return launch_float<float>(type, a, s);
@@ -1468,8 +1613,39 @@ hipError_t launch_mm(MmType type, const MmArgs& a, hipStream_t s) {
   }
 }
 
-hipError_t launch_mm_pair(MmType type, const MmArgs& a, const MmArgs& b, hipStream_t s) {
+}  // namespace
+
+// (whatever the operands' alignment turns out to be)
+size_t mm_workspace(MmType type, const MmArgs& a) {
+  Copy c[3];
+  const size_t copied = copies_bytes(type, c, copies(type, a, nullptr, c));
+  return std::max(copied + partial_bytes(a, choose(type, a, true)), partial_bytes(a, choose(type, a, false)));
+}
+
+size_t mm_pair_workspace(MmType type, const MmArgs& a, const MmArgs& b) {
+  Copy c[3];
+  const size_t copied = copies_bytes(type, c, copies(type, a, &b, c));
+  size_t n = 0;
+  for (bool dma : {false, true}) {
+    size_t part = std::max(partial_bytes(a, choose(type, a, dma)), partial_bytes(b, choose(type, b, dma)));
+    PairPlan p;
+    if (pair_up(type, a, b, dma, p)) part = std::max(part, pair_bytes(a, b, p));
+    n = std::max(n, part + (dma ? copied : 0));
+  }
+  return n;
+}
+
+hipError_t launch_mm(MmType type, const MmArgs& product, hipStream_t s) {
+  MmArgs a = product;
+  const hipError_t e = copy_operands(type, a, nullptr, s);
+  return e == hipSuccess ? launch_one(type, a, s) : e;
+}
+
+hipError_t launch_mm_pair(MmType type, const MmArgs& first, const MmArgs& second, hipStream_t s) {
+  MmArgs a = first, b = second;
   if (!a.out && !b.out) return hipSuccess;
+  const hipError_t copied = copy_operands(type, a, &b, s);
+  if (copied != hipSuccess) return copied;
   const bool dma = can_dma(type, a) && can_dma(type, b);
   PairPlan p;
   if (pair_up(type, a, b, dma, p)) {
@@ -1479,8 +1655,8 @@ hipError_t launch_mm_pair(MmType type, const MmArgs& a, const MmArgs& b, hipStre
     return a.epi == MM_PLAIN ? launch_pair<float, MM_PLAIN>(type, a, b, p, dma, s)
                              : launch_pair<float, MM_GATE_BWD>(type, a, b, p, dma, s);
   }
-  const hipError_t e = a.out && a.M > 0 ? launch_mm(type, a, s) : hipSuccess;
-  return e == hipSuccess && b.out ? launch_mm(type, b, s) : e;
+  const hipError_t e = a.out && a.M > 0 ? launch_one(type, a, s) : hipSuccess;
+  return e == hipSuccess && b.out ? launch_one(type, b, s) : e;
 }
 
 }  // namespace tabpack

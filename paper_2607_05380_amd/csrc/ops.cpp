@@ -67,29 +67,39 @@ bool known_act(int32_t act) { return act >= PACK_ACT_SILU && act <= PACK_ACT_REL
 MmType type_of(int32_t precision) { return precision == PACK_PREC_BF16 ? MM_BF16 : MM_FP32; }
 
 // The products of a gated block (x [T, D], hidden width F, y [T, O]).
-MmArgs mm_gate(int64_t T, int32_t D, int32_t F) {
+// (h and [dg | du] in rows of ff_ld() elements, zeros behind their ends)
+int64_t ff_ld(MmType t, int64_t cols) { return t == MM_BF16 ? PACK_FF_LD(PACK_PREC_BF16, cols) : cols; }
+MmArgs mm_gate(MmType t, int64_t T, int32_t D, int32_t F) {
   MmArgs a{};
-  a.M = (int32_t)T, a.N = F, a.K = D, a.epi = MM_GATE;
+  a.M = (int32_t)T, a.N = F, a.K = D, a.epi = MM_GATE, a.ldo = ff_ld(t, F), a.pad = (int32_t)(a.ldo - F);
   return a;
 }
-MmArgs mm_down(int64_t T, int32_t F, int32_t O) {
+MmArgs mm_down(MmType t, int64_t T, int32_t F, int32_t O) {
   MmArgs a{};
-  a.M = (int32_t)T, a.N = O, a.K = F, a.epi = MM_PLAIN;
+  a.M = (int32_t)T, a.N = O, a.K = F, a.epi = MM_PLAIN, a.lda = ff_ld(t, F), a.a_zero = 1;
   return a;
 }
-MmArgs mm_dh(int64_t T, int32_t F, int32_t O) {
+MmArgs mm_dh(MmType t, int64_t T, int32_t F, int32_t O) {
   MmArgs a{};
   a.M = (int32_t)T, a.N = F, a.K = O, a.b_rmaj = 1, a.epi = MM_GATE_BWD;
+  a.ldo = ff_ld(t, 2 * (int64_t)F), a.pad = (int32_t)(a.ldo - 2 * (int64_t)F);
   return a;
 }
-MmArgs mm_dx(int64_t T, int32_t D, int32_t F) {
+MmArgs mm_dx(MmType t, int64_t T, int32_t D, int32_t F) {
   MmArgs a{};
   a.M = (int32_t)T, a.N = D, a.K = 2 * F, a.b_rmaj = 1, a.epi = MM_PLAIN;
+  a.lda = ff_ld(t, 2 * (int64_t)F), a.a_zero = 1;
   return a;
 }
-MmArgs mm_dw(int64_t T, int32_t rows, int32_t cols) {
+MmArgs mm_dwd(MmType t, int64_t T, int32_t F, int32_t O) {
   MmArgs a{};
-  a.M = rows, a.N = cols, a.K = (int32_t)T, a.a_rmaj = a.b_rmaj = 1, a.epi = MM_PLAIN;
+  a.M = O, a.N = F, a.K = (int32_t)T, a.a_rmaj = a.b_rmaj = 1, a.epi = MM_PLAIN, a.ldb = ff_ld(t, F), a.b_zero = 1;
+  return a;
+}
+MmArgs mm_dwg(MmType t, int64_t T, int32_t D, int32_t F) {
+  MmArgs a{};
+  a.M = 2 * F, a.N = D, a.K = (int32_t)T, a.a_rmaj = a.b_rmaj = 1, a.epi = MM_PLAIN;
+  a.lda = ff_ld(t, 2 * (int64_t)F), a.a_zero = 1;
   return a;
 }
 MmArgs mm_q8(int64_t rows, int32_t outputs, int32_t depth, int32_t gate) {
@@ -134,10 +144,11 @@ int pack_gated_ff_workspace_size(int32_t precision, int64_t tokens, int32_t d_in
   if (rc != PACK_OK) return rc;
   const MmType t = type_of(precision);
   if (!backward)
-    *bytes = std::max(mm_workspace(t, mm_gate(tokens, d_in, hidden)), mm_workspace(t, mm_down(tokens, hidden, d_out)));
+    *bytes = std::max(mm_workspace(t, mm_gate(t, tokens, d_in, hidden)),
+                      mm_workspace(t, mm_down(t, tokens, hidden, d_out)));
   else
-    *bytes = std::max(mm_pair_workspace(t, mm_dh(tokens, hidden, d_out), mm_dw(tokens, d_out, hidden)),
-                      mm_pair_workspace(t, mm_dx(tokens, d_in, hidden), mm_dw(tokens, 2 * hidden, d_in)));
+    *bytes = std::max(mm_pair_workspace(t, mm_dh(t, tokens, hidden, d_out), mm_dwd(t, tokens, hidden, d_out)),
+                      mm_pair_workspace(t, mm_dx(t, tokens, d_in, hidden), mm_dwg(t, tokens, d_in, hidden)));
   return PACK_OK;
 }
 
@@ -158,14 +169,14 @@ int pack_gated_ff_forward(const void* x, int64_t ldx, const void* w_gate_up, int
   if (rc == PACK_OK) rc = check_work(work, work_bytes, need);
   if (rc != PACK_OK) return rc;
   const MmType t = type_of(precision);
-  MmArgs a = mm_gate(tokens, d_in, hidden);
+  MmArgs a = mm_gate(t, tokens, d_in, hidden);
   a.A = x, a.lda = ldx, a.B = w_gate_up, a.ldb = ldwg, a.act = act;
-  a.pre = gate_up_out, a.ldpre = 2 * (int64_t)hidden, a.out = hidden_out, a.ldo = hidden;
+  a.pre = gate_up_out, a.ldpre = 2 * (int64_t)hidden, a.out = hidden_out;
   a.work = static_cast<float*>(work), a.work_bytes = work_bytes;
   rc = done("gate and up projections", launch_mm(t, a, stream));
   if (rc != PACK_OK) return rc;
-  MmArgs d = mm_down(tokens, hidden, d_out);
-  d.A = hidden_out, d.lda = hidden, d.B = w_down, d.ldb = ldwd, d.add = residual, d.ldadd = ldr;
+  MmArgs d = mm_down(t, tokens, hidden, d_out);
+  d.A = hidden_out, d.B = w_down, d.ldb = ldwd, d.add = residual, d.ldadd = ldr;
   d.out = out, d.ldo = ldo, d.work = a.work, d.work_bytes = work_bytes;
   return done("down projection", launch_mm(t, d, stream));
 }
@@ -187,15 +198,14 @@ int pack_gated_ff_backward(const void* dy, int64_t lddy, const void* x, int64_t 
   if (rc == PACK_OK) rc = check_work(work, work_bytes, need);
   if (rc != PACK_OK) return rc;
   const MmType t = type_of(precision);
-  const int64_t ldg = 2 * (int64_t)hidden;
   // [dg | du] beside dw_down, then dx beside dw_gate_up
-  MmArgs dh = mm_dh(tokens, hidden, d_out), dwd = mm_dw(tokens, d_out, hidden);
-  MmArgs dx = mm_dx(tokens, d_in, hidden), dwg = mm_dw(tokens, 2 * hidden, d_in);
+  MmArgs dh = mm_dh(t, tokens, hidden, d_out), dwd = mm_dwd(t, tokens, hidden, d_out);
+  MmArgs dx = mm_dx(t, tokens, d_in, hidden), dwg = mm_dwg(t, tokens, d_in, hidden);
   dh.A = dy, dh.lda = lddy, dh.B = w_down, dh.ldb = ldwd, dh.act = act;
-  dh.pre = const_cast<void*>(gate_up), dh.ldpre = ldg, dh.out = dgate_up, dh.ldo = ldg;
-  dwd.A = dy, dwd.lda = lddy, dwd.B = hidden_in, dwd.ldb = hidden, dwd.out = dw_down_out, dwd.ldo = hidden;
-  dx.A = dgate_up, dx.lda = ldg, dx.B = w_gate_up, dx.ldb = ldwg, dx.out = dx_out, dx.ldo = lddx;
-  dwg.A = dgate_up, dwg.lda = ldg, dwg.B = x, dwg.ldb = ldx, dwg.out = dw_gate_up_out, dwg.ldo = d_in;
+  dh.pre = const_cast<void*>(gate_up), dh.ldpre = 2 * (int64_t)hidden, dh.out = dgate_up;
+  dwd.A = dy, dwd.lda = lddy, dwd.B = hidden_in, dwd.out = dw_down_out, dwd.ldo = hidden;
+  dx.A = dgate_up, dx.B = w_gate_up, dx.ldb = ldwg, dx.out = dx_out, dx.ldo = lddx;
+  dwg.A = dgate_up, dwg.B = x, dwg.ldb = ldx, dwg.out = dw_gate_up_out, dwg.ldo = d_in;
   for (MmArgs* a : {&dh, &dwd, &dx, &dwg}) a->work = static_cast<float*>(work), a->work_bytes = work_bytes;
   if (!dx_out && !dw_gate_up_out) dh.out = nullptr;
   hipError_t e = launch_mm_pair(t, dh, dwd, stream);

@@ -74,6 +74,9 @@ struct MmArgs {
   int64_t lda, ldb;
   int32_t M, N, K;        // N: output columns (gated: of each half)
   int32_t a_rmaj, b_rmaj; // 1: rows-contiguous
+  // 1: zeros follow each of the operand's rows in memory up to a multiple of 16 bytes
+  int32_t a_zero, b_zero;
+  int32_t pad;            // MM_GATE, MM_GATE_BWD: columns behind each row of out that are set to zero (bf16, fp32)
   int32_t epi, act;
   const void* add;        // MM_PLAIN: or NULL
   void* pre;              // [M, 2N] gate and up values (MM_GATE: or NULL)
@@ -83,7 +86,7 @@ struct MmArgs {
   const float* col_scale; // [N] or [2N]
   const float* bias;      // [N] or [2N], or NULL
   int32_t out_f32;        // MM_Q8*: type of out (elsewhere the operands')
-  float* work;            // partial sums of a split depth
+  float* work;            // aligned copies of operands, partial sums of a split depth
   size_t work_bytes;
   // filled in by launch_mm
   int32_t tiles_m, tiles_n, splits, steps_per_split;
@@ -93,7 +96,8 @@ size_t mm_workspace(MmType type, const MmArgs& a);
 hipError_t launch_mm(MmType type, const MmArgs& a, hipStream_t s);
 // Two independent products of one type, a with depth-contiguous A and
 // rows-contiguous B (MM_PLAIN or MM_GATE_BWD), b with rows-contiguous operands
-// (MM_PLAIN), the same work given to both: in one launch where that is faster.
+// (MM_PLAIN), of the same matrix A and the same work: in one launch where that is
+// faster.
 // One whose out is NULL is left out; the other's result does not depend on it.
 size_t mm_pair_workspace(MmType type, const MmArgs& a, const MmArgs& b);
 hipError_t launch_mm_pair(MmType type, const MmArgs& a, const MmArgs& b, hipStream_t s);

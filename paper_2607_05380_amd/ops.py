@@ -192,6 +192,11 @@ def _ff_inputs(x, w_gate_up, w_down):
     return prec, (tokens, d_in, hidden, d_out), (xp, ldx, wgp, ldwg, wdp, ldwd)
 
 
+def _ff_ld(x, cols):
+    """Elements from row to row of the hidden values and of the gradients of gate and up (see tabpack.h)."""
+    return (cols + 7) // 8 * 8 if x.dtype is torch.bfloat16 else cols
+
+
 def gated_ff(x, w_gate_up, w_down, act="silu", residual=None, save=False):
     """y = h w_down^T (+ residual) with [g | u] = x w_gate_up^T and h = act(g) u: x [tokens, d_in], w_gate_up
     [2 hidden, d_in] (gate rows, then up rows), w_down [d_out, hidden], all in one type; act "silu", "gelu" or
@@ -201,12 +206,12 @@ def gated_ff(x, w_gate_up, w_down, act="silu", residual=None, save=False):
     rp, ldr = (None, 0) if residual is None else _matrix(residual, "residual", x.dtype, (tokens, d_out))
     code = _act(act)
     gu = _empty(x, tokens, 2 * hidden) if save else None
-    h, y = _empty(x, tokens, hidden), _empty(x, tokens, d_out)
+    h, y = _empty(x, tokens, _ff_ld(x, hidden)), _empty(x, tokens, d_out)
     work = _work(x, "pack_gated_ff_workspace_size", prec, *dims, 0)
     _call("pack_gated_ff_forward", x, (w_gate_up, w_down, residual), *ptrs, rp, ldr, prec, code, *dims,
           gu.data_ptr() if save else None, h.data_ptr(), y.data_ptr(), d_out,
           None if work is None else work.data_ptr(), 0 if work is None else work.numel())
-    return (y, (gu, h)) if save else y
+    return (y, (gu, h[:, :hidden])) if save else y
 
 
 def gated_ff_backward(dy, x, w_gate_up, w_down, saved, act="silu", need_dx=True):
@@ -218,10 +223,15 @@ def gated_ff_backward(dy, x, w_gate_up, w_down, saved, act="silu", need_dx=True)
     gu, h = saved
     for t, name, cols in ((gu, "saved gate and up values", 2 * hidden), (h, "saved hidden values", hidden)):
         _matrix(t, name, x.dtype, (tokens, cols))
-        if not t.is_contiguous():
-            _fail(f"{name} must be contiguous")
+    if not gu.is_contiguous():
+        _fail("saved gate and up values must be contiguous")
     code = _act(act)
-    dgu = _empty(x, tokens, 2 * hidden)
+    ldh = _ff_ld(x, hidden)
+    if h.stride(0) != ldh or h.untyped_storage().nbytes() < (h.storage_offset() + tokens * ldh) * h.element_size():
+        own = _empty(x, tokens, ldh)  # (a copy of what gated_ff saved, in rows of another length)
+        own[:, :hidden] = h
+        h = own
+    dgu = _empty(x, tokens, _ff_ld(x, 2 * hidden))
     dx = _empty(x, tokens, d_in) if need_dx else None
     dwg, dwd = _empty(x, 2 * hidden, d_in), _empty(x, d_out, hidden)
     work = _work(x, "pack_gated_ff_workspace_size", prec, *dims, 1)

@@ -37,7 +37,7 @@ def _sum_err(n):
 
 @pytest.mark.parametrize("T,D,F,O,act,dtype", [
     (4100, 520, 2056, 1032, "silu", torch.bfloat16),     # 256 x 256 tiles with edges in both directions
-    (4100, 515, 2051, 1029, "gelu", torch.bfloat16),     # the same through registers
+    (4100, 515, 2051, 1029, "gelu", torch.bfloat16),     # the same from aligned copies
     (9000, 128, 1024, 128, "silu", torch.bfloat16),      # long token axis: split weight gradients
     (1500, 264, 520, 136, "gelu", torch.float32),
     (100, 2048, 4096, 2048, "silu", torch.bfloat16)], ids=str)
