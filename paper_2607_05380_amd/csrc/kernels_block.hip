@@ -19,11 +19,13 @@
 // A K step is 128 bytes of depth (64 bf16, 128 int8, 32 fp32).  Tiles (times:
 // bf16 products of M x N x K):
 //   small  128 x 128, 4 waves of 64 x 64, two steps in LDS (64 KB), two
-//          workgroups per CU.  Operands go straight to LDS; fp32, and operands
-//          whose rows do not start at 16 bytes or end inside a 16-byte vector
-//          where copying them first takes longer (see copies()), pass through
-//          registers, two steps ahead.  2048 x 4096 x 1024 22 us
-//          (0.8 PFLOP/s; huge 30, mini 31), through registers 31.
+//          workgroups per CU.  Operands go straight to LDS; those whose rows do
+//          not start at 16 bytes or end inside a 16-byte vector (in fp32; in the
+//          others where copying them first takes longer, see copies()) pass
+//          through registers, two steps ahead.  2048 x 4096 x 1024 22 us
+//          (0.8 PFLOP/s; huge 30, mini 31), through registers 31.  fp32: 4096 x
+//          1024 gated x 512 70 us (123 TFLOP/s; a library product of 8192 a
+//          side 153), through registers 78.
 //   huge   256 x 256, 8 waves of 128 x 64, 160 KB of LDS, one workgroup per CU
 //          (see huge_tile).  16,384 x 1024 x 4096 107 us (1.29 PFLOP/s; small
 //          128), where a large library product reaches 1.42.
@@ -468,7 +470,7 @@ __global__ __launch_bounds__(256) void join_kernel(MmArgs a) {
 
 // ------------------------------------------------------------------ loaders --
 // Straight to LDS (base and rows at 16 bytes, the contiguous extent a multiple
-// of 16 bytes): a region of R rows is R / 8 blocks of 1 KB, one load instruction
+// of 16 bytes or zeros behind it up to one): a region of R rows is R / 8 blocks of 1 KB, one load instruction
 // each; wave w of NW issues blocks w PER .. w PER + PER - 1.  grow(r): the operand's row
 // (rows-contiguous: element) that region row r holds, relative to P, or -1.
 // Lanes outside the operand have an offset past the descriptor's range and
@@ -498,9 +500,11 @@ struct Dma {
         kofs[p] = c * (16 / ES);
         voff[p] = g < 0 ? kOob : (uint32_t)(g * ldb + c * 16);
       } else {
-        constexpr int LPK = R / 8;  // lanes a depth row
+        constexpr int LPK = R * ES / 16;  // lanes a depth row
         const int k = b * (64 / LPK) + lane / LPK;
-        const int col = ((((lane % LPK) >> 1) ^ rmaj_x<R>(k)) << 4) + (lane & 1) * 8;
+        // (fp32 is read by consecutive lanes in consecutive banks: no swizzle)
+        const int col = ES == 4 ? (lane % LPK) * 4
+                                : ((((lane % LPK) >> 1) ^ rmaj_x<R>(k)) << 4) + (lane & 1) * 8;
         const int64_t g = grow(col);
         kofs[p] = k;
         voff[p] = g < 0 ? kOob : (uint32_t)(k * ldb + g * ES);
@@ -605,12 +609,21 @@ __device__ __forceinline__ void mma(bf16x8 b, bf16x8 a, f32x16& acc, float) {
 
 // The 16 bytes that lane needs of rows row .. row + 31 of a region for MFMA
 // step ks of 4, in inline assembly (see gemm_tiles.h): the caller waits.
-template <bool RM, int R>
+template <typename T, bool RM, int R>
 __device__ __forceinline__ bf16x8 frag_asm(const char* lds, int row, int ks, int lane) {
-  if constexpr (RM)
-    return frag_tr_asm<R>(lds, row, ks, lane);
-  else
+  if constexpr (!RM) {
     return frag_kmaj_asm<4>(lds, row, ks, lane);
+  } else if constexpr (sizeof(T) == 2) {
+    return frag_tr_asm<R>(lds, row, ks, lane);
+  } else {  // fp32 [32 depth rows][R]: depth 8 ks + 4 (lane / 32) .. + 3 of one row, two to an instruction
+    typedef __attribute__((address_space(3))) const char* lds_cptr;
+    const uint32_t at = (uint32_t)(uintptr_t)(lds_cptr)(lds + (8 * ks + 4 * (lane >> 5)) * (4 * R) +
+                                                       (row + (lane & 31)) * 4);
+    u32x2 x, y;
+    asm volatile("ds_read2st64_b32 %0, %1 offset0:0 offset1:%2" : "=v"(x) : "v"(at), "n"(R / 64));
+    asm volatile("ds_read2st64_b32 %0, %1 offset0:%2 offset1:%3" : "=v"(y) : "v"(at), "n"(R / 32), "n"(R / 64 * 3));
+    return __builtin_bit_cast(bf16x8, u32x4{x[0], x[1], y[0], y[1]});
+  }
 }
 // The same as ordinary reads, for regions that were written through registers.
 template <typename T, bool RM, int R>
@@ -735,9 +748,9 @@ __device__ __forceinline__ void small_tile(const MmArgs& a, uint32_t block, char
       bf16x8 fa[4][NB], fb[4][NB];
       auto rd = [&](int ks) {
 #pragma unroll
-        for (int i = 0; i < NB; ++i) fa[ks][i] = frag_asm<RA, R>(cur, wm * W + i * 32, ks, lane);
+        for (int i = 0; i < NB; ++i) fa[ks][i] = frag_asm<T, RA, R>(cur, wm * W + i * 32, ks, lane);
 #pragma unroll
-        for (int j = 0; j < NB; ++j) fb[ks][j] = frag_asm<RB, R>(cur + REGION, wn * W + j * 32, ks, lane);
+        for (int j = 0; j < NB; ++j) fb[ks][j] = frag_asm<T, RB, R>(cur + REGION, wn * W + j * 32, ks, lane);
       };
       rd(0);
       rd(1);
@@ -1271,11 +1284,13 @@ Plan plan_with(MmType type, const MmArgs& a, Tiles t, int64_t splits) {
 // 0.2 us a tile, small ones in 0.6, huge ones in 1.05 on a few CUs and 1.6 where
 // all of them run (the clock falls under their power); operands through
 // registers take 0.42 and 0.9, half as much again for each that is
-// rows-contiguous, fp32 0.7 and 2.45.
+// rows-contiguous; fp32 0.62 and 2.2, through registers 0.7 and 2.45.
 double step_us(MmType type, const MmArgs& a, Tiles t, bool dma, double wgs) {
   const double held = std::ceil(wgs / 256);
   if (t == TILES_HUGE) return wgs < 256 ? 1.05 + 0.55 * wgs / 256 : 1.6 * held;
-  if (type == MM_FP32) return t == TILES_MINI ? std::max(0.85, 0.7 * held) : 2.45 * held;
+  if (type == MM_FP32)
+    return t == TILES_MINI ? (dma ? std::max(0.75, 0.62 * held) : std::max(0.85, 0.7 * held))
+                           : (dma ? 2.2 : 2.45) * held;
   if (!dma)
     return (1 + 0.5 * (a.a_rmaj + a.b_rmaj)) *
            (t == TILES_MINI ? std::max(0.55, 0.42 * held) : std::max(1.05, 0.9 * held));
@@ -1297,7 +1312,7 @@ Plan search(MmType type, const MmArgs& a, bool dma) {
   best.us = 1e30;
   if (type != MM_FP32 && !a.a_rmaj && !a.b_rmaj && a.M <= 16) return plan_with(type, a, TILES_THIN, 1);
   for (Tiles t : {TILES_MINI, TILES_SMALL, TILES_HUGE}) {
-    if (t == TILES_HUGE && !dma) continue;
+    if (t == TILES_HUGE && (!dma || type == MM_FP32)) continue;
     int64_t last = 0;
     for (int64_t s : kSplits) {
       Plan p = plan_with(type, a, t, s);
@@ -1348,7 +1363,6 @@ bool odd_b(MmType type, const MmArgs& a) {
 // Whether both operands can go straight to LDS: rows at 16 bytes, whole 16-byte
 // vectors, and tile-relative offsets below 2 GiB.
 bool can_dma(MmType type, const MmArgs& a) {
-  if (type == MM_FP32) return false;
   const int es = elem_bytes(type);
   if (odd_a(type, a) || odd_b(type, a) || !rows16(a.A, a.lda, es) || !rows16(a.B, a.ldb, es)) return false;
   const int64_t lim = (int64_t)1 << 31;
@@ -1397,19 +1411,16 @@ hipError_t launch_tiles(MmType type, MmArgs a, hipStream_t s) {
       return hipGetLastError();
     }
   }
-  if constexpr (sizeof(T) != 4) {
-    if (p.tiles == TILES_HUGE)
-      hipLaunchKernelGGL((huge_kernel<T, RA, RB, EPI>), grid, dim3(512), 0, s, a);
-    else if (dma && p.tiles == TILES_SMALL)
-      hipLaunchKernelGGL((small_kernel<T, RA, RB, EPI, true, 2, 2>), grid, dim3(256), 0, s, a);
-    else if (dma)
-      hipLaunchKernelGGL((small_kernel<T, RA, RB, EPI, true, 1, 4>), grid, dim3(256), 0, s, a);
-  }
-  if (!dma) {
-    if (p.tiles == TILES_SMALL)
-      hipLaunchKernelGGL((small_kernel<T, RA, RB, EPI, false, 2, 2>), grid, dim3(256), 0, s, a);
-    else
-      hipLaunchKernelGGL((small_kernel<T, RA, RB, EPI, false, 1, 2>), grid, dim3(256), 0, s, a);
+  if (p.tiles == TILES_HUGE) {
+    if constexpr (sizeof(T) != 4) hipLaunchKernelGGL((huge_kernel<T, RA, RB, EPI>), grid, dim3(512), 0, s, a);
+  } else if (dma && p.tiles == TILES_SMALL) {
+    hipLaunchKernelGGL((small_kernel<T, RA, RB, EPI, true, 2, 2>), grid, dim3(256), 0, s, a);
+  } else if (dma) {
+    hipLaunchKernelGGL((small_kernel<T, RA, RB, EPI, true, 1, 4>), grid, dim3(256), 0, s, a);
+  } else if (p.tiles == TILES_SMALL) {
+    hipLaunchKernelGGL((small_kernel<T, RA, RB, EPI, false, 2, 2>), grid, dim3(256), 0, s, a);
+  } else {
+    hipLaunchKernelGGL((small_kernel<T, RA, RB, EPI, false, 1, 2>), grid, dim3(256), 0, s, a);
   }
   launch_join<EPI, T>(a, s);
   return hipGetLastError();
@@ -1487,18 +1498,14 @@ hipError_t launch_pair(MmType type, MmArgs a, MmArgs b, const PairPlan& p, bool 
   m.a = a, m.b = b;
   const dim3 grid(((m.na + 7) / 8 + (m.nb + 7) / 8) * 8);
   const Tiles t = p.a.tiles;
-  if constexpr (sizeof(T) != 4) {
-    if (dma && t == TILES_SMALL)
-      hipLaunchKernelGGL((small_pair_kernel<T, EPI, true, 2, 2>), grid, dim3(256), 0, s, m);
-    else if (dma)
-      hipLaunchKernelGGL((small_pair_kernel<T, EPI, true, 1, 4>), grid, dim3(256), 0, s, m);
-  }
-  if (!dma) {
-    if (t == TILES_SMALL)
-      hipLaunchKernelGGL((small_pair_kernel<T, EPI, false, 2, 2>), grid, dim3(256), 0, s, m);
-    else
-      hipLaunchKernelGGL((small_pair_kernel<T, EPI, false, 1, 2>), grid, dim3(256), 0, s, m);
-  }
+  if (dma && t == TILES_SMALL)
+    hipLaunchKernelGGL((small_pair_kernel<T, EPI, true, 2, 2>), grid, dim3(256), 0, s, m);
+  else if (dma)
+    hipLaunchKernelGGL((small_pair_kernel<T, EPI, true, 1, 4>), grid, dim3(256), 0, s, m);
+  else if (t == TILES_SMALL)
+    hipLaunchKernelGGL((small_pair_kernel<T, EPI, false, 2, 2>), grid, dim3(256), 0, s, m);
+  else
+    hipLaunchKernelGGL((small_pair_kernel<T, EPI, false, 1, 2>), grid, dim3(256), 0, s, m);
   if (a.out) launch_join<EPI, T>(a, s);
   if (b.out) launch_join<MM_PLAIN, T>(b, s);
   return hipGetLastError();
