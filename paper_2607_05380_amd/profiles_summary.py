@@ -36,7 +36,7 @@ EPIS = ["fwd", "fwd_eval", "dx", "dw", "ns", "de"]
 SIMPLE = ["dropout_words", "grad_sums", "head_fwd", "head_bwd", "head_train", "gather", "rows_to_bf16", "to_shadow",
           "eval_score", "dropout_mask", "select_partial", "select_pick", "select_update", "select_init", "select_final",
           "ensemble_mean", "muon_prep", "muon_norm", "muon_convert", "muon_update", "embed_table", "embed_grad",
-          "idx_check", "stream_copy", "norm_bwd", "norm_dw", "rows", "distill"]
+          "idx_check", "stream_copy", "norm_bwd", "norm_dw", "copy_rows", "rows", "distill"]
 # kernels of the student's operators: matrix products by tiles, operand kinds and epilogue, row kernels by mode
 MM_EPIS = ["plain", "gate", "gate_bwd", "q8", "q8_gate"]
 ROW_MODES = ["norm", "norm_q8", "quantize"]

@@ -14,6 +14,7 @@ from paper_2607_05380_amd import profiles_summary as ps
     ("_ZN7tabpack12_GLOBAL__N_111rows_kernelIDF16bLi64ELi16ELi1EEEvNS_7RowArgsE", "rows_bf16_norm_q8"),
     ("_ZN7tabpack12_GLOBAL__N_115norm_bwd_kernelIDF16bLi64ELi16EEEvNS_11NormBwdArgsE", "norm_bwd"),
     ("_ZN7tabpack12_GLOBAL__N_114distill_kernelIDF16bLi512ELi64ELb0EEEvNS_11DistillArgsE", "distill"),
+    ("_ZN7tabpack12_GLOBAL__N_116copy_rows_kernelENS0_8CopyArgsE", "copy_rows"),
     ("_ZN7tabpack12_GLOBAL__N_119rows_to_bf16_kernelEPKfPDF16bllll", "rows_to_bf16")])
 def test_short_name_of_operators(kernel, name):
     assert ps.short_name(kernel) == name
