@@ -458,7 +458,7 @@ int pack_distill_topk(const void* logits, int64_t ldz, int32_t precision, int64_
  * All matrices are in the precision; h and the saved g and u are rounded to it
  * (h is formed from the unrounded ones): h feeds matrix instructions, and the
  * saved values in fp32 would double the largest traffic of a training step. */
-#define PACK_FF_LD(precision, cols) ((precision) == PACK_PREC_BF16 ? ((cols) + 7) / 8 * 8 : (cols))
+#define PACK_FF_LD(precision, cols) ((precision) == PACK_PREC_BF16 ? ((cols) + 7) / 8 * 8 : ((cols) + 3) / 4 * 4)
 int pack_gated_ff_workspace_size(int32_t precision, int64_t tokens, int32_t d_in, int32_t hidden, int32_t d_out,
                                  int32_t backward, size_t* bytes);
 int pack_gated_ff_forward(const void* x, int64_t ldx, const void* w_gate_up, int64_t ldwg, const void* w_down,

@@ -20,9 +20,9 @@
 // bf16 products of M x N x K):
 //   small  128 x 128, 4 waves of 64 x 64, two steps in LDS (64 KB), two
 //          workgroups per CU.  Operands go straight to LDS; those whose rows do
-//          not start at 16 bytes or end inside a 16-byte vector (in fp32; in the
-//          others where copying them first takes longer, see copies()) pass
-//          through registers, two steps ahead.  2048 x 4096 x 1024 22 us
+//          not start at 16 bytes or end inside a 16-byte vector, where copying
+//          them first takes longer (see copies()), pass through registers, two
+//          steps ahead.  2048 x 4096 x 1024 22 us
 //          (0.8 PFLOP/s; huge 30, mini 31), through registers 31.  fp32: 4096 x
 //          1024 gated x 512 70 us (123 TFLOP/s; a library product of 8192 a
 //          side 153), through registers 78.
@@ -427,12 +427,19 @@ __device__ __forceinline__ void write_block(const MmArgs& a, const char* stage, 
   __builtin_amdgcn_wave_barrier();
 }
 
-// The sums of a split depth, joined in order of the splits.
+// Two products in one launch.
+struct MmPair {
+  MmArgs a, b;
+  uint32_t na, nb;  // workgroups of each
+};
+
+// The sums of a split depth, joined in order of the splits, by block `block` of
+// `blocks`.
 template <int EPI, typename T>
-__global__ __launch_bounds__(256) void join_kernel(MmArgs a) {
+__device__ __forceinline__ void join(const MmArgs& a, uint32_t block, uint32_t blocks) {
   const int64_t half = partial_half(a.N), chunks = half / 8, total = a.M * chunks;
   const int64_t ldp = partial_ld<EPI>(a.N);
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+  for (int64_t i = (int64_t)block * 256 + threadIdx.x; i < total; i += (int64_t)blocks * 256) {
     const int64_t m = i / chunks;
     const int n = (int)(i % chunks) * 8;
     const float* p = a.work + m * ldp + n;
@@ -466,6 +473,19 @@ __global__ __launch_bounds__(256) void join_kernel(MmArgs a) {
     else
       finish_row<EPI, T, true>(a, m, n, c, u, a.N - n);
   }
+}
+template <int EPI, typename T>
+__global__ __launch_bounds__(256) void join_kernel(MmArgs a) {
+  join<EPI, T>(a, blockIdx.x, gridDim.x);
+}
+// Both products of a pair: a second launch would cost 4 us, most of it its own
+// start (300 tokens of 37, hidden 301, fp32: a training step 50.6 us -> 47.6).
+template <int EPI, typename T>
+__global__ __launch_bounds__(256) void join_pair_kernel(MmPair p) {
+  if (blockIdx.x < p.na)
+    join<EPI, T>(p.a, blockIdx.x, p.na);
+  else
+    join<MM_PLAIN, T>(p.b, blockIdx.x - p.na, p.nb);
 }
 
 // ------------------------------------------------------------------ loaders --
@@ -1053,12 +1073,8 @@ __device__ __forceinline__ void huge_tile(const MmArgs& a, uint32_t block, char*
 // ----------------------------------------------------------------- kernels --
 // One product, or two independent ones in one launch, which fill the chip
 // together where each alone leaves CUs idle: b's workgroups spread evenly among
-// a's in octets (an octet covers the XCDs).
-struct MmPair {
-  MmArgs a, b;
-  uint32_t na, nb;  // workgroups of each
-};
-// The part of a pair's launch that this workgroup has: product 0 or 1 (2: none).
+// a's in octets (an octet covers the XCDs).  The part of the launch that this
+// workgroup has: product 0 or 1 (2: none).
 __device__ __forceinline__ int part_of(const MmPair& p, uint32_t& block) {
   const uint32_t oa = (p.na + 7) / 8, ob = (p.nb + 7) / 8, o = blockIdx.x / 8;
   const uint32_t lo = (uint32_t)((uint64_t)o * ob / (oa + ob)), hi = (uint32_t)(((uint64_t)o + 1) * ob / (oa + ob));
@@ -1391,11 +1407,15 @@ uint32_t apply(MmArgs& a, const Plan& p) {
   return blocks <= (1 << 22) ? (uint32_t)blocks : 0;  // (a launch is limited to 2^32 threads, m0 to 2^31)
 }
 
+// Workgroups that join a product's split depth (0: it is not split).
+uint32_t join_blocks(const MmArgs& a) {
+  if (a.splits < 2 || !a.out) return 0;
+  return (uint32_t)std::min(cdiv((int64_t)a.M * (partial_half(a.N) / 8), 256), (int64_t)4096);
+}
 template <int EPI, typename T>
 void launch_join(const MmArgs& a, hipStream_t s) {
-  if (a.splits < 2) return;
-  const int64_t n = cdiv((int64_t)a.M * (partial_half(a.N) / 8), 256);
-  hipLaunchKernelGGL((join_kernel<EPI, T>), dim3((uint32_t)(n < 4096 ? n : 4096)), dim3(256), 0, s, a);
+  const uint32_t n = join_blocks(a);
+  if (n) hipLaunchKernelGGL((join_kernel<EPI, T>), dim3(n), dim3(256), 0, s, a);
 }
 
 template <typename T, bool RA, bool RB, int EPI>
@@ -1506,8 +1526,13 @@ hipError_t launch_pair(MmType type, MmArgs a, MmArgs b, const PairPlan& p, bool 
     hipLaunchKernelGGL((small_pair_kernel<T, EPI, false, 2, 2>), grid, dim3(256), 0, s, m);
   else
     hipLaunchKernelGGL((small_pair_kernel<T, EPI, false, 1, 2>), grid, dim3(256), 0, s, m);
-  if (a.out) launch_join<EPI, T>(a, s);
-  if (b.out) launch_join<MM_PLAIN, T>(b, s);
+  m.na = join_blocks(a), m.nb = join_blocks(b);
+  if (m.na && m.nb) {
+    hipLaunchKernelGGL((join_pair_kernel<EPI, T>), dim3(m.na + m.nb), dim3(256), 0, s, m);
+  } else {
+    launch_join<EPI, T>(a, s);
+    launch_join<MM_PLAIN, T>(b, s);
+  }
   return hipGetLastError();
 }
 
@@ -1528,7 +1553,8 @@ hipError_t launch_float(MmType type, const MmArgs& a, hipStream_t s) {
 // rows where that and the product straight to LDS take less time than the
 // product through registers, by the model (10,000 tokens of 1023,
 // hidden 4095: forward 430 -> 262 us, backward 1856 -> 653; 3000 rows, 1023
-// columns, depth 4095 in 8 bits 49 -> 40).
+// columns, depth 4095 in 8 bits 49 -> 40; 1024 tokens of 1023, hidden 4095, fp32
+// 867 -> 801 forward and backward).
 struct Copy {
   const void* src;
   int64_t ld, rows, extent;  // elements
@@ -1551,7 +1577,7 @@ double time_of(MmType type, const MmArgs& a, const MmArgs* b, bool dma_a, bool d
 // The operands of a product (or of a pair, whose A is one matrix) that are
 // copied, A first; their number.  It depends on the sizes alone.
 int copies(MmType type, const MmArgs& a, const MmArgs* b, Copy (&c)[3]) {
-  if (type == MM_FP32 || a.M < 1 || (b && b->K < 1)) return 0;
+  if (a.M < 1 || (b && b->K < 1)) return 0;
   const bool aa = odd_a(type, a) || (b && odd_a(type, *b)), ab = odd_b(type, a), bb = b && odd_b(type, *b);
   if (!aa && !ab && !bb) return 0;
   int n = 0;

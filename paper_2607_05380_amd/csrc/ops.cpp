@@ -68,7 +68,7 @@ MmType type_of(int32_t precision) { return precision == PACK_PREC_BF16 ? MM_BF16
 
 // The products of a gated block (x [T, D], hidden width F, y [T, O]).
 // (h and [dg | du] in rows of ff_ld() elements, zeros behind their ends)
-int64_t ff_ld(MmType t, int64_t cols) { return t == MM_BF16 ? PACK_FF_LD(PACK_PREC_BF16, cols) : cols; }
+int64_t ff_ld(MmType t, int64_t cols) { return PACK_FF_LD(t == MM_BF16 ? PACK_PREC_BF16 : PACK_PREC_FP32, cols); }
 MmArgs mm_gate(MmType t, int64_t T, int32_t D, int32_t F) {
   MmArgs a{};
   a.M = (int32_t)T, a.N = F, a.K = D, a.epi = MM_GATE, a.ldo = ff_ld(t, F), a.pad = (int32_t)(a.ldo - F);

@@ -194,7 +194,7 @@ def _ff_inputs(x, w_gate_up, w_down):
 
 def _ff_ld(x, cols):
     """Elements from row to row of the hidden values and of the gradients of gate and up (see tabpack.h)."""
-    return (cols + 7) // 8 * 8 if x.dtype is torch.bfloat16 else cols
+    return (cols + 7) // 8 * 8 if x.dtype is torch.bfloat16 else (cols + 3) // 4 * 4
 
 
 def gated_ff(x, w_gate_up, w_down, act="silu", residual=None, save=False):

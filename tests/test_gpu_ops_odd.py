@@ -30,14 +30,16 @@ BLOCKS = [(2050, 515, 1027, 261), (2048, 512, 1025, 256), (2048, 513, 1024, 256)
           (300, 9001, 203, 101), (4000, 510, 2044, 514)]
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
 @pytest.mark.parametrize("case", BLOCKS, ids=lambda c: "x".join(map(str, c)))
-def test_gated_ff_odd(case):
+def test_gated_ff_odd(case, dtype):
     T, D, F, O = case
-    print(f"[odd] {T} {D} {F} {O}", flush=True)
+    VE = 16 // dtype.itemsize
+    print(f"[odd] {T} {D} {F} {O} {dtype}", flush=True)
     g = torch.Generator(device="cuda").manual_seed(T + D + F)
 
     def rand(r, c, std=1.0):
-        return (torch.randn(r, c, generator=g, device="cuda") * std).bfloat16()
+        return (torch.randn(r, c, generator=g, device="cuda") * std).to(dtype)
 
     x, wg, wd = rand(T, D), rand(2 * F, D, D ** -0.5), rand(O, F, F ** -0.5)
     r, dy = rand(T, O), rand(T, O)
@@ -57,18 +59,18 @@ def test_gated_ff_odd(case):
     for got, ref in zip(grads, (DGU @ wg.double(), DGU.t() @ x.double(), dy.double().t() @ HS)):
         assert float((got.double() - ref).abs().max()) <= 0.05 * float(ref.abs().max())
     # rows at 16 bytes with NaN inside their last vector, and rows at any element: the same products of the same copies
-    for pad, shift in ((7, 0), (3, 1)):
-        ld = [(n + pad) // 8 * 8 if shift == 0 else n + pad for n in (D, F, O)]
+    for pad, shift in ((VE - 1, 0), (3, 1)):
+        ld = [(n + pad) // VE * VE if shift == 0 else n + pad for n in (D, F, O)]
         a = (_view(x, ld[0], shift), _view(wg, ld[0], shift), _view(wd, ld[1], shift))
         rv, dv = _view(r, ld[2], shift), _view(dy, ld[2], shift)
         _poison()
         y2, saved2 = ops.gated_ff(*a, residual=rv, save=True)
-        if all(n % 8 for n in (D, F, O)):  # (otherwise unaligned views of aligned extents pass through registers)
+        if all(n % VE for n in (D, F, O)):  # (otherwise unaligned views of aligned extents pass through registers)
             assert torch.equal(y2, y)
         assert float((y2.double() - Y).abs().max()) <= 0.05 * float(Y.abs().max())
         again = ops.gated_ff_backward(dv, *a, saved)
         for got, ref in zip(again, grads):
-            if all(n % 8 for n in (D, F, O)):
+            if all(n % VE for n in (D, F, O)):
                 assert torch.equal(got, ref)
             assert float((got.double() - ref.double()).abs().max()) <= 0.05 * float(ref.abs().max())
     # saved values that went through a copy
