@@ -11,6 +11,7 @@ from paper_2607_05380_amd import profiles_summary as ps
     ("_ZN7tabpack12_GLOBAL__N_117small_pair_kernelIDF16bLi2ELb1ELi1ELi4EEEvNS0_6MmPairE", "mm_small_pair_bf16_gate_bwd"),
     ("_ZN7tabpack12_GLOBAL__N_111thin_kernelIaLi4ELi4EEEvNS_6MmArgsE", "mm_thin_i8_q8_gate"),
     ("_ZN7tabpack12_GLOBAL__N_111join_kernelILi0EDF16bEEvNS_6MmArgsE", "mm_join_bf16_plain"),
+    ("_ZN7tabpack12_GLOBAL__N_116join_pair_kernelILi2EfEEvNS0_6MmPairE", "mm_join_pair_f32_gate_bwd"),
     ("_ZN7tabpack12_GLOBAL__N_111rows_kernelIDF16bLi64ELi16ELi1EEEvNS_7RowArgsE", "rows_bf16_norm_q8"),
     ("_ZN7tabpack12_GLOBAL__N_115norm_bwd_kernelIDF16bLi64ELi16EEEvNS_11NormBwdArgsE", "norm_bwd"),
     ("_ZN7tabpack12_GLOBAL__N_114distill_kernelIDF16bLi512ELi64ELb0EEEvNS_11DistillArgsE", "distill"),
