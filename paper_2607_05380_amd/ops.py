@@ -227,7 +227,8 @@ def gated_ff_backward(dy, x, w_gate_up, w_down, saved, act="silu", need_dx=True)
         _fail("saved gate and up values must be contiguous")
     code = _act(act)
     ldh = _ff_ld(x, hidden)
-    if h.stride(0) != ldh or h.untyped_storage().nbytes() < (h.storage_offset() + tokens * ldh) * h.element_size():
+    if h.stride(0) != ldh or (ldh > hidden and h.untyped_storage().nbytes() <
+                              (h.storage_offset() + tokens * ldh) * h.element_size()):
         own = _empty(x, tokens, ldh)  # (a copy of what gated_ff saved, in rows of another length)
         own[:, :hidden] = h
         h = own

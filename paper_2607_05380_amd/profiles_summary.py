@@ -86,7 +86,8 @@ def short_name(kernel):
         if epi >= len(EPIS) or ak >= len(OPS) or bk >= len(OPS):
             return None
         return f"gemm_{t}_{OPS[ak]}_{OPS[bk]}_{EPIS[epi]}"
-    m = re.search(r"\d(small|small_pair|huge|thin|join|join_pair)_kernelI(DF16b|f|a)?((?:Lb\dE)*)Li(\d)E(DF16b|f|a)?", kernel)
+    m = re.search(r"\d(small|small_pair|huge|thin|join|join_pair)_kernelI(DF16b|f|a)?((?:Lb\dE)*)Li(\d)E(DF16b|f|a)?",
+                  kernel)
     if m:
         t = {"DF16b": "bf16", "f": "f32", "a": "i8"}[m.group(2) or m.group(5)]
         ops = "" if m.group(1) != "small" and m.group(1) != "huge" else "_" + "".join(
