@@ -384,6 +384,8 @@ int pack_profile_read(pack_handle* h, pack_kernel_stat* out, int32_t max, int32_
  *                takes it unrounded), or NULL; may be x or residual itself
  *   out          device [rows, cols]
  *   rstd_out     device fp32 [rows]: rho, for the backward pass, or NULL
+ * Holds for every finite v, also where v^2 is past the largest fp32 value.
+ * (Squares below 2^-126 lose bits: this shows only with eps near that.)
  * cols <= PACK_ROW_MAX_COLS, eps >= 0. */
 #define PACK_ROW_MAX_COLS 32768
 int pack_add_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, const float* weight,

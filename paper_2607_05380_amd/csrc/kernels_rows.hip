@@ -170,11 +170,13 @@ __device__ __forceinline__ float code_factor(float a) {
 // The codes of y are those of t = v w: rho > 0 is common to the row, so
 // q = rint(t 127 / max|t|) and the scale is max|t| rho / 127 -- a row's codes
 // do not depend on the order in which its squares were added.  A row that
-// holds an infinity or NaN gets codes 0 and scale NaN.
+// holds an infinity or NaN gets codes 0 and scale NaN.  Where the squares
+// overflow (values past 1.8e19) the row goes on 2^-80 times smaller, which
+// changes neither y nor the codes.
 template <typename T, int G, int EPT, int MODE>
 __global__ __launch_bounds__(G > 256 ? G : 256) void rows_kernel(RowArgs a) {
   constexpr int VE = kVec<T>, NT = G > 256 ? G : 256, RPB = NT / G, NV = EPT / VE;
-  __shared__ float red[2][2][16];
+  __shared__ float red[2][3][16];
   const int tid = threadIdx.x, t = tid % G;
   static_assert(G <= 64 || RPB == 1, "a row's barriers are the block's");
   int turn = 0;  // rows take turns with two sets of LDS words: a row's barriers lie between their uses
@@ -215,7 +217,20 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void rows_kernel(RowArgs a) {
       for (int e = 0; e < EPT; ++e) sq = fmaf(v[e], v[e], sq);
       sq = reduce_row<G, OpAdd>(sq, red[turn][0], tid);
       rho = 1.0f / sqrtf(sq / (float)a.cols + a.eps);
-      if (a.rstd && t == 0) a.rstd[row] = rho;
+      float rstd = rho;
+      if (!(sq < __builtin_inff())) {  // (the same for all threads of the row)
+        constexpr float kDown = 0x1p-80f;
+        float down = 0.0f;
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) {
+          v[e] *= kDown;
+          down = fmaf(v[e], v[e], down);
+        }
+        down = reduce_row<G, OpAdd>(down, red[turn][2], tid);
+        rho = 1.0f / sqrtf(down / (float)a.cols + a.eps * kDown * kDown);
+        rstd = rho * kDown;
+      }
+      if (a.rstd && t == 0) a.rstd[row] = rstd;
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const int c = (i * G + t) * VE;
