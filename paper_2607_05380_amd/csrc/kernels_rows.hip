@@ -272,8 +272,10 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void rows_kernel(RowArgs a) {
 }
 
 // --------------------------------------------------------- norm, backward --
-// With g = w dy, rho as saved and D = cols:
-//   dx = rho (g - v rho^2 / D sum_c g v) + dsum,   dweight = sum_rows dy v rho.
+// With g = w dy, rho as saved, n = v rho and D = cols:
+//   dx = rho (g - n / D sum_c g n) + dsum,   dweight = sum_rows dy n.
+// (The products are with n, of order 1 whatever the row's magnitude: those with v
+// and rho^2 leave fp32's range where v is large.)
 // A block walks over rows (gridDim apart) and keeps the columns' weight sums
 // in registers; its sums go to one row of `partial`, which a second kernel
 // adds up in order: no atomics, so the result does not change between runs.
@@ -303,8 +305,8 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void norm_bwd_kernel(NormBwdArgs
         os[i].raw = u32x4{0, 0, 0, 0};
     }
     const float rho = a.rstd[row];
-    // bf16 keeps v and g as floats; fp32 multiplies by the weight, read again from
-    // the cache, a second time (16,384 x 4096: bf16 93 us against 99 the other
+    // bf16 keeps n and g as floats; fp32 keeps n in v's place and forms g, the weight
+    // read again from the cache, a second time (16,384 x 4096: bf16 93 us against 99 the other
     // way, fp32 156 against 183)
     constexpr bool KEEP = sizeof(T) == 2;
     float kv[KEEP ? EPT : 1], kg[KEEP ? EPT : 1], dot = 0.0f;
@@ -317,14 +319,16 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void norm_bwd_kernel(NormBwdArgs
       gs[i].get(g);
 #pragma unroll
       for (int e = 0; e < VE; ++e) {
-        dw[i * VE + e] = fmaf(g[e] * v[e], rho, dw[i * VE + e]);
+        v[e] *= rho;
+        dw[i * VE + e] = fmaf(g[e], v[e], dw[i * VE + e]);
         g[e] *= w[e];
         dot = fmaf(g[e], v[e], dot);
         if constexpr (KEEP) kv[i * VE + e] = v[e], kg[i * VE + e] = g[e];
       }
+      if constexpr (!KEEP) vs[i].raw = __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]});
     }
     dot = reduce_row<G, OpAdd>(dot, red[turn], tid);
-    const float c1 = dot / (float)a.cols * rho * rho;
+    const float c1 = dot / (float)a.cols;
     T* dx = static_cast<T*>(a.dx) + row * a.ldx;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
