@@ -92,16 +92,22 @@ __device__ __forceinline__ float exp_neg(float x) { return __builtin_amdgcn_exp2
 // costs ten instructions more)
 __device__ __forceinline__ float logistic(float x) { return __builtin_amdgcn_rcpf(1.0f + exp_neg(x)); }
 constexpr float kInvSqrt2Pi = 0.39894228040143268f;
-// The normal distribution function at g, with e = exp(-g^2 / 2): Abramowitz and
-// Stegun 7.1.26 (erf to within 1.5e-7) for the tail beyond |g|, so that small
-// values on the negative side are not differences of large ones; no branches.
+// The normal distribution function at g, with e = exp(-g^2 / 2).  The tail beyond
+// x = |g| is e t P(t) with t = 1 / (1 + 0.31 x): its quotient by e falls like 1 / x
+// and is smooth in t.  P, of degree 7, was fitted in the largest relative error over
+// 0 <= x <= 14 (1.6e-7; evaluated in fp32 4.5e-7; e is 0 further out), so the
+// negative side keeps its leading digits, where 1 + erf would be a difference of
+// large values.  No branches.
 __device__ __forceinline__ float normal_cdf(float g, float e) {
-  const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(g), 0.3275911f * 0.70710678118654752f, 1.0f));
-  float p = fmaf(t, 1.061405429f, -1.453152027f);
-  p = fmaf(t, p, 1.421413741f);
-  p = fmaf(t, p, -0.284496736f);
-  p = fmaf(t, p, 0.254829592f);
-  const float tail = 0.5f * t * p * e;
+  const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(g), 0.31f, 1.0f));
+  float p = fmaf(t, 0.0358418226f, -0.141604945f);
+  p = fmaf(t, p, 0.155068398f);
+  p = fmaf(t, p, -0.0149038201f);
+  p = fmaf(t, p, 0.110110328f);
+  p = fmaf(t, p, 0.107771039f);
+  p = fmaf(t, p, 0.124060348f);
+  p = fmaf(t, p, 0.123656906f);
+  const float tail = t * p * e;
   return g < 0.0f ? tail : 1.0f - tail;
 }
 __device__ __forceinline__ float exp_half_square(float g) {
