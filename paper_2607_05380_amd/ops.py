@@ -11,7 +11,8 @@ class probabilities and served in 8 bits.  Its parts:
 
 Matrices are 2-D device tensors in bfloat16 or float32 whose rows are contiguous (any row stride and alignment).
 Every call runs HIP kernels on the current stream of the tensors' device; ``PackError`` says what an argument
-breaks.  Formulas and rules for empty, masked and non-finite rows are in ``include/tabpack.h``.
+breaks.  Nothing is recorded for autograd: gradients come from the backward calls, and under grad mode a tensor that
+requires a gradient is refused (``torch.no_grad()``, or the inside of an ``autograd.Function``, takes it).  Formulas and rules for empty, masked and non-finite rows are in ``include/tabpack.h``.
 """
 import ctypes
 import functools
@@ -66,9 +67,16 @@ def _prec(t, name):
 def _call(fn, like, others, *args):
     """The library call on the current stream of like's device (where all of others must be)."""
     dev = like.get_device()
+    grad = torch.is_grad_enabled()
+    lost = grad and like.requires_grad
     for t in others:
-        if t is not None and t.get_device() != dev:
-            _fail("all tensors must be on one device")
+        if t is not None:
+            if t.get_device() != dev:
+                _fail("all tensors must be on one device")
+            lost = lost or grad and t.requires_grad
+    if lost:
+        _fail("a tensor requires a gradient, which the operators do not record: call them under torch.no_grad() and "
+              "take gradients from their backward calls")
     call = getattr(tabpack.load_library(), fn)
     if dev == torch.cuda.current_device():
         rc = call(*args, _raw_stream(dev))
