@@ -166,6 +166,8 @@ def distill_topk(logits, idx, teacher, temperature=1.0, row_weight=None, grad=Tr
     rows, classes = logits.shape
     _matrix(idx, "idx", torch.int32)
     k = idx.shape[1]
+    if k >= 1 << 31:  # (the C call counts in 32 bits; of the sizes this one alone is no leading dimension)
+        _fail(f"k={k} must be below 2^31")
     if idx.shape[0] != rows:
         _fail(f"idx must have {rows} rows, not {idx.shape[0]}")
     _matrix(teacher, "teacher", torch.float32, (rows, k))
