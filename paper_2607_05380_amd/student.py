@@ -16,7 +16,7 @@ import argparse
 
 import torch
 
-from . import ops
+from . import ops, tabpack
 
 
 def teacher_entries(prob, k):
@@ -31,6 +31,13 @@ class Student:
 
     def __init__(self, d_in, classes, blocks=2, hidden=512, act="silu", dtype=torch.bfloat16, eps=1e-6, seed=0,
                  device="cuda"):
+        for name, n in (("d_in", d_in), ("classes", classes), ("blocks", blocks), ("hidden", hidden)):
+            if n < 1:
+                raise ops.PackError(f"{name}={n} must be positive")
+        if act not in tabpack.ACTIVATIONS:
+            raise ops.PackError(f"unknown activation {act!r}")
+        if dtype not in (torch.bfloat16, torch.float32):
+            raise ops.PackError(f"dtype must be bfloat16 or float32, not {dtype}")
         g = torch.Generator(device=device).manual_seed(seed)
 
         def normal(rows, cols):
@@ -119,7 +126,7 @@ class Student:
 
 
 def main(argv=None):
-    from . import configs, synth, tabpack
+    from . import configs, synth
     ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     ap.add_argument("--members", type=int, default=16)
     ap.add_argument("--rows", type=int, default=50_000)
