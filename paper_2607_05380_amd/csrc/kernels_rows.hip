@@ -521,7 +521,10 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void distill_kernel(DistillArgs 
       top = m;
     }
     total = reduce_row<G, OpAdd>(total, red[1], tid);
-    if constexpr (G <= 64) __builtin_amdgcn_wave_barrier();
+    if constexpr (G <= 64) {  // (wider rows had a block barrier since lane 0 wrote the entries' sum)
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
 
     const float tsum = *te.sum;
     const bool zero = !live || tsum == 0.0f;  // nothing of the row counts
