@@ -92,7 +92,9 @@ def short_name(kernel):
         t = {"DF16b": "bf16", "f": "f32", "a": "i8"}[m.group(2) or m.group(5)]
         ops = "" if m.group(1) != "small" and m.group(1) != "huge" else "_" + "".join(
             "kr"[int(b)] for b in re.findall(r"Lb(\d)E", m.group(3))[:2])
-        return f"mm_{m.group(1)}_{t}{ops}_{MM_EPIS[int(m.group(4))]}"
+        # small_kernel and small_pair_kernel: 64 x 64 tiles, or 128 x 128, which the name then says
+        nb = re.search(r"small(?:_pair)?_kernelI\w*?Li\d+ELb\dELi(\d)E", kernel)
+        return f"mm_{m.group(1)}_{t}{ops}_{MM_EPIS[int(m.group(4))]}" + ("_128" if nb and nb.group(1) == "2" else "")
     m = re.search(r"\drows_kernelI(DF16b|f)Li\d+ELi\d+ELi(\d)E", kernel)
     if m:
         return f"rows_{'f32' if m.group(1) == 'f' else 'bf16'}_{ROW_MODES[int(m.group(2))]}"
