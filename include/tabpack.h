@@ -366,7 +366,8 @@ int pack_profile_read(pack_handle* h, pack_kernel_stat* out, int32_t max, int32_
  * ensemble's class probabilities (pack_distill_topk), built of pre-normalised
  * gated blocks (pack_add_rms_norm, pack_gated_ff_*), and serve it in 8 bits
  * (pack_add_rms_norm_q8, pack_quantize_rows, pack_q8_matmul).  They need no
- * handle, keep nothing between calls and allocate nothing.
+ * handle, allocate nothing and keep no data between calls (a thread remembers how
+ * it laid out products of the last sizes, which follows from the sizes alone).
  *
  * Matrices are row-major with a leading dimension (elements from one row to
  * the next) of at least the row's length; elements of a row are contiguous.

@@ -1301,7 +1301,8 @@ Plan plan_with(MmType type, const MmArgs& a, Tiles t, int64_t splits) {
 }
 
 // A model of a product's time in us, fitted to measurements of 128..16384 rows,
-// 256..4096 columns and depths 1024..16384: a start, a time per K step that
+// 256..4096 columns and depths 1024..16384 (fewer rows and shorter depths are
+// extrapolated): a start, a time per K step that
 // grows with the tiles a CU holds, and the join's traffic.  Mini tiles step in
 // 0.2 us a tile, small ones in 0.6, huge ones in 1.05 on a few CUs and 1.6 where
 // all of them run (the clock falls under their power); operands through
@@ -1328,7 +1329,9 @@ constexpr int64_t kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
 // The layout that should be fastest.  Up to 16 rows the thin kernel (at depth
 // 1024 and 1024..4096 columns 3.8-5.1 us against 5.6-6.8 on mini tiles; at 32
 // rows it no longer gains: 7.0 / 6.6, depth 4096 13.4 / 9.9 split), the others
-// by the model.
+// by the model.  Thin products of few columns leave CUs idle, whatever their
+// depth: 1024 columns are 64 workgroups, at depth 4096 in bf16 7.5 us, 1.1 TB/s of
+// weights.
 Plan search(MmType type, const MmArgs& a, bool dma) {
   Plan best = plan_with(type, a, TILES_MINI, 1);
   best.us = 1e30;

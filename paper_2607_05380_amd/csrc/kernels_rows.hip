@@ -14,7 +14,7 @@
 // Measured on tensors larger than the caches, against 5.1 TB/s of a device copy:
 // norm with residual 65,536 x 1024 bf16 93 us (5.8 TB/s of reads and writes),
 // with 8-bit output 88 us, its backward with both gradients 106 us (5.1 TB/s),
-// quantising 35 us (5.8 TB/s); 500,000 x 64 bf16 norm 52 us (4 and 16 threads a
+// quantising 35 us (5.8 TB/s); 500,000 x 64 bf16 norm 53 us (4 and 16 threads a
 // row: a wave a row takes 181); distillation 4096 x 32,000 bf16 with 32 entries
 // a row 120 us (4.4 TB/s).  Odd lengths (4095) cost up to 1.3 times the time in
 // bf16, whose stores then share their lines; rows of 32,768 in the backward pass
