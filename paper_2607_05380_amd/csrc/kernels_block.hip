@@ -41,11 +41,12 @@
 // v_mfma_f32_32x32x2_f32, with B as the first operand, so that a lane holds 4
 // consecutive columns of one row of C.  Accumulators are fp32 or int32, added
 // in a fixed order; a depth split over workgroups is joined in a fixed order
-// by a second kernel.  What is rounded to bf16 between two products (h, the saved
-// g and u, dg and du) is rounded once, from fp32: the next product's
-// instructions take bf16, and fp32 copies would double the bytes of the gate
-// epilogues, which already are a third of those kernels' time (16,384 x 4096 x
-// 1024, backward 205 us, 670 MB).
+// by a second kernel.  What is rounded to bf16 between two products (h, dg and du)
+// is rounded once, from fp32, since the next product's instructions take bf16; g and
+// u are saved in fp32.  So a gradient in bf16 has sqrt(2) times the error of its own
+// rounding.  With g and u rounded as well it had 1.8 times, in a training step of
+// 16,384 tokens of 1024, hidden 4096, that took 1206 us instead of 1321 (2048
+// tokens 216, 229): the bytes of the two gate epilogues bound the difference.
 #include <algorithm>
 #include <cmath>
 
@@ -257,7 +258,7 @@ struct Cols {
 };
 template <int EPI, typename T, bool PART>
 struct Extra {
-  Raw8<T> g, u;
+  Raw8<std::conditional_t<EPI == MM_GATE_BWD, float, T>> g, u;
   float row_scale;
   __device__ __forceinline__ void load(const MmArgs& a, int64_t m, int n, int cnt) {
     if constexpr (is_q8(EPI)) row_scale = a.row_scale[m];
@@ -265,7 +266,7 @@ struct Extra {
       if (a.add) g.template load_some<PART>(static_cast<const T*>(a.add) + m * a.ldadd + n, cnt);
     }
     if constexpr (EPI == MM_GATE_BWD) {
-      const T* p = static_cast<const T*>(a.pre) + m * a.ldpre + n;
+      const float* p = a.pre + m * a.ldpre + n;
       g.template load_some<PART>(p, cnt);
       u.template load_some<PART>(p + a.N, cnt);
     }
@@ -305,7 +306,7 @@ __device__ __forceinline__ void finish8(const MmArgs& a, int64_t m, int n, float
     store_some<PART>(static_cast<T*>(a.out) + m * a.ldo + n, c, cnt);
   } else if constexpr (EPI == MM_GATE) {
     if (a.pre) {
-      T* p = static_cast<T*>(a.pre) + m * a.ldpre + n;
+      float* p = a.pre + m * a.ldpre + n;
       store_some<PART>(p, c, cnt);
       store_some<PART>(p + a.N, u, cnt);
     }
@@ -898,13 +899,15 @@ __device__ __forceinline__ void tie(bf16x8 (&f)[4]) {
 }
 
 // A wave's 128 x 64 sums to the outputs, one 64 x 64 half after the other.  No
-// other workgroup on the CU covers the waits, so what a quarter's rows read
-// besides the sums is asked for a quarter ahead.
+// other workgroup on the CU covers the waits, so what a piece's rows read besides
+// the sums is asked for a piece ahead: 32 rows, or 16 where they read two fp32
+// values an output (32 would not fit the registers).
 template <int EPI, typename T, typename A16>
 __device__ __forceinline__ void huge_out(const MmArgs& a, const A16 (&acc)[2][2][2], char* stage, int m0, int n0,
                                          int split, int lane) {
   typedef typename Ty<T>::acc_t acc_t;
-  constexpr int COLS = is_gate(EPI) ? 32 : 64, CH = COLS / 8, RP = 64 / CH, NP = 32 / RP;  // passes a quarter
+  constexpr int COLS = is_gate(EPI) ? 32 : 64, CH = COLS / 8, RP = 64 / CH;
+  constexpr int PIECE = EPI == MM_GATE_BWD ? 16 : 32, PIECES = 64 / PIECE, NP = PIECE / RP;  // NP passes a piece
   const int ch = lane % CH, r0 = lane / CH, n = n0 + 8 * ch;
   if (a.splits > 1 || n0 + COLS > a.N) {
 #pragma unroll
@@ -919,18 +922,18 @@ __device__ __forceinline__ void huge_out(const MmArgs& a, const A16 (&acc)[2][2]
   Extra<EPI, T, false> x[NP], y[NP];
   auto ask = [&](Extra<EPI, T, false>(&e)[NP], int q) {
 #pragma unroll
-    for (int p = 0; p < NP; ++p) e[p].load(a, min(m0 + q * 32 + p * RP + r0, a.M - 1), n, 8);
+    for (int p = 0; p < NP; ++p) e[p].load(a, min(m0 + q * PIECE + p * RP + r0, a.M - 1), n, 8);
   };
   ask(x, 0);
 #pragma unroll
   for (int h = 0; h < 2; ++h) {  // (unrolled: the first half's sums give up their registers)
     stage_block<acc_t, 2>(acc[h], stage, lane);
 #pragma unroll 1
-    for (int q = 0; q < 2; ++q) {
-      if (h + q < 2) ask(y, 2 * h + q + 1);
+    for (int q = 0; q < PIECES; ++q) {
+      if (PIECES * h + q + 1 < 2 * PIECES) ask(y, PIECES * h + q + 1);
 #pragma unroll
       for (int p = 0; p < NP; ++p) {
-        const int row = q * 32 + p * RP + r0, m = m0 + h * 64 + row;
+        const int row = q * PIECE + p * RP + r0, m = m0 + h * 64 + row;
         float c[8], u[8];
         unstage8<2>(stage, row, 2 * ch, c);
         if constexpr (is_gate(EPI)) unstage8<2>(stage, row, 8 + 2 * ch, u);
@@ -1458,7 +1461,7 @@ hipError_t launch_tiles(MmType type, MmArgs a, hipStream_t s) {
 // Two products in one launch: the same tiles, and depths split so that the
 // workgroups of both take about the same number of steps.  Not for huge tiles:
 // the gradients of gate and up beside the down weights' (16,384 tokens of 1024,
-// hidden 4096) 365 us together, 222 + 122 apart.
+// hidden 4096; g and u read in bf16) 365 us together, 222 + 122 apart.
 struct PairPlan {
   Plan a, b;
   double us;

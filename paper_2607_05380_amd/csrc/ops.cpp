@@ -154,7 +154,7 @@ int pack_gated_ff_workspace_size(int32_t precision, int64_t tokens, int32_t d_in
 
 int pack_gated_ff_forward(const void* x, int64_t ldx, const void* w_gate_up, int64_t ldwg, const void* w_down,
                           int64_t ldwd, const void* residual, int64_t ldr, int32_t precision, int32_t act,
-                          int64_t tokens, int32_t d_in, int32_t hidden, int32_t d_out, void* gate_up_out,
+                          int64_t tokens, int32_t d_in, int32_t hidden, int32_t d_out, float* gate_up_out,
                           void* hidden_out, void* out, int64_t ldo, void* work, size_t work_bytes,
                           hipStream_t stream) {
   int rc = check_ff(precision, act, tokens, d_in, hidden, d_out);
@@ -182,7 +182,7 @@ int pack_gated_ff_forward(const void* x, int64_t ldx, const void* w_gate_up, int
 }
 
 int pack_gated_ff_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* w_gate_up,
-                           int64_t ldwg, const void* w_down, int64_t ldwd, const void* gate_up, const void* hidden_in,
+                           int64_t ldwg, const void* w_down, int64_t ldwd, const float* gate_up, const void* hidden_in,
                            int32_t precision, int32_t act, int64_t tokens, int32_t d_in, int32_t hidden,
                            int32_t d_out, void* dgate_up, void* dx_out, int64_t lddx, void* dw_gate_up_out,
                            void* dw_down_out, void* work, size_t work_bytes, hipStream_t stream) {
@@ -202,7 +202,7 @@ int pack_gated_ff_backward(const void* dy, int64_t lddy, const void* x, int64_t 
   MmArgs dh = mm_dh(t, tokens, hidden, d_out), dwd = mm_dwd(t, tokens, hidden, d_out);
   MmArgs dx = mm_dx(t, tokens, d_in, hidden), dwg = mm_dwg(t, tokens, d_in, hidden);
   dh.A = dy, dh.lda = lddy, dh.B = w_down, dh.ldb = ldwd, dh.act = act;
-  dh.pre = const_cast<void*>(gate_up), dh.ldpre = 2 * (int64_t)hidden, dh.out = dgate_up;
+  dh.pre = const_cast<float*>(gate_up), dh.ldpre = 2 * (int64_t)hidden, dh.out = dgate_up;
   dwd.A = dy, dwd.lda = lddy, dwd.B = hidden_in, dwd.out = dw_down_out, dwd.ldo = hidden;
   dx.A = dgate_up, dx.B = w_gate_up, dx.ldb = ldwg, dx.out = dx_out, dx.ldo = lddx;
   dwg.A = dgate_up, dwg.B = x, dwg.ldb = ldx, dwg.out = dw_gate_up_out, dwg.ldo = d_in;

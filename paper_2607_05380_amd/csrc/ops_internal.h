@@ -79,7 +79,7 @@ struct MmArgs {
   int32_t pad;            // MM_GATE, MM_GATE_BWD: columns behind each row of out that are set to zero (bf16, fp32)
   int32_t epi, act;
   const void* add;        // MM_PLAIN: or NULL
-  void* pre;              // [M, 2N] gate and up values (MM_GATE: or NULL)
+  float* pre;             // [M, 2N] gate and up values (MM_GATE: or NULL)
   void* out;
   int64_t ldadd, ldpre, ldo;
   const float* row_scale;

@@ -210,12 +210,12 @@ def _ff_ld(x, cols):
 def gated_ff(x, w_gate_up, w_down, act="silu", residual=None, save=False):
     """y = h w_down^T (+ residual) with [g | u] = x w_gate_up^T and h = act(g) u: x [tokens, d_in], w_gate_up
     [2 hidden, d_in] (gate rows, then up rows), w_down [d_out, hidden], all in one type; act "silu", "gelu" or
-    "relu".  save=True: (y, saved), saved = ([g | u], h) for gated_ff_backward."""
+    "relu".  save=True: (y, saved), saved = ([g | u] in fp32, h) for gated_ff_backward."""
     prec, dims, ptrs = _ff_inputs(x, w_gate_up, w_down)
     tokens, _, hidden, d_out = dims
     rp, ldr = (None, 0) if residual is None else _matrix(residual, "residual", x.dtype, (tokens, d_out))
     code = _act(act)
-    gu = _empty(x, tokens, 2 * hidden) if save else None
+    gu = _empty(x, tokens, 2 * hidden, dtype=torch.float32) if save else None
     h, y = _empty(x, tokens, _ff_ld(x, hidden)), _empty(x, tokens, d_out)
     work = _work(x, "pack_gated_ff_workspace_size", prec, *dims, 0)
     _call("pack_gated_ff_forward", x, (w_gate_up, w_down, residual), *ptrs, rp, ldr, prec, code, *dims,
@@ -231,8 +231,8 @@ def gated_ff_backward(dy, x, w_gate_up, w_down, saved, act="silu", need_dx=True)
     tokens, d_in, hidden, d_out = dims
     gp, ldg = _matrix(dy, "dy", x.dtype, (tokens, d_out))
     gu, h = saved
-    for t, name, cols in ((gu, "saved gate and up values", 2 * hidden), (h, "saved hidden values", hidden)):
-        _matrix(t, name, x.dtype, (tokens, cols))
+    _matrix(gu, "saved gate and up values", torch.float32, (tokens, 2 * hidden))
+    _matrix(h, "saved hidden values", x.dtype, (tokens, hidden))
     if not gu.is_contiguous():
         _fail("saved gate and up values must be contiguous")
     code = _act(act)

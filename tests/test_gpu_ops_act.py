@@ -50,7 +50,7 @@ def test_gated_ff_activation(tokens, act, dtype):
     y, saved = ops.gated_ff(x, eye, one, act=act, save=True)
     g = g.astype(np.float64)
     v, rel, d, dtol = _act(act, g)
-    assert torch.equal(saved[0], x)
+    assert torch.equal(saved[0], x.float())
     tol = np.abs(v) * (rel + 2 * HALF[dtype]) + 1e-40
     assert _off(y[:, 0], v, tol) is None, _off(y[:, 0], v, tol)
     dy = torch.ones(tokens, 1, device="cuda").to(dtype)
