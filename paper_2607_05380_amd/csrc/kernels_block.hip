@@ -1564,7 +1564,7 @@ hipError_t launch_float(MmType type, const MmArgs& a, hipStream_t s) {
 // workspace is asked for cannot depend on pointers) are first copied to aligned
 // rows where that and the product straight to LDS take less time than the
 // product through registers, by the model (10,000 tokens of 1023,
-// hidden 4095: forward 430 -> 262 us, backward 1856 -> 653; 3000 rows, 1023
+// hidden 4095, g and u then in bf16: forward 430 -> 262 us, backward 1856 -> 653; 3000 rows, 1023
 // columns, depth 4095 in 8 bits 49 -> 40; 1024 tokens of 1023, hidden 4095, fp32
 // 867 -> 801 forward and backward).
 struct Copy {
