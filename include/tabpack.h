@@ -364,9 +364,11 @@ int pack_profile_read(pack_handle* h, pack_kernel_stat* out, int32_t max, int32_
  * Operators of a student network.  An ensemble of up to 32 members answers
  * with up to 32 forward passes; these calls train one network on the
  * ensemble's class probabilities (pack_distill_topk), built of pre-normalised
- * gated blocks (pack_add_rms_norm, pack_gated_ff_*), and serve it in 8 bits
- * (pack_add_rms_norm_q8, pack_quantize_rows, pack_q8_matmul).  They need no
- * handle, allocate nothing and keep no data between calls (a thread remembers how
+ * gated blocks (pack_add_rms_norm or pack_add_layer_norm, pack_gated_ff_*,
+ * pack_dropout) over a table's columns (pack_embed for categorical ones), and
+ * serve it in 8 bits (pack_add_rms_norm_q8, pack_quantize_rows, pack_q8_matmul,
+ * or with 8-bit floating point codes pack_quantize_blocks, pack_quantize_tiles,
+ * pack_f8_matmul).  They need no handle, allocate nothing and keep no data between calls (a thread remembers how
  * it laid out products of the last sizes, which follows from the sizes alone).
  *
  * Matrices are row-major with a leading dimension (elements from one row to
@@ -502,6 +504,104 @@ int pack_q8_matmul(const int8_t* x, int64_t ldx, const float* x_scale, const int
                    const float* w_scale, const float* bias, int32_t gate, int32_t precision, int64_t rows,
                    int32_t outputs, int32_t depth, void* out, int64_t ldo, void* work, size_t work_bytes,
                    hipStream_t stream);
+
+/* Layer norm: y = (v - mu) rho w + b with v = x + residual, mu = mean_c v and
+ * rho = (mean_c (v - mu)^2 + eps)^(-1/2) per row.
+ *   x, residual  device [rows, cols]; residual NULL: v = x
+ *   weight       device fp32 [cols]; bias device fp32 [cols] or NULL (0)
+ *   sum_out      device [rows, cols]: v rounded to the precision (the norm
+ *                takes it unrounded), or NULL; may be x or residual itself
+ *   out          device [rows, cols]
+ *   mean_out, rstd_out  device fp32 [rows]: mu and rho, for the backward pass, or NULL
+ * Holds for every finite v, also where a sum or square is past the largest fp32
+ * value.  A row that holds an infinity or NaN is NaN.  cols <= PACK_ROW_MAX_COLS,
+ * eps >= 0 (with eps = 0 a row of equal values is NaN). */
+int pack_add_layer_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, const float* weight,
+                        const float* bias, int32_t precision, int64_t rows, int32_t cols, float eps, void* sum_out,
+                        int64_t lds, void* out, int64_t ldo, float* mean_out, float* rstd_out, hipStream_t stream);
+
+/* Its gradients from its sum v (as it was stored), mu and rho: with
+ * n = (v - mu) rho and g = weight dy,
+ *   dx = rho (g - sum_c g / cols - n sum_c g n / cols) + dsum   (of x and of the residual)
+ *   dweight = sum over the rows of dy n,  dbias = sum over the rows of dy
+ *   dsum         the gradient that reaches v on its other path, or NULL
+ *   dx_out       device [rows, cols]; may be dy or dsum itself
+ *   dweight_out  device fp32 [cols]; dbias_out device fp32 [cols] or NULL
+ *   work         device scratch of pack_layer_norm_backward_workspace_size() bytes, 4-byte aligned */
+int pack_layer_norm_backward_workspace_size(int64_t rows, int32_t cols, size_t* bytes);
+int pack_layer_norm_backward(const void* dy, int64_t ldy, const void* sum, int64_t lds, const float* weight,
+                             const float* mean, const float* rstd, const void* dsum, int64_t ldd, int32_t precision,
+                             int64_t rows, int32_t cols, void* dx_out, int64_t ldx, float* dweight_out,
+                             float* dbias_out, void* work, size_t work_bytes, hipStream_t stream);
+
+/* Dropout whose mask is not stored: out = (residual +) x / (1 - p) where an
+ * element is kept, residual (or 0) where it is not, whatever x holds there.
+ * Element (r, c) is kept if the 16-bit half c % 2 of word (c / 2) % 4 of
+ * Philox4x32-10 with counter (c / 8, r, site, step mod 2^32) and key
+ * (seed mod 2^32, (seed >> 32) xor 2^30) is at least floor(p 2^16): the mask
+ * depends on (seed, step, site, r, c) alone.  The gradient of x is the same call
+ * on dy without a residual; the residual's is dy itself.
+ *   p        in [0, 1]; 0 keeps every element, 1 none
+ *   site     which dropout of a network this is (one step's masks differ by it)
+ *   step_at  device int64 or NULL: the step, read when the kernel runs (a
+ *            captured graph then draws new masks at each replay); NULL: step
+ *   out      device [rows, cols]; may be x or residual itself */
+int pack_dropout(const void* x, int64_t ldx, const void* residual, int64_t ldr, int32_t precision, int64_t rows,
+                 int32_t cols, double p, uint64_t seed, uint64_t step, const int64_t* step_at, uint32_t site, void* out,
+                 int64_t ldo, hipStream_t stream);
+
+/* Lookup in a table: out[t] = scale table[idx[t]] (rounded once).
+ *   idx      device [tokens], int32 or (idx64 != 0) int64.  A negative index
+ *            gives a row of zeros, one >= rows a row of NaN.
+ *   table    device [rows, cols]; out device [tokens, cols]
+ * rows and tokens < 2^31, cols <= 2^24. */
+int pack_embed(const void* idx, int32_t idx64, const void* table, int64_t ldt, int32_t precision, int64_t tokens,
+               int64_t rows, int32_t cols, float scale, void* out, int64_t ldo, hipStream_t stream);
+
+/* The table's gradient: dtable_out[v] = scale times the sum over the t with
+ * idx[t] = v of dy[t], in fp32 and a fixed order, rounded once.  Indices that are
+ * negative or >= rows add to no row; rows that no index names are 0.
+ *   dy          device [tokens, cols]
+ *   dtable_out  device [rows, cols], dense
+ *   work        device scratch, 16-byte aligned, of
+ *               pack_embed_backward_workspace_size() bytes */
+int pack_embed_backward_workspace_size(int32_t precision, int64_t tokens, int64_t rows, int32_t cols, size_t* bytes);
+int pack_embed_backward(const void* dy, int64_t ldy, const void* idx, int32_t idx64, int32_t precision, int64_t tokens,
+                        int64_t rows, int32_t cols, float scale, void* dtable_out, void* work, size_t work_bytes,
+                        hipStream_t stream);
+
+/* 8-bit floating point codes (e4m3 as of the OCP format: largest value 448, no
+ * infinity) with a scale for each block: q = e4m3(x 448 / max|x|), to the nearest
+ * (ties to the even code), scale = max|x| / 448 over the block.
+ * pack_quantize_blocks: a block is PACK_F8_BLOCK columns of a row (activations);
+ *   scale_out  device fp32 [ceil(cols / 128), rows]
+ * pack_quantize_tiles: a block is 128 x 128 of one of `parts` row ranges of x
+ *   [parts rows, cols] (weights [outputs, depth]; a gated weight has 2 parts);
+ *   scale_out  device fp32 [parts ceil(rows / 128), ceil(cols / 128)]
+ * A block whose largest magnitude is 0 (or below 448 / FLT_MAX) has codes 0 and
+ * scale 0; one that holds an infinity or NaN has codes 0 and scale NaN. */
+#define PACK_F8_BLOCK 128
+int pack_quantize_blocks(const void* x, int64_t ldx, int32_t precision, int64_t rows, int32_t cols, void* q_out,
+                         int64_t ldq, float* scale_out, hipStream_t stream);
+int pack_quantize_tiles(const void* x, int64_t ldx, int32_t precision, int64_t rows, int32_t parts, int32_t cols,
+                        void* q_out, int64_t ldq, float* scale_out, hipStream_t stream);
+
+/* Product of such codes, block by block of the depth:
+ *   out[m, n] = sum_b x_scale[b, m] w_scale[n / 128, b] sum_(k in block b) x[m, k] w[n, k] (+ bias[n])
+ * with sums in fp32.
+ *   gate     -1: w holds `outputs` rows; PACK_ACT_*: w, w_scale and bias hold
+ *            gate rows, then up rows (w_scale as of 2 parts), and out is
+ *            act(gate value) up value
+ *   x        device e4m3 [rows, depth], x_scale device fp32 [ceil(depth / 128), rows]
+ *   w        device e4m3, w_scale device fp32, bias device fp32 or NULL
+ *   out      device [rows, outputs] in the precision
+ *   work     device scratch, 16-byte aligned, of
+ *            pack_f8_matmul_workspace_size() bytes
+ * depth and outputs in [1, 2^24]. */
+int pack_f8_matmul_workspace_size(int64_t rows, int32_t outputs, int32_t depth, int32_t gate, size_t* bytes);
+int pack_f8_matmul(const void* x, int64_t ldx, const float* x_scale, const void* w, int64_t ldw, const float* w_scale,
+                   const float* bias, int32_t gate, int32_t precision, int64_t rows, int32_t outputs, int32_t depth,
+                   void* out, int64_t ldo, void* work, size_t work_bytes, hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -8,7 +8,8 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SRC = ["kernels_gemm.hip", "kernels_aux.hip", "kernels_muon.hip", "kernels_embed.hip", "select_static.hip",
-       "kernels_rows.hip", "kernels_block.hip", "host.cpp", "ops.cpp"]
+       "kernels_rows.hip", "kernels_layer_norm.hip", "kernels_embed_table.hip", "kernels_dropout.hip",
+       "kernels_quant.hip", "kernels_block.hip", "host.cpp", "ops.cpp"]
 LIB = os.path.join(HERE, "libtabpack.so")
 
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-Wall",

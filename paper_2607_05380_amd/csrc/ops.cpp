@@ -125,6 +125,42 @@ int check_q8(int64_t rows, int32_t outputs, int32_t depth, int32_t gate) {
   return PACK_OK;
 }
 
+MmArgs mm_f8(int64_t rows, int32_t outputs, int32_t depth, int32_t gate) {
+  MmArgs a{};
+  a.M = (int32_t)rows, a.N = outputs, a.K = depth, a.epi = gate < 0 ? MM_F8_OUT : MM_F8_GATE;
+  a.act = gate < 0 ? 0 : gate;
+  return a;
+}
+
+int check_f8(int64_t rows, int32_t outputs, int32_t depth, int32_t gate) {
+  if (gate != -1 && !known_act(gate)) return bad("unknown gate %d", gate);
+  if (rows < 0 || rows > kMaxExtent) return bad("rows=%lld out of [0, 2^31 - 1]", (long long)rows);
+  if (outputs < 1 || outputs > kMaxWidth) return bad("outputs=%d out of [1, 2^24]", outputs);
+  if (depth < 1 || depth > kMaxWidth) return bad("depth=%d out of [1, 2^24]", depth);
+  return PACK_OK;
+}
+
+int check_table(int32_t precision, int64_t tokens, int64_t rows, int32_t cols) {
+  if (!known(precision)) return bad("unknown precision %d", precision);
+  if (tokens < 0 || tokens > kMaxExtent) return bad("tokens=%lld out of [0, 2^31 - 1]", (long long)tokens);
+  if (rows < 1 || rows > kMaxExtent) return bad("rows=%lld out of [1, 2^31 - 1]", (long long)rows);
+  if (cols < 1 || cols > kMaxWidth) return bad("cols=%d out of [1, 2^24]", cols);
+  return PACK_OK;
+}
+
+int block_codes(bool tile, BlockCodeArgs& a, int32_t precision, hipStream_t stream) {
+  if (!known(precision)) return bad("unknown precision %d", precision);
+  if (a.parts < 1 || a.parts > kMaxWidth) return bad("parts=%d out of [1, 2^24]", a.parts);
+  if (a.rows < 0 || a.rows > kMaxExtent / a.parts)
+    return bad("rows=%lld of %d parts out of [0, 2^31 - 1]", (long long)a.rows, a.parts);
+  if (a.cols < 1 || a.cols > kMaxWidth) return bad("cols=%d out of [1, 2^24]", a.cols);
+  if (!ld_ok(a.ldx, a.cols) || !ld_ok(a.ldq, a.cols))
+    return bad("a leading dimension is smaller than cols=%d or too large", a.cols);
+  if (a.rows == 0) return PACK_OK;
+  if (!a.x || !a.q || !a.scale) return bad("NULL device pointer");
+  return done("block codes", launch_block_codes(precision, tile, a, stream));
+}
+
 int check_work(const void* work, size_t have, size_t need) {
   if (need == 0) return PACK_OK;
   if (!work) return bad("work is NULL");
@@ -315,6 +351,154 @@ int pack_distill_topk(const void* logits, int64_t ldz, int32_t precision, int64_
   a.logits = logits, a.ldz = ldz, a.idx = idx, a.teacher = teacher, a.weight = row_weight;
   a.loss = loss_out, a.grad = grad_out, a.ldg = ldg, a.rows = rows, a.classes = classes, a.k = k, a.tau = temperature;
   return done("distillation", launch_distill(precision, a, stream));
+}
+
+int pack_add_layer_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, const float* weight,
+                        const float* bias, int32_t precision, int64_t rows, int32_t cols, float eps, void* sum_out,
+                        int64_t lds, void* out, int64_t ldo, float* mean_out, float* rstd_out, hipStream_t stream) {
+  const int rc = check_rows(precision, rows, cols);
+  if (rc != PACK_OK) return rc;
+  if (!(eps >= 0.0f && eps <= FLT_MAX)) return bad("eps must be finite and not negative");
+  if (!ld_ok(ldx, cols) || (residual && !ld_ok(ldr, cols)) || (sum_out && !ld_ok(lds, cols)) || !ld_ok(ldo, cols))
+    return bad("a leading dimension is smaller than cols=%d or too large", cols);
+  if (rows == 0) return PACK_OK;
+  if (!x || !weight || !out) return bad("NULL device pointer");
+  LayerNormArgs a{};
+  a.x = x, a.ldx = ldx, a.residual = residual, a.ldr = ldr, a.weight = weight, a.bias = bias;
+  a.rows = rows, a.cols = cols, a.eps = eps;
+  a.sum = sum_out, a.lds = lds, a.out = out, a.ldo = ldo, a.mean = mean_out, a.rstd = rstd_out;
+  return done("layer norm", launch_layer_norm(precision, a, stream));
+}
+
+int pack_layer_norm_backward_workspace_size(int64_t rows, int32_t cols, size_t* bytes) {
+  if (!bytes) return bad("bytes is NULL");
+  const int rc = check_rows(PACK_PREC_FP32, rows, cols);
+  if (rc != PACK_OK) return rc;
+  *bytes = (size_t)layer_norm_bwd_blocks(rows, cols) * (size_t)cols * 8;
+  return PACK_OK;
+}
+
+int pack_layer_norm_backward(const void* dy, int64_t ldy, const void* sum, int64_t lds, const float* weight,
+                             const float* mean, const float* rstd, const void* dsum, int64_t ldd, int32_t precision,
+                             int64_t rows, int32_t cols, void* dx_out, int64_t ldx, float* dweight_out,
+                             float* dbias_out, void* work, size_t work_bytes, hipStream_t stream) {
+  int rc = check_rows(precision, rows, cols);
+  if (rc != PACK_OK) return rc;
+  if (!ld_ok(ldy, cols) || !ld_ok(lds, cols) || (dsum && !ld_ok(ldd, cols)) || !ld_ok(ldx, cols))
+    return bad("a leading dimension is smaller than cols=%d or too large", cols);
+  size_t need = 0;
+  rc = pack_layer_norm_backward_workspace_size(rows, cols, &need);
+  if (rc != PACK_OK) return rc;
+  if (!weight || !dweight_out || !work || (rows > 0 && (!dy || !sum || !mean || !rstd || !dx_out)))
+    return bad("NULL device pointer");
+  if (work_bytes < need) return bad("workspace has %zu bytes, %zu needed", work_bytes, need);
+  if (!aligned(work, 4)) return bad("workspace must be 4-byte aligned");
+  LayerNormBwdArgs a{};
+  a.sum = sum, a.lds = lds, a.dy = dy, a.ldy = ldy, a.dsum = dsum, a.ldd = ldd;
+  a.weight = weight, a.mean = mean, a.rstd = rstd, a.dx = dx_out, a.ldx = ldx;
+  a.dweight = dweight_out, a.dbias = dbias_out, a.partial = static_cast<float*>(work), a.rows = rows, a.cols = cols;
+  return done("layer norm backward", launch_layer_norm_bwd(precision, a, stream));
+}
+
+int pack_dropout(const void* x, int64_t ldx, const void* residual, int64_t ldr, int32_t precision, int64_t rows,
+                 int32_t cols, double p, uint64_t seed, uint64_t step, const int64_t* step_at, uint32_t site, void* out,
+                 int64_t ldo, hipStream_t stream) {
+  if (!known(precision)) return bad("unknown precision %d", precision);
+  if (rows < 0 || rows > kMaxExtent) return bad("rows=%lld out of [0, 2^31 - 1]", (long long)rows);
+  if (cols < 1) return bad("cols=%d must be positive", cols);
+  if (!(p >= 0.0 && p <= 1.0)) return bad("p must lie in [0, 1]");
+  if (!ld_ok(ldx, cols) || (residual && !ld_ok(ldr, cols)) || !ld_ok(ldo, cols))
+    return bad("a leading dimension is smaller than cols=%d or too large", cols);
+  if (step_at && !aligned(step_at, 8)) return bad("step_at must be 8-byte aligned");
+  if (rows == 0) return PACK_OK;
+  if (!x || !out) return bad("NULL device pointer");
+  constexpr uint32_t kTag = 4;  // (the packs' streams have tags 1 to 3)
+  DropoutArgs a{};
+  a.x = x, a.ldx = ldx, a.residual = residual, a.ldr = ldr, a.out = out, a.ldo = ldo, a.rows = rows, a.cols = cols;
+  a.threshold = (uint32_t)(p * 65536.0), a.scale = p < 1.0 ? (float)(1.0 / (1.0 - p)) : 0.0f;
+  a.key0 = (uint32_t)seed, a.key1 = (uint32_t)(seed >> 32) ^ (kTag << 28);
+  a.site = site, a.step = (uint32_t)step, a.step_at = step_at;
+  return done("dropout", launch_dropout(precision, a, stream));
+}
+
+int pack_embed(const void* idx, int32_t idx64, const void* table, int64_t ldt, int32_t precision, int64_t tokens,
+               int64_t rows, int32_t cols, float scale, void* out, int64_t ldo, hipStream_t stream) {
+  const int rc = check_table(precision, tokens, rows, cols);
+  if (rc != PACK_OK) return rc;
+  if (!ld_ok(ldt, cols) || !ld_ok(ldo, cols))
+    return bad("a leading dimension is smaller than cols=%d or too large", cols);
+  if (tokens == 0) return PACK_OK;
+  if (!idx || !table || !out) return bad("NULL device pointer");
+  EmbedArgs a{};
+  a.idx = idx, a.idx64 = idx64, a.table = table, a.ldt = ldt, a.out = out, a.ldo = ldo;
+  a.tokens = tokens, a.rows = rows, a.cols = cols, a.scale = scale;
+  return done("embedding", launch_embed(precision, a, stream));
+}
+
+int pack_embed_backward_workspace_size(int32_t precision, int64_t tokens, int64_t rows, int32_t cols, size_t* bytes) {
+  if (!bytes) return bad("bytes is NULL");
+  const int rc = check_table(precision, tokens, rows, cols);
+  if (rc != PACK_OK) return rc;
+  *bytes = embed_bwd_bytes(precision, tokens, rows, cols);
+  return PACK_OK;
+}
+
+int pack_embed_backward(const void* dy, int64_t ldy, const void* idx, int32_t idx64, int32_t precision, int64_t tokens,
+                        int64_t rows, int32_t cols, float scale, void* dtable_out, void* work, size_t work_bytes,
+                        hipStream_t stream) {
+  int rc = check_table(precision, tokens, rows, cols);
+  if (rc != PACK_OK) return rc;
+  if (!ld_ok(ldy, cols)) return bad("a leading dimension is smaller than cols=%d or too large", cols);
+  if (!dtable_out || (tokens > 0 && (!dy || !idx))) return bad("NULL device pointer");
+  rc = check_work(work, work_bytes, embed_bwd_bytes(precision, tokens, rows, cols));
+  if (rc != PACK_OK) return rc;
+  EmbedBwdArgs a{};
+  a.idx = idx, a.idx64 = idx64, a.dy = dy, a.ldy = ldy, a.dtable = dtable_out, a.work = work;
+  a.tokens = tokens, a.rows = rows, a.cols = cols, a.scale = scale;
+  return done("embedding backward", launch_embed_bwd(precision, a, stream));
+}
+
+int pack_quantize_blocks(const void* x, int64_t ldx, int32_t precision, int64_t rows, int32_t cols, void* q_out,
+                         int64_t ldq, float* scale_out, hipStream_t stream) {
+  BlockCodeArgs a{};
+  a.x = x, a.ldx = ldx, a.rows = rows, a.parts = 1, a.cols = cols;
+  a.q = static_cast<uint8_t*>(q_out), a.ldq = ldq, a.scale = scale_out;
+  return block_codes(false, a, precision, stream);
+}
+
+int pack_quantize_tiles(const void* x, int64_t ldx, int32_t precision, int64_t rows, int32_t parts, int32_t cols,
+                        void* q_out, int64_t ldq, float* scale_out, hipStream_t stream) {
+  BlockCodeArgs a{};
+  a.x = x, a.ldx = ldx, a.rows = rows, a.parts = parts, a.cols = cols;
+  a.q = static_cast<uint8_t*>(q_out), a.ldq = ldq, a.scale = scale_out;
+  return block_codes(true, a, precision, stream);
+}
+
+int pack_f8_matmul_workspace_size(int64_t rows, int32_t outputs, int32_t depth, int32_t gate, size_t* bytes) {
+  if (!bytes) return bad("bytes is NULL");
+  const int rc = check_f8(rows, outputs, depth, gate);
+  if (rc != PACK_OK) return rc;
+  *bytes = mm_workspace(MM_F8, mm_f8(rows, outputs, depth, gate));
+  return PACK_OK;
+}
+
+int pack_f8_matmul(const void* x, int64_t ldx, const float* x_scale, const void* w, int64_t ldw, const float* w_scale,
+                   const float* bias, int32_t gate, int32_t precision, int64_t rows, int32_t outputs, int32_t depth,
+                   void* out, int64_t ldo, void* work, size_t work_bytes, hipStream_t stream) {
+  if (!known(precision)) return bad("unknown precision %d", precision);
+  int rc = check_f8(rows, outputs, depth, gate);
+  if (rc != PACK_OK) return rc;
+  if (!ld_ok(ldx, depth) || !ld_ok(ldw, depth) || !ld_ok(ldo, outputs))
+    return bad("a leading dimension is smaller than its matrix's rows or too large");
+  if (rows == 0) return PACK_OK;
+  if (!x || !x_scale || !w || !w_scale || !out) return bad("NULL device pointer");
+  MmArgs a = mm_f8(rows, outputs, depth, gate);
+  rc = check_work(work, work_bytes, mm_workspace(MM_F8, a));
+  if (rc != PACK_OK) return rc;
+  a.A = x, a.lda = ldx, a.B = w, a.ldb = ldw, a.row_scale = x_scale, a.col_scale = w_scale, a.bias = bias;
+  a.out = out, a.ldo = ldo, a.out_f32 = precision == PACK_PREC_FP32;
+  a.work = static_cast<float*>(work), a.work_bytes = work_bytes;
+  return done("8-bit floating point product", launch_mm(MM_F8, a, stream));
 }
 
 }  // extern "C"

@@ -8,11 +8,17 @@ class probabilities and served in 8 bits.  Its parts:
   gated_ff, gated_ff_backward         y = (act(x Wg^T) * (x Wu^T)) Wd^T (+ residual), and its gradients
   q8_matmul                           product of 8-bit codes with scales per row and output, optionally gated
   add_rms_norm_q8, quantize_rows      the norm, or plain rows, as 8-bit codes with a scale per row
+  embed, embed_backward               rows of a table by index (categorical columns, tokens), and the table's gradient
+  add_layer_norm, layer_norm_backward the norm with a mean and a bias, and its gradients
+  dropout                             dropout whose mask is a function of (seed, step, site) and is never stored
+  quantize_blocks, quantize_tiles     rows and weights as 8-bit floating point codes with a scale per block of 128
+  f8_matmul                           product of those codes, optionally gated
 
 Matrices are 2-D device tensors in bfloat16 or float32 whose rows are contiguous (any row stride and alignment).
 Every call runs HIP kernels on the current stream of the tensors' device; ``PackError`` says what an argument
 breaks.  Nothing is recorded for autograd: gradients come from the backward calls, and under grad mode a tensor that
-requires a gradient is refused (``torch.no_grad()``, or the inside of an ``autograd.Function``, takes it).  Formulas and rules for empty, masked and non-finite rows are in ``include/tabpack.h``.
+requires a gradient is refused (``torch.no_grad()``, or the inside of an ``autograd.Function``, takes it).  Formulas
+and rules for empty, masked and non-finite rows are in ``include/tabpack.h``.
 """
 import ctypes
 import functools
@@ -273,6 +279,163 @@ def q8_matmul(q, scale, w, w_scale, bias=None, gate=None, dtype=torch.bfloat16):
     out = _empty(q, rows, outputs, dtype=dtype)
     work = _work(q, "pack_q8_matmul_workspace_size", rows, outputs, depth, code)
     _call("pack_q8_matmul", q, (scale, w, w_scale, bias), qp, ldq, sp, wp, ldw, wsp, bp, code, _PREC[dtype], rows,
+          outputs, depth, out.data_ptr(), outputs, None if work is None else work.data_ptr(),
+          0 if work is None else work.numel())
+    return out
+
+
+# ------------------------------------------------------------------ layer norm
+def add_layer_norm(x, weight, bias=None, residual=None, eps=1e-5):
+    """(y, v, mean, rstd): v = x + residual (x itself without one), mean and rstd = (mean (v - mean)^2 + eps)^(-1/2) per
+    row, y = (v - mean) rstd weight + bias.  x, residual [rows, cols], weight and bias fp32 [cols]; y and v in x's type,
+    mean and rstd fp32 [rows]."""
+    xp, ldx, rp, ldr, wp, prec, rows, cols = _norm_inputs(x, weight, residual)
+    bp = None if bias is None else _vector(bias, "bias", cols)
+    v = x if residual is None else _empty(x, rows, cols)
+    y = _empty(x, rows, cols)
+    mean, rstd = _empty(x, rows, dtype=torch.float32), _empty(x, rows, dtype=torch.float32)
+    _call("pack_add_layer_norm", x, (weight, bias, residual), xp, ldx, rp, ldr, wp, bp, prec, rows, cols, float(eps),
+          None if residual is None else v.data_ptr(), cols, y.data_ptr(), cols, mean.data_ptr(), rstd.data_ptr())
+    return y, v, mean, rstd
+
+
+def layer_norm_backward(dy, v, weight, mean, rstd, dv=None):
+    """(dx, dweight, dbias) of add_layer_norm: dx is the gradient of x and of the residual, dv the gradient that reaches
+    the sum v on its other path (None: none).  dx in v's type, dweight and dbias fp32."""
+    prec = _prec(v, "v")
+    vp, ldv = _matrix(v, "v")
+    yp, ldy = _matrix(dy, "dy", v.dtype, v.shape)
+    rows, cols = v.shape
+    dp, ldd = (None, 0) if dv is None else _matrix(dv, "dv", v.dtype, v.shape)
+    wp, mp, rp = _vector(weight, "weight", cols), _vector(mean, "mean", rows), _vector(rstd, "rstd", rows)
+    dx, sums = _empty(v, rows, cols), _empty(v, 2, cols, dtype=torch.float32)
+    dw, db = sums.unbind()
+    work = _empty(v, _bytes("pack_layer_norm_backward_workspace_size", rows, cols), dtype=torch.uint8)
+    _call("pack_layer_norm_backward", v, (dy, weight, mean, rstd, dv), yp, ldy, vp, ldv, wp, mp, rp, dp, ldd, prec, rows,
+          cols, dx.data_ptr(), cols, dw.data_ptr(), db.data_ptr(), work.data_ptr(), work.numel())
+    return dx, dw, db
+
+
+# --------------------------------------------------------------------- dropout
+def dropout(x, p, seed, step, site=0, residual=None):
+    """y = (residual +) x / (1 - p) where an element is kept, residual (or 0) elsewhere.  The mask follows from (seed,
+    step, site, row, column) alone, so nothing of it is kept: x's gradient is ``dropout(dy, p, seed, step, site)``.
+    x, residual [rows, cols]; p in [0, 1]; seed below 2^64; step (taken mod 2^32) a number, or a device tensor of one
+    int64, which the kernel reads when it runs: a captured graph then draws new masks at each replay; site below 2^32
+    tells the dropouts of one network apart."""
+    prec = _prec(x, "x")
+    xp, ldx = _matrix(x, "x")
+    rows, cols = x.shape
+    rp, ldr = (None, 0) if residual is None else _matrix(residual, "residual", x.dtype, x.shape)
+    if isinstance(step, torch.Tensor):
+        at, number = _vector(step.reshape(-1) if step.dim() == 0 else step, "step", 1, torch.int64), 0
+    else:
+        at, number = None, int(step) & 0xFFFFFFFFFFFFFFFF
+    if not 0 <= seed < 1 << 64:
+        _fail("seed must lie in [0, 2^64)")
+    if not 0 <= site < 1 << 32:
+        _fail("site must lie in [0, 2^32)")
+    y = _empty(x, rows, cols)
+    _call("pack_dropout", x, (residual, step if at else None), xp, ldx, rp, ldr, prec, rows, cols, float(p), int(seed),
+          number, at, int(site), y.data_ptr(), cols)
+    return y
+
+
+# ------------------------------------------------------------------ embeddings
+def _indices(idx):
+    if not (isinstance(idx, torch.Tensor) and idx.is_cuda and idx.dtype in (torch.int32, torch.int64) and idx.dim() == 1
+            and idx.is_contiguous()):
+        _fail("idx must be a contiguous 1-D device tensor of int32 or int64")
+    return idx.data_ptr(), int(idx.dtype == torch.int64), idx.shape[0]
+
+
+def embed(idx, table, scale=1.0):
+    """Rows of a table times a scale: table[idx] * scale, [tokens, cols] in the table's type.  idx [tokens] int32 or
+    int64; a negative index gives a row of zeros, one past the table a row of NaN."""
+    prec = _prec(table, "table")
+    tp, ldt = _matrix(table, "table")
+    rows, cols = table.shape
+    ip, wide, tokens = _indices(idx)
+    y = _empty(table, tokens, cols)
+    _call("pack_embed", table, (idx,), ip, wide, tp, ldt, prec, tokens, rows, cols, float(scale), y.data_ptr(), cols)
+    return y
+
+
+def embed_backward(dy, idx, rows, scale=1.0):
+    """The gradient of embed's table of ``rows`` rows from dy [tokens, cols], in dy's type: sums in fp32 and a fixed
+    order, rounded once.  Indices that are negative or past the table add to no row."""
+    prec = _prec(dy, "dy")
+    dp, ldd = _matrix(dy, "dy")
+    ip, wide, tokens = _indices(idx)
+    if dy.shape[0] != tokens:
+        _fail(f"dy must have {tokens} rows, not {dy.shape[0]}")
+    cols = dy.shape[1]
+    if not 1 <= rows < 1 << 31:
+        _fail(f"rows={rows} must lie in [1, 2^31)")
+    work = _work(dy, "pack_embed_backward_workspace_size", prec, tokens, rows, cols)
+    dtable = _empty(dy, rows, cols)
+    _call("pack_embed_backward", dy, (idx,), dp, ldd, ip, wide, prec, tokens, rows, cols, float(scale),
+          dtable.data_ptr(), None if work is None else work.data_ptr(), 0 if work is None else work.numel())
+    return dtable
+
+
+# ------------------------------------------------------- 8-bit floating point
+_E4M3 = torch.float8_e4m3fn
+_BLOCK = 128  # PACK_F8_BLOCK
+
+
+def quantize_blocks(x):
+    """(q, scale): rows as e4m3 codes (float8_e4m3fn [rows, cols]) with a scale for each 128 columns of a row (fp32
+    [ceil(cols / 128), rows], the order in which f8_matmul reads them)."""
+    prec = _prec(x, "x")
+    xp, ldx = _matrix(x, "x")
+    rows, cols = x.shape
+    q, scale = _empty(x, rows, cols, dtype=_E4M3), _empty(x, -(-cols // _BLOCK), rows, dtype=torch.float32)
+    _call("pack_quantize_blocks", x, (), xp, ldx, prec, rows, cols, q.data_ptr(), cols, scale.data_ptr())
+    return q, scale
+
+
+def quantize_tiles(w, gated=False):
+    """(q, scale): a weight [outputs, depth] as e4m3 codes with a scale for each 128 x 128 of it (fp32 [ceil(outputs /
+    128), ceil(depth / 128)]).  gated: w holds gate rows and as many up rows, whose tiles begin anew and whose scales
+    follow."""
+    prec = _prec(w, "w")
+    wp, ldw = _matrix(w, "w")
+    rows, cols = w.shape
+    parts = 2 if gated else 1
+    if rows % parts:
+        _fail("a gated w holds as many gate rows as up rows")
+    q = _empty(w, rows, cols, dtype=_E4M3)
+    scale = _empty(w, parts * -(-rows // parts // _BLOCK), -(-cols // _BLOCK), dtype=torch.float32)
+    _call("pack_quantize_tiles", w, (), wp, ldw, prec, rows // parts, parts, cols, q.data_ptr(), cols, scale.data_ptr())
+    return q, scale
+
+
+def f8_matmul(q, scale, w, w_scale, bias=None, gate=None, dtype=torch.bfloat16):
+    """x w^T (+ bias) of e4m3 codes q [rows, depth] and w [outputs, depth] with the scales of quantize_blocks and
+    quantize_tiles, sums in fp32; [rows, outputs] in ``dtype``.  gate: an activation name; w, w_scale and bias then hold
+    the gate rows and the up rows (``quantize_tiles(w, gated=True)``), and the result is act(gate) * up."""
+    qp, ldq = _matrix(q, "q", _E4M3)
+    rows, depth = q.shape
+    wp, ldw = _matrix(w, "w", _E4M3)
+    n = w.shape[0]
+    if w.shape[1] != depth:
+        _fail(f"w must have {depth} columns, not {w.shape[1]}")
+    code = -1 if gate is None else _act(gate)
+    if gate is not None and n % 2:
+        _fail("a gated w holds as many gate rows as up rows")
+    if dtype not in _PREC:
+        _fail("dtype must be bfloat16 or float32")
+    outputs, blocks = n if gate is None else n // 2, -(-depth // _BLOCK)
+    sp, _ = _matrix(scale, "scale", torch.float32, (blocks, rows))
+    tiles = -(-outputs // _BLOCK) * (1 if gate is None else 2)
+    wsp, _ = _matrix(w_scale, "w_scale", torch.float32, (tiles, blocks))
+    if not (scale.is_contiguous() and w_scale.is_contiguous()):
+        _fail("scale and w_scale must be contiguous")
+    bp = None if bias is None else _vector(bias, "bias", n)
+    out = _empty(q, rows, outputs, dtype=dtype)
+    work = _work(q, "pack_f8_matmul_workspace_size", rows, outputs, depth, code)
+    _call("pack_f8_matmul", q, (scale, w, w_scale, bias), qp, ldq, sp, wp, ldw, wsp, bp, code, _PREC[dtype], rows,
           outputs, depth, out.data_ptr(), outputs, None if work is None else work.data_ptr(),
           0 if work is None else work.numel())
     return out

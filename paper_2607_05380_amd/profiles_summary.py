@@ -36,9 +36,11 @@ EPIS = ["fwd", "fwd_eval", "dx", "dw", "ns", "de"]
 SIMPLE = ["dropout_words", "grad_sums", "head_fwd", "head_bwd", "head_train", "gather", "rows_to_bf16", "to_shadow",
           "eval_score", "dropout_mask", "select_partial", "select_pick", "select_update", "select_init", "select_final",
           "ensemble_mean", "muon_prep", "muon_norm", "muon_convert", "muon_update", "embed_table", "embed_grad",
-          "idx_check", "stream_copy", "norm_bwd", "norm_dw", "copy_rows", "rows", "distill"]
+          "idx_check", "stream_copy", "norm_bwd", "norm_dw", "copy_rows", "rows", "distill",
+          "layer_norm", "layer_norm_bwd", "layer_norm_cols", "layer_norm_sums", "dropout", "embed", "sort_one",
+          "sort_count", "sort_scan", "sort_move", "run_sum", "run_join", "row_codes", "tile_codes"]
 # kernels of the student's operators: matrix products by tiles, operand kinds and epilogue, row kernels by mode
-MM_EPIS = ["plain", "gate", "gate_bwd", "q8", "q8_gate"]
+MM_EPIS = ["plain", "gate", "gate_bwd", "q8", "q8_gate", "plain", "gate"]
 ROW_MODES = ["norm", "norm_q8", "quantize"]
 
 
@@ -86,10 +88,10 @@ def short_name(kernel):
         if epi >= len(EPIS) or ak >= len(OPS) or bk >= len(OPS):
             return None
         return f"gemm_{t}_{OPS[ak]}_{OPS[bk]}_{EPIS[epi]}"
-    m = re.search(r"\d(small|small_pair|huge|thin|join|join_pair)_kernelI(DF16b|f|a)?((?:Lb\dE)*)Li(\d)E(DF16b|f|a)?",
+    m = re.search(r"\d(small|small_pair|huge|thin|join|join_pair)_kernelI(DF16b|f|a|h|c)?((?:Lb\dE)*)Li(\d)E(DF16b|f|a|h|c)?",
                   kernel)
     if m:
-        t = {"DF16b": "bf16", "f": "f32", "a": "i8"}[m.group(2) or m.group(5)]
+        t = {"DF16b": "bf16", "f": "f32", "a": "i8", "h": "f8", "c": "f8_widened"}[m.group(2) or m.group(5)]
         ops = "" if m.group(1) != "small" and m.group(1) != "huge" else "_" + "".join(
             "kr"[int(b)] for b in re.findall(r"Lb(\d)E", m.group(3))[:2])
         # small_kernel and small_pair_kernel: 64 x 64 tiles, or 128 x 128, which the name then says

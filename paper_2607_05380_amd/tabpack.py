@@ -33,7 +33,10 @@ SYMBOLS = ["pack_last_error", "pack_init", "pack_destroy", "pack_get_hparams", "
            "pack_add_rms_norm", "pack_add_rms_norm_q8", "pack_quantize_rows",
            "pack_rms_norm_backward_workspace_size", "pack_rms_norm_backward", "pack_distill_topk",
            "pack_gated_ff_workspace_size", "pack_gated_ff_forward", "pack_gated_ff_backward",
-           "pack_q8_matmul_workspace_size", "pack_q8_matmul"]
+           "pack_q8_matmul_workspace_size", "pack_q8_matmul", "pack_add_layer_norm",
+           "pack_layer_norm_backward_workspace_size", "pack_layer_norm_backward", "pack_dropout", "pack_embed",
+           "pack_embed_backward_workspace_size", "pack_embed_backward", "pack_quantize_blocks", "pack_quantize_tiles",
+           "pack_f8_matmul_workspace_size", "pack_f8_matmul"]
 
 
 class MemberHP(ctypes.Structure):
@@ -94,7 +97,7 @@ def load_library(path=LIB_PATH):
         raise PackError(f"{path} is missing: build it first (python -m paper_2607_05380_amd.build)")
     L = ctypes.CDLL(path)
     vp, i32, i64, u64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_size_t
-    f32 = ctypes.c_float
+    f32, f64, u32 = ctypes.c_float, ctypes.c_double, ctypes.c_uint32
     H = vp
     sig = {
         "pack_last_error": ([], ctypes.c_char_p),
@@ -136,6 +139,19 @@ def load_library(path=LIB_PATH):
                                     i64, vp, vp, vp, sz, vp], ctypes.c_int),
         "pack_q8_matmul_workspace_size": ([i64, i32, i32, i32, ctypes.POINTER(sz)], ctypes.c_int),
         "pack_q8_matmul": ([vp, i64, vp, vp, i64, vp, vp, i32, i32, i64, i32, i32, vp, i64, vp, sz, vp], ctypes.c_int),
+        "pack_add_layer_norm": ([vp, i64, vp, i64, vp, vp, i32, i64, i32, f32, vp, i64, vp, i64, vp, vp, vp],
+                                ctypes.c_int),
+        "pack_layer_norm_backward_workspace_size": ([i64, i32, ctypes.POINTER(sz)], ctypes.c_int),
+        "pack_layer_norm_backward": ([vp, i64, vp, i64, vp, vp, vp, vp, i64, i32, i64, i32, vp, i64, vp, vp, vp, sz,
+                                      vp], ctypes.c_int),
+        "pack_dropout": ([vp, i64, vp, i64, i32, i64, i32, f64, u64, u64, vp, u32, vp, i64, vp], ctypes.c_int),
+        "pack_embed": ([vp, i32, vp, i64, i32, i64, i64, i32, f32, vp, i64, vp], ctypes.c_int),
+        "pack_embed_backward_workspace_size": ([i32, i64, i64, i32, ctypes.POINTER(sz)], ctypes.c_int),
+        "pack_embed_backward": ([vp, i64, vp, i32, i32, i64, i64, i32, f32, vp, vp, sz, vp], ctypes.c_int),
+        "pack_quantize_blocks": ([vp, i64, i32, i64, i32, vp, i64, vp, vp], ctypes.c_int),
+        "pack_quantize_tiles": ([vp, i64, i32, i64, i32, i32, vp, i64, vp, vp], ctypes.c_int),
+        "pack_f8_matmul_workspace_size": ([i64, i32, i32, i32, ctypes.POINTER(sz)], ctypes.c_int),
+        "pack_f8_matmul": ([vp, i64, vp, vp, i64, vp, vp, i32, i32, i64, i32, i32, vp, i64, vp, sz, vp], ctypes.c_int),
         "pack_distill_topk": ([vp, i64, i32, i64, i32, vp, vp, i32, f32, vp, vp, vp, i64, vp], ctypes.c_int),
     }
     for name, (args, res) in sig.items():
