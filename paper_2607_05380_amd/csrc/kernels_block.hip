@@ -578,7 +578,8 @@ struct Dma {
   }
   // block p of the region at `lds` with the step that starts at depth k0
   __device__ __forceinline__ void issue(char* lds, int64_t k0, int64_t kend, int p) const {
-    const uint32_t v = k0 + kofs[p] < kend ? voff[p] : kOob;
+    const int left = (int)min(kend - k0, (int64_t)1 << 30);  // of the depth
+    const uint32_t v = kofs[p] < left ? voff[p] : kOob;
     if constexpr (!RM)
       dma16(rsrc, lds + (blk0 + p) * 1024, v, (uint32_t)(k0 * ES));
     else
@@ -1042,15 +1043,19 @@ __device__ __forceinline__ void small_tile(const MmArgs& a, uint32_t block, char
 // a constant distance goes into the instruction's offset.  Depth-contiguous:
 // v[ks], row block i 4 KB on (32 rows do not change the swizzle).
 // Rows-contiguous: v[i], MFMA step ks 4 KB on.
-template <bool RM, int NI>
+// ONE: one address, from which MFMA step ks's follows (bits 5 and 6 of the
+// swizzled place are those of 2 ks, exclusive-or): fewer registers, more instructions.
+template <bool RM, int NI, bool ONE = false>
 struct FragAddr {
-  uint32_t v[RM ? NI : 4];
+  static_assert(!(RM && ONE));
+  uint32_t v[RM ? NI : ONE ? 1 : 4];
   __device__ __forceinline__ void init(const char* lds, int row0, int lane) {
     typedef __attribute__((address_space(3))) const char* lds_cptr;
     const uint32_t base = (uint32_t)(uintptr_t)(lds_cptr)lds;
     if constexpr (!RM) {
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks) v[ks] = base + kmaj16_off<4>(row0 + (lane & 31), 2 * ks + (lane >> 5));
+      for (int ks = 0; ks < (ONE ? 1 : 4); ++ks)
+        v[ks] = base + kmaj16_off<4>(row0 + (lane & 31), 2 * ks + (lane >> 5));
     } else {
       const int s = lane & 15, g = lane >> 4;
 #pragma unroll
@@ -1062,7 +1067,8 @@ struct FragAddr {
   __device__ __forceinline__ void read(bf16x8& f, uint32_t region) const {
     if constexpr (!RM) {
       u32x4 r;
-      asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(r) : "v"(v[KS] + region), "n"(I * 4096));
+      const uint32_t at = (ONE ? v[0] ^ (KS << 5) : v[KS]) + region;
+      asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(r) : "v"(at), "n"(I * 4096));
       f = __builtin_bit_cast(bf16x8, r);
     } else {
       u32x2 x, y;
@@ -1133,6 +1139,8 @@ __device__ __forceinline__ void huge_out(const MmArgs& a, const A16 (&acc)[2][2]
   }
 }
 
+__device__ __forceinline__ void tie(float (&f)[4]) { asm volatile("" : "+v"(f[0]), "+v"(f[1]), "+v"(f[2]), "+v"(f[3])); }
+
 // 256 x 256 tiles on 8 waves (2 x 4, two to a SIMD), each 128 x 64.  A K step
 // is two phases, one half (64 x 64) of the wave's sums each; a phase is a read
 // part (the half's fragments from LDS) and a product part (16 MFMAs, with the
@@ -1185,8 +1193,8 @@ __device__ __forceinline__ void huge_tile(const MmArgs& a, uint32_t block, char*
   auto ask_b = [&](int h, int step, int slot, int p) {
     lb[h].issue(smem + slot * kRegion, kbeg + (int64_t)step * KE, kend, p);
   };
-  FragAddr<RA, 2> fa;
-  FragAddr<RB, 1> fb;
+  FragAddr<RA, 2, kF8<T>> fa;
+  FragAddr<RB, 1, kF8<T>> fb;
   fa.init(smem, wm * 64, lane);
   fb.init(smem, wn * 32, lane);
   acc16 acc[2][2][2];  // [A half][32-row block][B half]
@@ -1196,6 +1204,12 @@ __device__ __forceinline__ void huge_tile(const MmArgs& a, uint32_t block, char*
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int j = 0; j < 2; ++j) clear(acc[h][i][j]);
+  // 8-bit floating point: the scales of this step, and the next one's
+  F8Scales<EPI, 4> now, next;
+  auto f8_load = [&](int kt) {
+    next.load(a, m0 + wm * 128, n0 + wn * (is_gate(EPI) ? 32 : 64), (int)(kbeg / KE) + kt, lane);
+  };
+  if constexpr (kF8<T>) f8_load(0);
 #pragma unroll
   for (int n = 0; n < 8; ++n)
 #pragma unroll
@@ -1206,17 +1220,16 @@ __device__ __forceinline__ void huge_tile(const MmArgs& a, uint32_t block, char*
         ask_b(n % 4 == 2, n / 4, n, p);
     }
   wait_vm<10, false>();
+  if constexpr (kF8<T>) {
+    tie(next.row);
+    now = next;
+  }
   bar();
   if (wm == 1) bar();
   bf16x8 x0[4], x1[4], y0[4], y1[4];  // A row blocks 0 and 1 of the half; B halves
   // end of a phase's reads, and its products
-  // 8-bit floating point: the scales of this phase's half of the rows, and the next one's
-  F8Scales<EPI, 2> now, next;
-  auto f8_load = [&](int kt, int h) {
-    next.load(a, m0 + wm * 128 + h * 64, n0 + wn * (is_gate(EPI) ? 32 : 64), (int)(kbeg / KE) + kt, lane);
-  };
-  if constexpr (kF8<T>) f8_load(0, 0);
-  auto products = [&](acc16 (&c)[2][2], auto vm, auto ask) {
+  auto products = [&](acc16 (&c)[2][2], auto which, auto vm, auto ask) {
+    constexpr int half = decltype(which)::value;
     __builtin_amdgcn_sched_barrier(0);
     wait_vm<decltype(vm)::value, false>();
     bar();
@@ -1245,7 +1258,7 @@ __device__ __forceinline__ void huge_tile(const MmArgs& a, uint32_t block, char*
         }
         if (b > 0) {
           const int i = (b - 1) & 1, j = (b - 1) >> 1;
-          const float s = now.row[i] * now.lo(j);
+          const float s = now.row[2 * half + i] * now.lo(j);
           add_scaled(c[i][j], t[(b - 1) & 1], s, s);
           __builtin_amdgcn_sched_barrier(0);
         }
@@ -1270,33 +1283,32 @@ __device__ __forceinline__ void huge_tile(const MmArgs& a, uint32_t block, char*
   auto after = [](int sl, int n) { return sl + n < SLOTS ? sl + n : sl + n - SLOTS; };
 #pragma unroll 1
   for (int kt = 0; kt < nk; ++kt) {
-    if constexpr (kF8<T>) {
-      now = next;
-      f8_load(kt, 1);
-    }
+    if constexpr (kF8<T>) f8_load(kt + 1);
     fa.template read4<0>(x0, slot * kRegion);
     fa.template read4<1>(x1, slot * kRegion);
     fb.template read4<0>(y0, after(slot, 1) * kRegion);
     fb.template read4<0>(y1, after(slot, 2) * kRegion);
-    products(acc[0], std::integral_constant<int, 8>{}, [&](int q) {
+    products(acc[0], std::integral_constant<int, 0>{}, std::integral_constant<int, kF8<T> ? 12 : 8>{}, [&](int q) {
       if (q < 2)
         ask_a(0, kt + 2, after(slot, 8), q);
       else
         ask_b(0, kt + 2, after(slot, 9), q - 2);
     });
-    if constexpr (kF8<T>) {
-      now = next;
-      f8_load(kt + 1, 0);
-    }
     fa.template read4<0>(x0, after(slot, 3) * kRegion);
     fa.template read4<1>(x1, after(slot, 3) * kRegion);
-    products(acc[1], std::integral_constant<int, 6>{}, [&](int q) {
+    products(acc[1], std::integral_constant<int, 1>{}, std::integral_constant<int, kF8<T> ? 10 : 6>{}, [&](int q) {
       if (q < 2)
         ask_b(1, kt + 2, slot, q);
       else
         ask_a(1, kt + 2, after(slot, 1), q - 2);
     });
     slot = after(slot, 4);
+    if constexpr (kF8<T>) {
+      // (used here, so that the compiler's wait for them counts this step's loads
+      // behind them; a use in the next step waited for the regions' too)
+      tie(next.row);
+      now = next;
+    }
   }
   if (wm == 0) bar();
   wait_vm<0, true>();
@@ -1334,7 +1346,7 @@ __global__ __launch_bounds__(256, NB * NS == 4 ? 2 : 4) void small_pair_kernel(M
 }
 template <typename T, bool RA, bool RB, int EPI>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void huge_kernel(MmArgs a) {
-  __shared__ __attribute__((aligned(16))) char smem[kHugeSlots * kRegion];
+  __shared__ __attribute__((aligned(128))) char smem[kHugeSlots * kRegion];
   huge_tile<T, RA, RB, EPI>(a, blockIdx.x, smem);
 }
 // -------------------------------------------------------------- thin tiles --

@@ -120,16 +120,17 @@ __device__ __forceinline__ uint32_t exclusive_sum(uint32_t v, uint32_t* waves, i
   return before;
 }
 
-// Zeros over the table by block `block` of `blocks` of NT threads.
+// Zeros over part `part` of `parts` of the table, by block `block` of `blocks` of NT threads.
 template <typename T, int NT>
-__device__ __forceinline__ void fill(const EmbedBwdArgs& a, uint32_t block, uint32_t blocks) {
+__device__ __forceinline__ void fill(const EmbedBwdArgs& a, uint32_t block, uint32_t blocks, int part = 0,
+                                     int parts = 1) {
   constexpr int VE = kVec<T>;
-  const int64_t n = a.rows * a.cols;
+  const int64_t each = (a.rows * a.cols / parts / VE + 1) * VE, n = min(a.rows * a.cols, (part + 1) * each);
   T* const p = static_cast<T*>(a.dtable);
   float zero[VE];
 #pragma unroll
   for (int e = 0; e < VE; ++e) zero[e] = 0.0f;
-  for (int64_t i = ((int64_t)block * NT + threadIdx.x) * VE; i < n; i += (int64_t)blocks * NT * VE)
+  for (int64_t i = part * each + ((int64_t)block * NT + threadIdx.x) * VE; i < n; i += (int64_t)blocks * NT * VE)
     store_vec(p + i, zero, (int)(n - i < VE ? n - i : VE));
 }
 
@@ -189,49 +190,58 @@ __global__ __launch_bounds__(1024) void sort_one_kernel(EmbedBwdArgs a, uint32_t
   }
 }
 
-// Longer lists, one digit of DB bits: blocks of kSortTile tokens.
-constexpr int kSortTile = 4096, kSortItems = kSortTile / 256;
+// Longer lists, one digit of DB bits a launch: blocks of 256 IPT tokens.  The
+// first launch counts each block's first digits.  A move knows where every token
+// goes, so it also counts the next digits of the blocks that it moves them to
+// (whole numbers: the order of these additions does not matter).  Up to kDirect
+// blocks a move adds up the counts of the blocks before its own by itself, past
+// that a launch between them does.  The blocks behind the sort's write zeros.
+constexpr uint32_t kDirect = 64;
 struct SortArgs {
-  const uint32_t* keys;    // NULL in the first round: from the indices
+  const uint32_t* keys;
   const uint32_t* places;
   uint32_t* keys_out;
   uint32_t* places_out;
-  uint32_t* counts;        // [digits, blocks]: of each block; then the places before it
-  uint32_t* totals;        // [digits]
+  uint32_t* counts;        // [digits, blocks] of each block; behind a scan: of the blocks before it
+  uint32_t* next;          // the same of the next digit, or NULL
+  uint32_t* totals;        // [digits] (with a scan)
   uint32_t blocks;
-  int shift;
+  int shift, round, rounds;
 };
-__device__ __forceinline__ uint32_t sort_key(const EmbedBwdArgs& a, const SortArgs& s, int64_t i) {
-  return i >= a.tokens ? kNoKey : s.keys ? s.keys[i] : key_of(a, i);
-}
-template <typename T, int DB>
+template <typename T, int DB, int IPT>
 __global__ __launch_bounds__(256) void sort_count_kernel(EmbedBwdArgs a, SortArgs s) {
   __shared__ uint32_t count[1 << DB];
   if (blockIdx.x >= s.blocks) {
-    fill<T, 256>(a, blockIdx.x - s.blocks, gridDim.x - s.blocks);
+    fill<T, 256>(a, blockIdx.x - s.blocks, gridDim.x - s.blocks, 0, s.rounds + 1);
     return;
   }
   for (int d = threadIdx.x; d < 1 << DB; d += 256) count[d] = 0;
   __syncthreads();
-  const int64_t first = (int64_t)blockIdx.x * kSortTile + threadIdx.x;
+  const int64_t first = (int64_t)blockIdx.x * (256 * IPT) + threadIdx.x;
+  uint32_t key[IPT];
 #pragma unroll
-  for (int j = 0; j < kSortItems; ++j) {
+  for (int j = 0; j < IPT; ++j) {
     const int64_t i = first + 256 * j;
-    if (i < a.tokens) atomicAdd(&count[(sort_key(a, s, i) >> s.shift) & ((1 << DB) - 1)], 1u);  // (whole numbers)
+    key[j] = i < a.tokens ? key_of(a, i) : kNoKey;
   }
+#pragma unroll
+  for (int j = 0; j < IPT; ++j)
+    if (first + 256 * j < a.tokens) atomicAdd(&count[key[j] & ((1 << DB) - 1)], 1u);
   __syncthreads();
-  for (int d = threadIdx.x; d < 1 << DB; d += 256) s.counts[(int64_t)d * s.blocks + blockIdx.x] = count[d];
+  for (int d = threadIdx.x; d < 1 << DB; d += 256) {
+    s.counts[(int64_t)d * s.blocks + blockIdx.x] = count[d];
+    for (int r = 1; r < s.rounds; ++r) s.counts[(((int64_t)r << DB) + d) * s.blocks + blockIdx.x] = 0;
+  }
 }
-// A block: one digit's counts over the blocks of tokens, to the places before each.
+// A block: one digit's counts over the blocks of tokens, to those of the blocks before each.
 __global__ __launch_bounds__(256) void sort_scan_kernel(SortArgs s) {
-  __shared__ uint32_t waves[4];
+  __shared__ uint32_t waves[4], last;
   uint32_t* const c = s.counts + (int64_t)blockIdx.x * s.blocks;
   uint32_t carry = 0;
   for (uint32_t base = 0; base < s.blocks; base += 256) {
     const uint32_t i = base + threadIdx.x, v = i < s.blocks ? c[i] : 0;
     const uint32_t before = exclusive_sum<256>(v, waves, threadIdx.x);
     if (i < s.blocks) c[i] = carry + before;
-    __shared__ uint32_t last;
     if (threadIdx.x == 255) last = before + v;
     __syncthreads();
     carry += last;
@@ -239,46 +249,67 @@ __global__ __launch_bounds__(256) void sort_scan_kernel(SortArgs s) {
   }
   if (threadIdx.x == 0) s.totals[blockIdx.x] = carry;
 }
-template <int DB>
+template <typename T, int DB, int IPT, bool DIRECT>
 __global__ __launch_bounds__(256) void sort_move_kernel(EmbedBwdArgs a, SortArgs s) {
   constexpr int D = 1 << DB, PER = D / 256;
   __shared__ uint32_t count[4][D], waves[4];
+  if (blockIdx.x >= s.blocks) {
+    fill<T, 256>(a, blockIdx.x - s.blocks, gridDim.x - s.blocks, s.round + 1, s.rounds + 1);
+    return;
+  }
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   for (int i = tid; i < 4 * D; i += 256) count[i / D][i % D] = 0;
-  __syncthreads();
-  const int64_t first = (int64_t)blockIdx.x * kSortTile + wave * (64 * kSortItems) + lane;
-  uint32_t key[kSortItems], rank[kSortItems];
+  const int64_t first = (int64_t)blockIdx.x * (256 * IPT) + wave * (64 * IPT) + lane;
+  uint32_t key[IPT], place[IPT], rank[IPT];
 #pragma unroll
-  for (int j = 0; j < kSortItems; ++j) key[j] = sort_key(a, s, first + 64 * j);
-#pragma unroll
-  for (int j = 0; j < kSortItems; ++j) rank[j] = rank_digit<DB>((key[j] >> s.shift) & (D - 1), count[wave], lane);
-  // a thread's PER digits: tokens of lower digits, then those of the blocks before, then of the waves before
-  uint32_t total[PER], sum = 0;
+  for (int j = 0; j < IPT; ++j) {
+    const int64_t i = first + 64 * j;
+    const bool in = i < a.tokens;
+    key[j] = !in ? kNoKey : s.round ? s.keys[i] : key_of(a, i);
+    place[j] = !in ? 0 : s.round ? s.places[i] : (uint32_t)i;
+  }
+  // a thread's PER digits: tokens with the digit, and those of the blocks before
+  uint32_t total[PER], before[PER], sum = 0;
 #pragma unroll
   for (int q = 0; q < PER; ++q) {
-    total[q] = s.totals[tid * PER + q];
+    const uint32_t* const c = s.counts + (int64_t)(tid * PER + q) * s.blocks;
+    if constexpr (DIRECT) {
+      total[q] = before[q] = 0;
+#pragma unroll 8
+      for (uint32_t b = 0; b < s.blocks; ++b) {
+        const uint32_t n = c[b];
+        total[q] += n;
+        before[q] += b < blockIdx.x ? n : 0;
+      }
+    } else {
+      total[q] = s.totals[tid * PER + q];
+      before[q] = c[blockIdx.x];
+    }
     sum += total[q];
   }
-  uint32_t before = exclusive_sum<256>(sum, waves, tid);  // (its barriers stand behind the ranks)
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < IPT; ++j) rank[j] = rank_digit<DB>((key[j] >> s.shift) & (D - 1), count[wave], lane);
+  // where each wave's first token of a digit goes: behind the lower digits, the blocks and the waves before
+  uint32_t lower = exclusive_sum<256>(sum, waves, tid);  // (its barriers stand behind the ranks)
 #pragma unroll
   for (int q = 0; q < PER; ++q) {
-    const int d = tid * PER + q;
-    uint32_t at = before + s.counts[(int64_t)d * s.blocks + blockIdx.x];
-    before += total[q];
+    uint32_t at = lower + before[q];
+    lower += total[q];
     for (int w = 0; w < 4; ++w) {
-      const uint32_t c = count[w][d];
-      count[w][d] = at;
+      const uint32_t c = count[w][tid * PER + q];
+      count[w][tid * PER + q] = at;
       at += c;
     }
   }
   __syncthreads();
 #pragma unroll
-  for (int j = 0; j < kSortItems; ++j) {
-    const int64_t i = first + 64 * j;
-    if (i >= a.tokens) continue;
+  for (int j = 0; j < IPT; ++j) {
+    if (first + 64 * j >= a.tokens) continue;
     const uint32_t to = count[wave][(key[j] >> s.shift) & (D - 1)] + rank[j];
     s.keys_out[to] = key[j];
-    s.places_out[to] = s.keys ? s.places[i] : (uint32_t)i;
+    s.places_out[to] = place[j];
+    if (s.next) atomicAdd(&s.next[(int64_t)((key[j] >> (s.shift + DB)) & (D - 1)) * s.blocks + to / (256 * IPT)], 1u);
   }
 }
 
@@ -317,28 +348,37 @@ __global__ __launch_bounds__(256) void run_sum_kernel(EmbedBwdArgs a, SumArgs s)
   float acc[VE];
 #pragma unroll
   for (int e = 0; e < VE; ++e) acc[e] = 0.0f;
+  uint32_t key[U], place[U];  // of the next U tokens
+  auto ask = [&](int64_t i) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t at = min(i + u, i1 - 1);
+      key[u] = s.keys[at];
+      place[u] = s.places[at];
+    }
+  };
+  ask(i0);
   for (int64_t i = i0; i < i1; i += U) {
-    uint32_t key[U];
+    uint32_t now[U];
     Vec<T> v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t at = i + u;
-      key[u] = at < i1 ? s.keys[at] : kNoKey;
+      now[u] = key[u];
       // (tokens that add to no row are not read)
-      v[u].load(static_cast<const T*>(a.dy) + (key[u] < a.rows ? (int64_t)s.places[at] * a.ldy : 0) + c,
-                key[u] < a.rows ? n : 0);
+      v[u].load(static_cast<const T*>(a.dy) + (int64_t)place[u] * a.ldy + c, key[u] < a.rows ? n : 0);
     }
+    if (i + U < i1) ask(i + U);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (i + u >= i1) break;
-      if (key[u] != cur) {
+      if (now[u] != cur) {
         if (begun) {
 #pragma unroll
           for (int e = 0; e < VE; ++e) partial[e] = acc[e];
         } else {
           write_row<T>(a, cur, c, acc);
         }
-        cur = key[u];
+        cur = now[u];
         begun = false;
 #pragma unroll
         for (int e = 0; e < VE; ++e) acc[e] = 0.0f;
@@ -378,9 +418,26 @@ __global__ __launch_bounds__(256) void run_join_kernel(EmbedBwdArgs a, SumArgs s
 #pragma unroll
       for (int e = 0; e < VE; ++e) acc[e] = s.partial[(chunk * 2 + 1) * s.ldp + c + e];
     }
-    for (int64_t b = chunk + 1 + group; b * s.chunk < a.tokens && s.keys[b * s.chunk] == key; b += groups) {
+    // the next B chunks' first keys and sums are asked for together
+    constexpr int B = 8;
+    bool more = true;
+    for (int64_t b0 = chunk + 1 + group; more; b0 += (int64_t)B * groups) {
+      bool goes[B];
+      f32x4 v[B][VE / 4];
 #pragma unroll
-      for (int e = 0; e < VE; ++e) acc[e] += s.partial[b * 2 * s.ldp + c + e];
+      for (int u = 0; u < B; ++u) {
+        const int64_t b = min(b0 + (int64_t)u * groups, (int64_t)s.chunks - 1);
+        goes[u] = b0 + (int64_t)u * groups < s.chunks && s.keys[b * s.chunk] == key;
+#pragma unroll
+        for (int q = 0; q < VE / 4; ++q)
+          v[u][q] = *reinterpret_cast<const f32x4*>(s.partial + b * 2 * s.ldp + c + 4 * q);
+      }
+#pragma unroll
+      for (int u = 0; u < B; ++u) {
+#pragma unroll
+        for (int e = 0; e < VE; ++e) acc[e] += goes[u] ? v[u][e / 4][e % 4] : 0.0f;
+      }
+      more = goes[B - 1];
     }
   }
 #pragma unroll
@@ -395,14 +452,15 @@ __global__ __launch_bounds__(256) void run_join_kernel(EmbedBwdArgs a, SumArgs s
 }
 
 // ------------------------------------------------------------------- host --
-constexpr int64_t kSortOne = 16384;  // tokens that one workgroup sorts
+constexpr int64_t kSortOne = 4096;  // tokens that one workgroup sorts
 
 int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
 // How a gradient is laid out over launches, and its workspace.
 struct BwdPlan {
   int bits, digit, rounds;  // of the keys, of a digit, digits
-  uint32_t blocks;          // of tokens in the long sort
+  int items;                // tokens a thread of the long sort
+  uint32_t blocks;          // of tokens in it
   SumArgs sum;
   size_t keys, counts, totals, partial, bytes;  // byte offsets
 };
@@ -411,23 +469,24 @@ BwdPlan plan(int prec, int64_t tokens, int64_t rows, int32_t cols) {
   const int ve = prec == PACK_PREC_BF16 ? 8 : 4;
   while (p.bits < 32 && (rows >> p.bits) > 0) ++p.bits;  // keys 0 .. rows
   const bool one = tokens <= kSortOne;
+  p.items = tokens <= 256 * (int64_t)kDirect ? 1 : 4;
+  p.blocks = one ? 0 : (uint32_t)((tokens + 256 * p.items - 1) / (256 * p.items));
   // digits of 8 bits, or of 11 where that saves a round
-  p.digit = !one && (p.bits + 10) / 11 < (p.bits + 7) / 8 ? 11 : 8;
+  p.digit = p.items > 1 && (p.bits + 10) / 11 < (p.bits + 7) / 8 ? 11 : 8;
   p.rounds = (p.bits + p.digit - 1) / p.digit;
-  p.blocks = one ? 0 : (uint32_t)((tokens + kSortTile - 1) / kSortTile);
   const int64_t vectors = ((int64_t)cols + ve - 1) / ve;
   while (p.sum.g < 6 && ((int64_t)1 << p.sum.g) < vectors) ++p.sum.g;
   p.sum.columns = (int)((vectors + (1 << p.sum.g) - 1) >> p.sum.g);
-  // chunks for some 2048 waves, of 16 to 1024 tokens
+  // chunks for some 4096 waves, of 16 to 1024 tokens
   int64_t chunk = 16;
-  while (chunk < 1024 && tokens * p.sum.columns * (1 << p.sum.g) / 64 > 2048 * chunk) chunk *= 2;
+  while (chunk < 1024 && tokens * p.sum.columns * (1 << p.sum.g) / 64 > 4096 * chunk) chunk *= 2;
   p.sum.chunk = (int)chunk;
   p.sum.chunks = (int)((tokens + chunk - 1) / chunk);
   p.sum.ldp = vectors * ve;
   p.keys = 0;
   size_t at = (size_t)up(tokens * 4, 16) * (one ? 2 : 4);
   p.counts = at;
-  at += one ? 0 : (size_t)up(((int64_t)p.blocks << p.digit) * 4, 16);
+  at += (size_t)up(((int64_t)p.blocks << p.digit) * p.rounds * 4, 16);
   p.totals = at;
   at += one ? 0 : ((size_t)4 << p.digit);
   p.partial = at;
@@ -436,16 +495,25 @@ BwdPlan plan(int prec, int64_t tokens, int64_t rows, int32_t cols) {
   return p;
 }
 
-template <typename T, int DB>
+template <typename T, int DB, int IPT>
 hipError_t sort_long(const EmbedBwdArgs& a, const BwdPlan& p, SortArgs s, uint32_t* (&buf)[2][2], uint32_t zeros,
                      hipStream_t st) {
+  const dim3 grid(p.blocks + zeros), block(256);
+  uint32_t* const counts = s.counts;
+  s.rounds = p.rounds;
+  hipLaunchKernelGGL((sort_count_kernel<T, DB, IPT>), grid, block, 0, st, a, s);
   for (int r = 0; r < p.rounds; ++r) {
-    s.keys = r ? buf[(r + 1) & 1][0] : nullptr, s.places = r ? buf[(r + 1) & 1][1] : nullptr;
+    s.round = r, s.shift = r * DB;
+    s.keys = buf[(r + 1) & 1][0], s.places = buf[(r + 1) & 1][1];
     s.keys_out = buf[r & 1][0], s.places_out = buf[r & 1][1];
-    s.shift = r * DB;
-    hipLaunchKernelGGL((sort_count_kernel<T, DB>), dim3(p.blocks + (r ? 0 : zeros)), dim3(256), 0, st, a, s);
-    hipLaunchKernelGGL(sort_scan_kernel, dim3(1 << DB), dim3(256), 0, st, s);
-    hipLaunchKernelGGL((sort_move_kernel<DB>), dim3(p.blocks), dim3(256), 0, st, a, s);
+    s.counts = counts + (((int64_t)r << DB) * p.blocks);
+    s.next = r + 1 < p.rounds ? counts + (((int64_t)(r + 1) << DB) * p.blocks) : nullptr;
+    if (p.blocks <= kDirect) {
+      hipLaunchKernelGGL((sort_move_kernel<T, DB, IPT, true>), grid, block, 0, st, a, s);
+    } else if constexpr (IPT > 1) {
+      hipLaunchKernelGGL(sort_scan_kernel, dim3(1 << DB), block, 0, st, s);
+      hipLaunchKernelGGL((sort_move_kernel<T, DB, IPT, false>), grid, block, 0, st, a, s);
+    }
   }
   return hipGetLastError();
 }
@@ -458,25 +526,26 @@ hipError_t embed_bwd_t(int prec, const EmbedBwdArgs& a, hipStream_t st) {
   const int64_t list = up(a.tokens * 4, 16);
   uint32_t* buf[2][2];
   for (int i = 0; i < 4; ++i) buf[i / 2][i % 2] = reinterpret_cast<uint32_t*>(w + p.keys + i * list);
-  // blocks that write zeros beside the sort: 64 KB each or more, up to four a CU
+  // blocks that write zeros beside the sort: 16 KB each a launch or more, up to four a CU
   const int64_t bytes = a.rows * a.cols * (int64_t)sizeof(T);
-  const uint32_t zeros = (uint32_t)std::min<int64_t>((bytes + 65535) / 65536, 1024);
   hipError_t e;
   int last = 0;  // the buffer that holds the sorted list
   if (a.tokens <= kSortOne) {
-    const dim3 grid(1 + std::min(zeros, 256u)), block(1024);
+    const dim3 grid(1 + (uint32_t)std::min<int64_t>((bytes + 65535) / 65536, 512)), block(1024);
     if (a.tokens <= 1024)
       hipLaunchKernelGGL((sort_one_kernel<T, 1>), grid, block, 0, st, a, buf[0][0], buf[0][1], p.bits);
-    else if (a.tokens <= 4096)
-      hipLaunchKernelGGL((sort_one_kernel<T, 4>), grid, block, 0, st, a, buf[0][0], buf[0][1], p.bits);
     else
-      hipLaunchKernelGGL((sort_one_kernel<T, 16>), grid, block, 0, st, a, buf[0][0], buf[0][1], p.bits);
+      hipLaunchKernelGGL((sort_one_kernel<T, 4>), grid, block, 0, st, a, buf[0][0], buf[0][1], p.bits);
     e = hipGetLastError();
   } else {
+    const uint32_t zeros = (uint32_t)std::min<int64_t>((bytes / (p.rounds + 1) + 16383) / 16384, 1024);
     SortArgs s{};
     s.counts = reinterpret_cast<uint32_t*>(w + p.counts), s.totals = reinterpret_cast<uint32_t*>(w + p.totals);
     s.blocks = p.blocks;
-    e = p.digit == 8 ? sort_long<T, 8>(a, p, s, buf, zeros, st) : sort_long<T, 11>(a, p, s, buf, zeros, st);
+    if (p.digit == 11)
+      e = sort_long<T, 11, 4>(a, p, s, buf, zeros, st);
+    else
+      e = p.items == 1 ? sort_long<T, 8, 1>(a, p, s, buf, zeros, st) : sort_long<T, 8, 4>(a, p, s, buf, zeros, st);
     last = (p.rounds + 1) & 1;
   }
   if (e != hipSuccess || a.tokens == 0) return e;
