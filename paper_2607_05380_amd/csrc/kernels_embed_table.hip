@@ -71,6 +71,11 @@ hipError_t embed_t(const EmbedArgs& a, hipStream_t s) {
 // ------------------------------------------------------------------- sort --
 constexpr uint32_t kNoKey = 0xffffffffu;  // places behind the last token: after every key
 
+// A token of the list: its key, and its place in the batch (one store moves both).
+struct alignas(8) Token {
+  uint32_t key, place;
+};
+
 // A token's key: its row, or `rows` for one that adds to none.
 __device__ __forceinline__ uint32_t key_of(const EmbedBwdArgs& a, int64_t t) {
   const int64_t r = row_of(a.idx, a.idx64, t, a.rows);
@@ -84,8 +89,8 @@ __device__ __forceinline__ void wave_order() {
 
 // The wave's next 64 keys' digits d: how many of the wave's keys before this one
 // have it.  count: the wave's counts, 1 << DB.
-template <int DB>
-__device__ __forceinline__ uint32_t rank_digit(uint32_t d, uint32_t* count, int lane) {
+template <int DB, typename C>
+__device__ __forceinline__ uint32_t rank_digit(uint32_t d, C* count, int lane) {
   uint64_t same = ~0ull;
 #pragma unroll
   for (int b = 0; b < DB; ++b) {
@@ -96,7 +101,7 @@ __device__ __forceinline__ uint32_t rank_digit(uint32_t d, uint32_t* count, int 
   const uint32_t before = (uint32_t)__popcll(same & ((1ull << lane) - 1));
   const uint32_t base = count[d];
   wave_order();
-  if (before == 0) count[d] = base + (uint32_t)__popcll(same);
+  if (before == 0) count[d] = (C)(base + (uint32_t)__popcll(same));
   wave_order();
   return base + before;
 }
@@ -136,7 +141,7 @@ __device__ __forceinline__ void fill(const EmbedBwdArgs& a, uint32_t block, uint
 
 // Up to 1024 IPT tokens in one workgroup (block 0; the others write zeros).
 template <typename T, int IPT>
-__global__ __launch_bounds__(1024) void sort_one_kernel(EmbedBwdArgs a, uint32_t* keys, uint32_t* places, int bits) {
+__global__ __launch_bounds__(1024) void sort_one_kernel(EmbedBwdArgs a, Token* list, int bits) {
   __shared__ uint32_t lds_key[1024 * IPT], lds_place[1024 * IPT], count[16][256], waves[4];
   if (blockIdx.x > 0) {
     fill<T, 1024>(a, blockIdx.x - 1, gridDim.x - 1);
@@ -186,52 +191,48 @@ __global__ __launch_bounds__(1024) void sort_one_kernel(EmbedBwdArgs a, uint32_t
 #pragma unroll
   for (int j = 0; j < IPT; ++j) {
     const int i = first + 64 * j;
-    if (i < n) keys[i] = key[j], places[i] = place[j];
+    if (i < n) list[i] = Token{key[j], place[j]};
   }
 }
 
-// Longer lists, one digit of DB bits a launch: blocks of 256 IPT tokens.  The
-// first launch counts each block's first digits.  A move knows where every token
-// goes, so it also counts the next digits of the blocks that it moves them to
-// (whole numbers: the order of these additions does not matter).  Up to kDirect
-// blocks a move adds up the counts of the blocks before its own by itself, past
-// that a launch between them does.  The blocks behind the sort's write zeros.
+// Longer lists, a digit of DB bits in two launches or three: blocks of NT IPT
+// tokens count theirs, then move them.  Up to kDirect blocks a move adds up the
+// counts of the blocks before its own by itself, past that a launch between them
+// does.  The blocks behind the sort's write zeros.  What bounds the moves of a long
+// list is its scattered stores: larger blocks have longer runs of a digit.
 constexpr uint32_t kDirect = 64;
 struct SortArgs {
-  const uint32_t* keys;
-  const uint32_t* places;
-  uint32_t* keys_out;
-  uint32_t* places_out;
-  uint32_t* counts;        // [digits, blocks] of each block; behind a scan: of the blocks before it
-  uint32_t* next;          // the same of the next digit, or NULL
-  uint32_t* totals;        // [digits] (with a scan)
+  const Token* list;
+  Token* out;
+  uint32_t* counts;  // up to kDirect blocks [blocks, digits], past that [digits, blocks]; behind a scan: those before
+  uint32_t* totals;  // [digits] (with a scan)
   uint32_t blocks;
-  int shift, round, rounds;
+  int shift, round, launch, launches;  // (launches: those that write zeros)
 };
-template <typename T, int DB, int IPT>
-__global__ __launch_bounds__(256) void sort_count_kernel(EmbedBwdArgs a, SortArgs s) {
+__device__ __forceinline__ Token sort_token(const EmbedBwdArgs& a, const SortArgs& s, int64_t i) {
+  if (i >= a.tokens) return Token{kNoKey, 0};
+  return s.round ? s.list[i] : Token{key_of(a, i), (uint32_t)i};
+}
+template <typename T, int DB, int NT, int IPT>
+__global__ __launch_bounds__(NT) void sort_count_kernel(EmbedBwdArgs a, SortArgs s) {
   __shared__ uint32_t count[1 << DB];
   if (blockIdx.x >= s.blocks) {
-    fill<T, 256>(a, blockIdx.x - s.blocks, gridDim.x - s.blocks, 0, s.rounds + 1);
+    fill<T, NT>(a, blockIdx.x - s.blocks, gridDim.x - s.blocks, s.launch, s.launches);
     return;
   }
-  for (int d = threadIdx.x; d < 1 << DB; d += 256) count[d] = 0;
+  for (int d = threadIdx.x; d < 1 << DB; d += NT) count[d] = 0;
   __syncthreads();
-  const int64_t first = (int64_t)blockIdx.x * (256 * IPT) + threadIdx.x;
+  const int64_t first = (int64_t)blockIdx.x * (NT * IPT) + threadIdx.x;
   uint32_t key[IPT];
 #pragma unroll
-  for (int j = 0; j < IPT; ++j) {
-    const int64_t i = first + 256 * j;
-    key[j] = i < a.tokens ? key_of(a, i) : kNoKey;
-  }
+  for (int j = 0; j < IPT; ++j) key[j] = sort_token(a, s, first + NT * j).key;
 #pragma unroll
-  for (int j = 0; j < IPT; ++j)
-    if (first + 256 * j < a.tokens) atomicAdd(&count[key[j] & ((1 << DB) - 1)], 1u);
+  for (int j = 0; j < IPT; ++j)  // (whole numbers: the order of these additions does not matter)
+    if (first + NT * j < a.tokens) atomicAdd(&count[(key[j] >> s.shift) & ((1 << DB) - 1)], 1u);
   __syncthreads();
-  for (int d = threadIdx.x; d < 1 << DB; d += 256) {
-    s.counts[(int64_t)d * s.blocks + blockIdx.x] = count[d];
-    for (int r = 1; r < s.rounds; ++r) s.counts[(((int64_t)r << DB) + d) * s.blocks + blockIdx.x] = 0;
-  }
+  // (in the order in which a move, or the scan, reads them)
+  const int64_t of_digit = s.blocks <= kDirect ? 1 : s.blocks, of_block = s.blocks <= kDirect ? 1 << DB : 1;
+  for (int d = threadIdx.x; d < 1 << DB; d += NT) s.counts[d * of_digit + blockIdx.x * of_block] = count[d];
 }
 // A block: one digit's counts over the blocks of tokens, to those of the blocks before each.
 __global__ __launch_bounds__(256) void sort_scan_kernel(SortArgs s) {
@@ -249,78 +250,105 @@ __global__ __launch_bounds__(256) void sort_scan_kernel(SortArgs s) {
   }
   if (threadIdx.x == 0) s.totals[blockIdx.x] = carry;
 }
-template <typename T, int DB, int IPT, bool DIRECT>
-__global__ __launch_bounds__(256) void sort_move_kernel(EmbedBwdArgs a, SortArgs s) {
-  constexpr int D = 1 << DB, PER = D / 256;
-  __shared__ uint32_t count[4][D], waves[4];
+template <typename T, int DB, int NT, int IPT, bool DIRECT>
+__global__ __launch_bounds__(NT) void sort_move_kernel(EmbedBwdArgs a, SortArgs s) {
+  constexpr int D = 1 << DB, W = NT / 64, PER = D / NT > 0 ? D / NT : 1;
+  __shared__ __attribute__((aligned(16))) uint16_t count[W][D];  // of each wave, at most 64 IPT
+  __shared__ uint32_t base[D], waves[W];
   if (blockIdx.x >= s.blocks) {
-    fill<T, 256>(a, blockIdx.x - s.blocks, gridDim.x - s.blocks, s.round + 1, s.rounds + 1);
+    fill<T, NT>(a, blockIdx.x - s.blocks, gridDim.x - s.blocks, s.launch, s.launches);
     return;
   }
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  for (int i = tid; i < 4 * D; i += 256) count[i / D][i % D] = 0;
-  const int64_t first = (int64_t)blockIdx.x * (256 * IPT) + wave * (64 * IPT) + lane;
-  uint32_t key[IPT], place[IPT], rank[IPT];
+  for (int i = tid; i < W * D / 2; i += NT) reinterpret_cast<uint32_t*>(&count[0][0])[i] = 0;
+  const int64_t first = (int64_t)blockIdx.x * (NT * IPT) + wave * (64 * IPT) + lane;
+  Token token[IPT];
+  uint32_t rank[IPT];
 #pragma unroll
-  for (int j = 0; j < IPT; ++j) {
-    const int64_t i = first + 64 * j;
-    const bool in = i < a.tokens;
-    key[j] = !in ? kNoKey : s.round ? s.keys[i] : key_of(a, i);
-    place[j] = !in ? 0 : s.round ? s.places[i] : (uint32_t)i;
-  }
+  for (int j = 0; j < IPT; ++j) token[j] = sort_token(a, s, first + 64 * j);
   // a thread's PER digits: tokens with the digit, and those of the blocks before
   uint32_t total[PER], before[PER], sum = 0;
+  const bool has = tid * PER < D;
 #pragma unroll
   for (int q = 0; q < PER; ++q) {
-    const uint32_t* const c = s.counts + (int64_t)(tid * PER + q) * s.blocks;
+    total[q] = before[q] = 0;
+    const int d = has ? tid * PER + q : 0;
     if constexpr (DIRECT) {
-      total[q] = before[q] = 0;
-#pragma unroll 8
-      for (uint32_t b = 0; b < s.blocks; ++b) {
-        const uint32_t n = c[b];
-        total[q] += n;
-        before[q] += b < blockIdx.x ? n : 0;
+      for (uint32_t b0 = 0; b0 < s.blocks; b0 += 32) {
+        uint32_t n[32];
+#pragma unroll
+        for (uint32_t u = 0; u < 32; ++u) n[u] = s.counts[min(b0 + u, s.blocks - 1) * D + d];
+#pragma unroll
+        for (uint32_t u = 0; u < 32; ++u) {
+          total[q] += b0 + u < s.blocks ? n[u] : 0;
+          before[q] += b0 + u < blockIdx.x ? n[u] : 0;
+        }
       }
     } else {
-      total[q] = s.totals[tid * PER + q];
-      before[q] = c[blockIdx.x];
+      total[q] = s.totals[d];
+      before[q] = s.counts[(int64_t)d * s.blocks + blockIdx.x];
     }
+    if (!has) total[q] = 0;
     sum += total[q];
   }
   __syncthreads();
 #pragma unroll
-  for (int j = 0; j < IPT; ++j) rank[j] = rank_digit<DB>((key[j] >> s.shift) & (D - 1), count[wave], lane);
-  // where each wave's first token of a digit goes: behind the lower digits, the blocks and the waves before
-  uint32_t lower = exclusive_sum<256>(sum, waves, tid);  // (its barriers stand behind the ranks)
+  for (int j = 0; j < IPT; ++j) rank[j] = rank_digit<DB>((token[j].key >> s.shift) & (D - 1), count[wave], lane);
+  // where the block's first token of a digit goes, behind the lower digits and the blocks before; each wave's
+  // behind those of the waves before
+  uint32_t lower = exclusive_sum<NT>(sum, waves, tid);  // (its barriers stand behind the ranks)
+  if (has) {
 #pragma unroll
-  for (int q = 0; q < PER; ++q) {
-    uint32_t at = lower + before[q];
-    lower += total[q];
-    for (int w = 0; w < 4; ++w) {
-      const uint32_t c = count[w][tid * PER + q];
-      count[w][tid * PER + q] = at;
-      at += c;
+    for (int q = 0; q < PER; ++q) {
+      base[tid * PER + q] = lower + before[q];
+      lower += total[q];
+      uint32_t at = 0;
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        const uint32_t c = count[w][tid * PER + q];
+        count[w][tid * PER + q] = (uint16_t)at;
+        at += c;
+      }
     }
   }
   __syncthreads();
 #pragma unroll
   for (int j = 0; j < IPT; ++j) {
     if (first + 64 * j >= a.tokens) continue;
-    const uint32_t to = count[wave][(key[j] >> s.shift) & (D - 1)] + rank[j];
-    s.keys_out[to] = key[j];
-    s.places_out[to] = place[j];
-    if (s.next) atomicAdd(&s.next[(int64_t)((key[j] >> (s.shift + DB)) & (D - 1)) * s.blocks + to / (256 * IPT)], 1u);
+    const uint32_t d = (token[j].key >> s.shift) & (D - 1);
+    s.out[base[d] + count[wave][d] + rank[j]] = token[j];
   }
 }
 
 // ------------------------------------------------------------------- sums --
+// A row whose tokens begin in a chunk and end in it or in the next one is its
+// chunk's alone: the group that has its beginning goes on into the next chunk, whose
+// group leaves them out.  Longer rows have a part of each chunk: the one where they
+// begin, and those that they pass through or end in.
 struct SumArgs {
-  const uint32_t* keys;
-  const uint32_t* places;
-  float* partial;  // [chunks, 2, ldp]: the sum of a chunk's first row, begun before it, and of its last one, which goes on
+  const Token* list;
+  float* partial;  // [chunks, 2, ldp]: the part of a chunk's first row, begun before it, and of its last one, which goes on
   int64_t ldp;
   int32_t chunk;   // tokens of a chunk
   int32_t chunks, g, columns;  // 1 << g threads own a vector of columns each; groups side by side over the columns
+  int32_t per;     // chunks that a block of the join looks through
+};
+__device__ __forceinline__ uint32_t key_at(const EmbedBwdArgs& a, const SumArgs& s, int64_t i) {
+  return i < 0 || i >= a.tokens ? kNoKey : s.list[i].key;  // (kNoKey: no token's)
+}
+// Whether the row of the chunk's last token goes on behind it, and as a long one,
+// and whether it begins in the chunk.
+struct Tail {
+  uint32_t key;
+  bool open, starts, lasts;  // into the next chunk; in this one; past the next one
+  __device__ __forceinline__ Tail(const EmbedBwdArgs& a, const SumArgs& s, int64_t chunk) {
+    const int64_t i0 = chunk * s.chunk, i1 = i0 + s.chunk;
+    const uint32_t before = key_at(a, s, i0 - 1), after = key_at(a, s, i1), past = key_at(a, s, i1 + s.chunk);
+    key = key_at(a, s, i1 - 1);
+    open = key < a.rows && after == key;
+    starts = before != key;  // (sorted: if the token before the chunk has it, the whole chunk has)
+    lasts = past == key;
+  }
 };
 
 template <typename T>
@@ -341,114 +369,136 @@ __global__ __launch_bounds__(256) void run_sum_kernel(EmbedBwdArgs a, SumArgs s)
   const int n = a.cols - c;
   if (n <= 0) return;
   const int64_t i0 = chunk * s.chunk, i1 = min(a.tokens, i0 + s.chunk);
-  const uint32_t after = i1 < a.tokens ? s.keys[i1] : kNoKey;
-  uint32_t cur = s.keys[i0];
-  bool begun = i0 > 0 && s.keys[i0 - 1] == cur;  // before this chunk
+  Token token[U];  // the next U
+  auto ask = [&](int64_t i) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) token[u] = s.list[min(i + u, a.tokens - 1)];
+  };
+  ask(i0);
+  const Tail tail(a, s, chunk);
+  // the first tokens' row begun before: the chunk before's own, or one with a part here
+  const uint32_t first = token[0].key, before = key_at(a, s, i0 - 1);
+  const bool begun = before == first;
+  const bool skip = begun && (tail.key != first || !tail.open) && key_at(a, s, i0 - s.chunk - 1) != first;
+  // a short row at the end is followed into the next chunk
+  const bool follow = tail.open && tail.starts && !tail.lasts;
+  const int64_t end = follow ? min(a.tokens, i1 + s.chunk) : i1;
   float* const partial = s.partial + chunk * 2 * s.ldp + c;
+  uint32_t cur = first;
+  bool head = begun;  // the present row was begun before the chunk
   float acc[VE];
 #pragma unroll
   for (int e = 0; e < VE; ++e) acc[e] = 0.0f;
-  uint32_t key[U], place[U];  // of the next U tokens
-  auto ask = [&](int64_t i) {
+  auto flush = [&] {  // the present row has ended
+    if (!head) {
+      write_row<T>(a, cur, c, acc);
+    } else if (!skip) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t at = min(i + u, i1 - 1);
-      key[u] = s.keys[at];
-      place[u] = s.places[at];
+      for (int e = 0; e < VE; ++e) partial[e] = acc[e];
     }
   };
-  ask(i0);
-  for (int64_t i = i0; i < i1; i += U) {
-    uint32_t now[U];
+  for (int64_t i = i0; i < end; i += U) {
+    uint32_t key[U];
     Vec<T> v[U];
+    // (every place is a token's: what is read of rows that are not this group's to add is not used)
+    if (n >= VE) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      now[u] = key[u];
-      // (tokens that add to no row are not read)
-      v[u].load(static_cast<const T*>(a.dy) + (int64_t)place[u] * a.ldy + c, key[u] < a.rows ? n : 0);
+      for (int u = 0; u < U; ++u)
+        v[u].raw = *reinterpret_cast<const u32x4_any*>(static_cast<const T*>(a.dy) + (int64_t)token[u].place * a.ldy + c);
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u].load(static_cast<const T*>(a.dy) + (int64_t)token[u].place * a.ldy + c, n);
     }
-    if (i + U < i1) ask(i + U);
+#pragma unroll
+    for (int u = 0; u < U; ++u) key[u] = token[u].key;
+    if (i + U < end) ask(i + U);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (i + u >= i1) break;
-      if (now[u] != cur) {
-        if (begun) {
-#pragma unroll
-          for (int e = 0; e < VE; ++e) partial[e] = acc[e];
-        } else {
-          write_row<T>(a, cur, c, acc);
-        }
-        cur = now[u];
-        begun = false;
+      if (i + u >= end) break;
+      if (key[u] != cur) {
+        flush();
+        if (i + u >= i1 || key[u] >= a.rows) return;  // (the followed row's end; those without a row come last)
+        cur = key[u];
+        head = false;
 #pragma unroll
         for (int e = 0; e < VE; ++e) acc[e] = 0.0f;
       }
-      if (cur >= a.rows) return;  // (these come last)
+      if (cur >= a.rows) return;
       float x[VE];
       v[u].get(x);
 #pragma unroll
       for (int e = 0; e < VE; ++e) acc[e] += x[e];
     }
   }
-  if (!begun && after != cur) {
-    write_row<T>(a, cur, c, acc);
+  if (follow || !tail.open) {
+    flush();
   } else {
 #pragma unroll
-    for (int e = 0; e < VE; ++e) partial[(begun ? 0 : s.ldp) + e] = acc[e];
+    for (int e = 0; e < VE; ++e) partial[(head ? 0 : s.ldp) + e] = acc[e];
   }
 }
 
-// A block: the row that goes on from one chunk into the next ones, for one group
-// of columns.  Its threads' groups take every NG-th chunk.
-template <typename T>
-__global__ __launch_bounds__(256) void run_join_kernel(EmbedBwdArgs a, SumArgs s) {
-  constexpr int VE = kVec<T>;
-  __shared__ float part[256][VE + 1];
-  const int64_t chunk = blockIdx.x / s.columns, i0 = chunk * s.chunk, i1 = i0 + s.chunk;
-  if (i1 >= a.tokens) return;
-  const uint32_t key = s.keys[i1 - 1];
-  if (key >= a.rows || s.keys[i1] != key || (i0 > 0 && s.keys[i0 - 1] == key && s.keys[i0] == key)) return;
-  const int lane = threadIdx.x & ((1 << s.g) - 1), group = threadIdx.x >> s.g, groups = 256 >> s.g;
-  const int c = (((int)(blockIdx.x % s.columns) << s.g) + lane) * VE;
-  float acc[VE];
-#pragma unroll
-  for (int e = 0; e < VE; ++e) acc[e] = 0.0f;
-  if (c < a.cols) {
-    if (group == 0) {
-#pragma unroll
-      for (int e = 0; e < VE; ++e) acc[e] = s.partial[(chunk * 2 + 1) * s.ldp + c + e];
-    }
-    // the next B chunks' first keys and sums are asked for together
-    constexpr int B = 8;
-    bool more = true;
-    for (int64_t b0 = chunk + 1 + group; more; b0 += (int64_t)B * groups) {
-      bool goes[B];
-      f32x4 v[B][VE / 4];
-#pragma unroll
-      for (int u = 0; u < B; ++u) {
-        const int64_t b = min(b0 + (int64_t)u * groups, (int64_t)s.chunks - 1);
-        goes[u] = b0 + (int64_t)u * groups < s.chunks && s.keys[b * s.chunk] == key;
-#pragma unroll
-        for (int q = 0; q < VE / 4; ++q)
-          v[u][q] = *reinterpret_cast<const f32x4*>(s.partial + b * 2 * s.ldp + c + 4 * q);
-      }
-#pragma unroll
-      for (int u = 0; u < B; ++u) {
-#pragma unroll
-        for (int e = 0; e < VE; ++e) acc[e] += goes[u] ? v[u][e / 4][e % 4] : 0.0f;
-      }
-      more = goes[B - 1];
-    }
+// A block: the long rows that begin in its chunks, for one group of columns, one
+// after the other.  Its threads' groups take a row's chunks in turn.
+template <typename T, int NT>
+__global__ __launch_bounds__(NT) void run_join_kernel(EmbedBwdArgs a, SumArgs s) {
+  constexpr int VE = kVec<T>, B = 4;
+  __shared__ float part[NT][VE + 1];
+  __shared__ uint32_t key_of_chunk[16];
+  const int64_t first = (int64_t)(blockIdx.x / s.columns) * s.per;
+  if (threadIdx.x < (uint32_t)s.per) {
+    const Tail t(a, s, first + threadIdx.x);
+    key_of_chunk[threadIdx.x] = t.open && t.starts && t.lasts ? t.key : kNoKey;
   }
-#pragma unroll
-  for (int e = 0; e < VE; ++e) part[threadIdx.x][e] = acc[e];
   __syncthreads();
-  if (group > 0 || c >= a.cols) return;
-  for (int q = 1; q < groups; ++q) {
+  const int lane = threadIdx.x & ((1 << s.g) - 1), group = threadIdx.x >> s.g, groups = NT >> s.g;
+  const int c = (((int)(blockIdx.x % s.columns) << s.g) + lane) * VE;
+  for (int q = 0; q < s.per; ++q) {
+    const uint32_t key = key_of_chunk[q];
+    if (key == kNoKey) continue;  // (the same for the whole block)
+    const int64_t chunk = first + q;
+    float acc[VE];
 #pragma unroll
-    for (int e = 0; e < VE; ++e) acc[e] += part[(q << s.g) + lane][e];
+    for (int e = 0; e < VE; ++e) acc[e] = 0.0f;
+    if (c < a.cols) {
+      if (group == 0) {
+#pragma unroll
+        for (int e = 0; e < VE; ++e) acc[e] = s.partial[(chunk * 2 + 1) * s.ldp + c + e];
+      }
+      // the next B chunks' first keys and sums are asked for together
+      bool more = true;
+      for (int64_t b0 = chunk + 1 + group; more; b0 += (int64_t)B * groups) {
+        bool goes[B];
+        f32x4 v[B][VE / 4];
+#pragma unroll
+        for (int u = 0; u < B; ++u) {
+          const int64_t b = min(b0 + (int64_t)u * groups, (int64_t)s.chunks - 1);
+          goes[u] = b0 + (int64_t)u * groups < s.chunks && s.list[b * s.chunk].key == key;
+#pragma unroll
+          for (int h = 0; h < VE / 4; ++h)
+            v[u][h] = *reinterpret_cast<const f32x4*>(s.partial + b * 2 * s.ldp + c + 4 * h);
+        }
+#pragma unroll
+        for (int u = 0; u < B; ++u) {
+#pragma unroll
+          for (int e = 0; e < VE; ++e) acc[e] += goes[u] ? v[u][e / 4][e % 4] : 0.0f;
+        }
+        more = goes[B - 1];
+      }
+    }
+    // the groups' sums by halves
+    for (int h = groups / 2; h >= 1; h /= 2) {
+#pragma unroll
+      for (int e = 0; e < VE; ++e) part[threadIdx.x][e] = acc[e];
+      __syncthreads();
+      if (group < h) {
+#pragma unroll
+        for (int e = 0; e < VE; ++e) acc[e] += part[((group + h) << s.g) + lane][e];
+      }
+      __syncthreads();
+    }
+    if (group == 0 && c < a.cols) write_row<T>(a, key, c, acc);
   }
-  write_row<T>(a, key, c, acc);
 }
 
 // ------------------------------------------------------------------- host --
@@ -459,20 +509,21 @@ int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 // How a gradient is laid out over launches, and its workspace.
 struct BwdPlan {
   int bits, digit, rounds;  // of the keys, of a digit, digits
-  int items;                // tokens a thread of the long sort
-  uint32_t blocks;          // of tokens in it
+  bool wide;                // blocks of 4096 tokens, not of 256
+  uint32_t blocks;          // of tokens in the long sort
   SumArgs sum;
-  size_t keys, counts, totals, partial, bytes;  // byte offsets
+  size_t counts, totals, partial, bytes;  // byte offsets
 };
 BwdPlan plan(int prec, int64_t tokens, int64_t rows, int32_t cols) {
   BwdPlan p{};
   const int ve = prec == PACK_PREC_BF16 ? 8 : 4;
   while (p.bits < 32 && (rows >> p.bits) > 0) ++p.bits;  // keys 0 .. rows
   const bool one = tokens <= kSortOne;
-  p.items = tokens <= 256 * (int64_t)kDirect ? 1 : 4;
-  p.blocks = one ? 0 : (uint32_t)((tokens + 256 * p.items - 1) / (256 * p.items));
+  p.wide = tokens > 256 * (int64_t)kDirect;
+  const int64_t tile = p.wide ? 4096 : 256;
+  p.blocks = one ? 0 : (uint32_t)((tokens + tile - 1) / tile);
   // digits of 8 bits, or of 11 where that saves a round
-  p.digit = p.items > 1 && (p.bits + 10) / 11 < (p.bits + 7) / 8 ? 11 : 8;
+  p.digit = p.wide && (p.bits + 10) / 11 < (p.bits + 7) / 8 ? 11 : 8;
   p.rounds = (p.bits + p.digit - 1) / p.digit;
   const int64_t vectors = ((int64_t)cols + ve - 1) / ve;
   while (p.sum.g < 6 && ((int64_t)1 << p.sum.g) < vectors) ++p.sum.g;
@@ -483,10 +534,13 @@ BwdPlan plan(int prec, int64_t tokens, int64_t rows, int32_t cols) {
   p.sum.chunk = (int)chunk;
   p.sum.chunks = (int)((tokens + chunk - 1) / chunk);
   p.sum.ldp = vectors * ve;
-  p.keys = 0;
-  size_t at = (size_t)up(tokens * 4, 16) * (one ? 2 : 4);
+  // blocks of the join: as many as the chip holds at a time, of 1 to 16 chunks
+  p.sum.per = 1;
+  const int64_t held = p.sum.g >= 5 ? 512 : 2048;
+  while (p.sum.per < 16 && (int64_t)p.sum.chunks * p.sum.columns > held * p.sum.per) p.sum.per *= 2;
+  size_t at = (size_t)up(tokens * 8, 16) * (one ? 1 : 2);
   p.counts = at;
-  at += (size_t)up(((int64_t)p.blocks << p.digit) * p.rounds * 4, 16);
+  at += (size_t)up(((int64_t)p.blocks << p.digit) * 4, 16);
   p.totals = at;
   at += one ? 0 : ((size_t)4 << p.digit);
   p.partial = at;
@@ -495,24 +549,24 @@ BwdPlan plan(int prec, int64_t tokens, int64_t rows, int32_t cols) {
   return p;
 }
 
-template <typename T, int DB, int IPT>
-hipError_t sort_long(const EmbedBwdArgs& a, const BwdPlan& p, SortArgs s, uint32_t* (&buf)[2][2], uint32_t zeros,
-                     hipStream_t st) {
-  const dim3 grid(p.blocks + zeros), block(256);
-  uint32_t* const counts = s.counts;
-  s.rounds = p.rounds;
-  hipLaunchKernelGGL((sort_count_kernel<T, DB, IPT>), grid, block, 0, st, a, s);
-  for (int r = 0; r < p.rounds; ++r) {
-    s.round = r, s.shift = r * DB;
-    s.keys = buf[(r + 1) & 1][0], s.places = buf[(r + 1) & 1][1];
-    s.keys_out = buf[r & 1][0], s.places_out = buf[r & 1][1];
-    s.counts = counts + (((int64_t)r << DB) * p.blocks);
-    s.next = r + 1 < p.rounds ? counts + (((int64_t)(r + 1) << DB) * p.blocks) : nullptr;
+// The list ends up in buf[(rounds + 1) & 1].
+template <typename T, int DB, int NT, int IPT>
+hipError_t sort_long(const EmbedBwdArgs& a, const BwdPlan& p, SortArgs s, Token* const (&buf)[2], hipStream_t st) {
+  s.launches = 2 * p.rounds;
+  // blocks that write zeros: a KB a wave and launch or more, up to four blocks a CU
+  const int64_t bytes = a.rows * a.cols * (int64_t)sizeof(T) / s.launches, each = NT * 16;
+  const dim3 grid(p.blocks + (uint32_t)std::min<int64_t>((bytes + each - 1) / each, 1024)), block(NT);
+  for (s.round = 0; s.round < p.rounds; ++s.round) {
+    s.shift = s.round * DB;
+    s.list = buf[(s.round + 1) & 1], s.out = buf[s.round & 1];
+    s.launch = 2 * s.round;
+    hipLaunchKernelGGL((sort_count_kernel<T, DB, NT, IPT>), grid, block, 0, st, a, s);
+    ++s.launch;
     if (p.blocks <= kDirect) {
-      hipLaunchKernelGGL((sort_move_kernel<T, DB, IPT, true>), grid, block, 0, st, a, s);
+      hipLaunchKernelGGL((sort_move_kernel<T, DB, NT, IPT, true>), grid, block, 0, st, a, s);
     } else if constexpr (IPT > 1) {
-      hipLaunchKernelGGL(sort_scan_kernel, dim3(1 << DB), block, 0, st, s);
-      hipLaunchKernelGGL((sort_move_kernel<T, DB, IPT, false>), grid, block, 0, st, a, s);
+      hipLaunchKernelGGL(sort_scan_kernel, dim3(1 << DB), dim3(256), 0, st, s);
+      hipLaunchKernelGGL((sort_move_kernel<T, DB, NT, IPT, false>), grid, block, 0, st, a, s);
     }
   }
   return hipGetLastError();
@@ -523,38 +577,40 @@ hipError_t embed_bwd_t(int prec, const EmbedBwdArgs& a, hipStream_t st) {
   const BwdPlan p = plan(prec, a.tokens, a.rows, a.cols);
   if ((int64_t)p.sum.chunks * p.sum.columns >= (int64_t)1 << 24) return hipErrorInvalidConfiguration;  // (2^32 threads)
   char* const w = static_cast<char*>(a.work);
-  const int64_t list = up(a.tokens * 4, 16);
-  uint32_t* buf[2][2];
-  for (int i = 0; i < 4; ++i) buf[i / 2][i % 2] = reinterpret_cast<uint32_t*>(w + p.keys + i * list);
-  // blocks that write zeros beside the sort: 16 KB each a launch or more, up to four a CU
-  const int64_t bytes = a.rows * a.cols * (int64_t)sizeof(T);
+  Token* const buf[2] = {reinterpret_cast<Token*>(w), reinterpret_cast<Token*>(w + up(a.tokens * 8, 16))};
   hipError_t e;
   int last = 0;  // the buffer that holds the sorted list
   if (a.tokens <= kSortOne) {
+    const int64_t bytes = a.rows * a.cols * (int64_t)sizeof(T);
     const dim3 grid(1 + (uint32_t)std::min<int64_t>((bytes + 65535) / 65536, 512)), block(1024);
     if (a.tokens <= 1024)
-      hipLaunchKernelGGL((sort_one_kernel<T, 1>), grid, block, 0, st, a, buf[0][0], buf[0][1], p.bits);
+      hipLaunchKernelGGL((sort_one_kernel<T, 1>), grid, block, 0, st, a, buf[0], p.bits);
     else
-      hipLaunchKernelGGL((sort_one_kernel<T, 4>), grid, block, 0, st, a, buf[0][0], buf[0][1], p.bits);
+      hipLaunchKernelGGL((sort_one_kernel<T, 4>), grid, block, 0, st, a, buf[0], p.bits);
     e = hipGetLastError();
   } else {
-    const uint32_t zeros = (uint32_t)std::min<int64_t>((bytes / (p.rounds + 1) + 16383) / 16384, 1024);
     SortArgs s{};
     s.counts = reinterpret_cast<uint32_t*>(w + p.counts), s.totals = reinterpret_cast<uint32_t*>(w + p.totals);
     s.blocks = p.blocks;
-    if (p.digit == 11)
-      e = sort_long<T, 11, 4>(a, p, s, buf, zeros, st);
+    if (!p.wide)
+      e = sort_long<T, 8, 256, 1>(a, p, s, buf, st);
     else
-      e = p.items == 1 ? sort_long<T, 8, 1>(a, p, s, buf, zeros, st) : sort_long<T, 8, 4>(a, p, s, buf, zeros, st);
+      e = p.digit == 8 ? sort_long<T, 8, 1024, 4>(a, p, s, buf, st) : sort_long<T, 11, 1024, 4>(a, p, s, buf, st);
     last = (p.rounds + 1) & 1;
   }
   if (e != hipSuccess || a.tokens == 0) return e;
   SumArgs s = p.sum;
-  s.keys = buf[last][0], s.places = buf[last][1];
+  s.list = buf[last];
   s.partial = reinterpret_cast<float*>(w + p.partial);
   const int64_t units = (int64_t)s.chunks * s.columns, per = 256 >> s.g;
   hipLaunchKernelGGL((run_sum_kernel<T>), dim3((uint32_t)((units + per - 1) / per)), dim3(256), 0, st, a, s);
-  if (s.chunks > 1) hipLaunchKernelGGL((run_join_kernel<T>), dim3((uint32_t)units), dim3(256), 0, st, a, s);
+  if (s.chunks > 2) {  // (a row over two chunks is short)
+    const int64_t joins = ((int64_t)s.chunks + s.per - 1) / s.per * s.columns;
+    if (s.g >= 5)
+      hipLaunchKernelGGL((run_join_kernel<T, 1024>), dim3((uint32_t)joins), dim3(1024), 0, st, a, s);
+    else
+      hipLaunchKernelGGL((run_join_kernel<T, 256>), dim3((uint32_t)joins), dim3(256), 0, st, a, s);
+  }
   return hipGetLastError();
 }
 
