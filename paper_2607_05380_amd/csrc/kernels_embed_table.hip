@@ -536,7 +536,7 @@ BwdPlan plan(int prec, int64_t tokens, int64_t rows, int32_t cols) {
   p.sum.ldp = vectors * ve;
   // blocks of the join: as many as the chip holds at a time, of 1 to 16 chunks
   p.sum.per = 1;
-  const int64_t held = p.sum.g >= 5 ? 512 : 2048;
+  const int64_t held = p.sum.g >= 5 ? 512 : 4096;
   while (p.sum.per < 16 && (int64_t)p.sum.chunks * p.sum.columns > held * p.sum.per) p.sum.per *= 2;
   size_t at = (size_t)up(tokens * 8, 16) * (one ? 1 : 2);
   p.counts = at;

@@ -356,7 +356,7 @@ hipError_t backward_t(const LayerNormBwdArgs& a, hipStream_t s) {
 // Rows of partial sums: those of the root-mean-square norm's backward pass up to
 // 16,384 columns, past them 64 groups of rows, of 32 rows at least, for each block of columns.
 int layer_norm_bwd_blocks(int64_t rows, int32_t cols) {
-  if (cols <= 16384) return norm_bwd_blocks(rows, cols);
+  if (cols <= 16384) return norm_bwd_blocks((rows + 1) / 2, cols);
   const int64_t want = (rows + 31) / 32;
   return (int)(want < 64 ? (want > 0 ? want : 1) : 64);
 }
