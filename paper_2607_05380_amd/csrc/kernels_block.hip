@@ -1,6 +1,7 @@
 // Matrix products of the student network on gfx950: the gated feed-forward
-// block (forward and backward, bf16 and fp32) and the 8-bit product with a
-// scale per row and per output, plain or gated.
+// block (forward and backward, bf16 and fp32) and the 8-bit products, plain or
+// gated: of whole numbers with a scale per row and per output, and of floating
+// point codes with a scale per block of 128 of the depth.
 //
 // All of them are C[m, n] = sum_k A(m, k) B(n, k) with an epilogue per element
 // (MmEpi).  Operands are depth-contiguous or rows-contiguous, so that the
@@ -37,7 +38,14 @@
 // What bounds the large tiles is power: with random operands the MFMAs alone,
 // without loads or LDS reads, take 0.82 of the time of the whole loop, and with
 // zeros the loop is 1.4 times faster.
-// MFMAs: v_mfma_f32_32x32x16_bf16, v_mfma_i32_32x32x32_i8,
+// 8-bit floating point: a K step is one block of scales.  Its products are summed
+// from zero by the matrix instructions (32 x 32 x 64) and added to the sums by one
+// multiply-add an element with the row's scale times the columns': 64 of them
+// a step and 64 x 64 block beside 8 MFMAs of 64 cycles, hidden behind them.  8192
+// a side 481 us, 2.28 PFLOP/s (a library product with one scale in all 2.62; whole
+// numbers 440 us), 128 x 128 tiles 567; results in fp32 956 (see f8x_t).  20,011 x 1024 ->
+// 4096 gated 213 us, of which the gate epilogues a third: nothing covers them.
+// MFMAs: v_mfma_f32_32x32x16_bf16, v_mfma_i32_32x32x32_i8, v_mfma_f32_32x32x64_f8f6f4,
 // v_mfma_f32_32x32x2_f32, with B as the first operand, so that a lane holds 4
 // consecutive columns of one row of C.  Accumulators are fp32 or int32, added
 // in a fixed order; a depth split over workgroups is joined in a fixed order
@@ -540,7 +548,8 @@ __global__ __launch_bounds__(256) void join_pair_kernel(MmPair p) {
 // (rows-contiguous: element) that region row r holds, relative to P, or -1.
 // Lanes outside the operand have an offset past the descriptor's range and
 // read zeros, so depth past the end adds nothing.
-template <int NW, int ES, bool RM, int R = 128>
+// SHORT: the depth's end is compared in 32 bits (fewer registers).
+template <int NW, int ES, bool RM, int R = 128, bool SHORT = false>
 struct Dma {
   static constexpr int PER = R / 8 / NW;
   const char* base;
@@ -578,8 +587,14 @@ struct Dma {
   }
   // block p of the region at `lds` with the step that starts at depth k0
   __device__ __forceinline__ void issue(char* lds, int64_t k0, int64_t kend, int p) const {
-    const int left = (int)min(kend - k0, (int64_t)1 << 30);  // of the depth
-    const uint32_t v = kofs[p] < left ? voff[p] : kOob;
+    bool in;
+    if constexpr (SHORT) {
+      const int left = (int)min(kend - k0, (int64_t)1 << 30);
+      in = kofs[p] < left;
+    } else {
+      in = k0 + kofs[p] < kend;
+    }
+    const uint32_t v = in ? voff[p] : kOob;
     if constexpr (!RM)
       dma16(rsrc, lds + (blk0 + p) * 1024, v, (uint32_t)(k0 * ES));
     else
@@ -1171,8 +1186,8 @@ __device__ __forceinline__ void huge_tile(const MmArgs& a, uint32_t block, char*
   const int nk = (int)((kend - kbeg + KE - 1) / KE);
   const T* A = static_cast<const T*>(a.A) + (RA ? (int64_t)m0 : m0 * a.lda);
   const T* B = static_cast<const T*>(a.B) + (RB ? (int64_t)n0 : n0 * a.ldb);
-  Dma<8, ES, RA> la[2];
-  Dma<8, ES, RB> lb[2];
+  Dma<8, ES, RA, 128, kF8<T>> la[2];
+  Dma<8, ES, RB, 128, kF8<T>> lb[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     // A half h: the rows of phases 2h, 2h + 1 of both wave rows; B half h: the
@@ -1350,7 +1365,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   huge_tile<T, RA, RB, EPI>(a, blockIdx.x, smem);
 }
 // -------------------------------------------------------------- thin tiles --
-// Up to 16 rows of A (depth-contiguous operands, bf16 and int8): a workgroup
+// Up to 16 rows of A (depth-contiguous operands, bf16 and 8 bits): a workgroup
 // owns 16 columns (gated: 16 gate and 16 up rows of B), its NW waves share the
 // depth in strips of 256 bytes, and every weight byte is read once, straight
 // into MFMA operands (16 x 16 blocks; lane l holds 16 bytes of depth of row

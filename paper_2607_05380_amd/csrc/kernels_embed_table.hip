@@ -15,9 +15,14 @@
 //
 // The sort is by digits of the index from the lowest on.  A wave ranks 64 tokens
 // at a time: lanes with the same digit find each other by ballots, one of them
-// advances the wave's count of the digit.  Up to 16,384 tokens one workgroup holds
-// all of them in LDS and one launch sorts; longer lists take three launches a
-// digit (counts per block of 4096, their running sums, the move).
+// advances the wave's count of the digit.  Up to 4096 tokens one workgroup holds
+// all of them in registers and LDS, and one launch sorts (16,384 that way took
+// 34 us, in 64 workgroups 24); longer lists take two launches a digit or three.
+//
+// Measured: 65,536 tokens of 100,003 x 512 bf16 looked up in 18 us; the gradient
+// of 16,384 tokens of 32,000 x 1024 bf16 47 us (sort and zeros 24, six launches of 5
+// to 8 us; sums 14, at 3.3 TB/s; join 7), of 1,000,000 tokens of 1600 x 32 fp32 75 (count 9, scan 4,
+// move 16, sums 32, at 4.1 TB/s of gathered rows of 128 bytes, join 10).
 #include <algorithm>
 
 #include "ops_internal.h"

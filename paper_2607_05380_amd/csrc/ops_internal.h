@@ -1,6 +1,7 @@
 // Launch interface between the host entry points of the student's operators
 // (ops.cpp) and their kernels (kernels_rows.hip, kernels_layer_norm.hip,
-// kernels_embed_table.hip, kernels_dropout.hip, kernels_quant.hip, kernels_block.hip).
+// kernels_embed_table.hip, kernels_dropout.hip, kernels_quant.hip,
+// kernels_block.hip).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>

@@ -1,6 +1,7 @@
 // What the row kernels share (kernels_rows.hip, kernels_layer_norm.hip,
-// kernels_embed_table.hip, kernels_dropout.hip, kernels_quant.hip): vectors of 16 bytes at any alignment of
-// the element, reductions over the threads of a row, blocks of a launch over rows.
+// kernels_embed_table.hip, kernels_dropout.hip, kernels_quant.hip): vectors of
+// 16 bytes at any alignment of the element, reductions over the threads of a row,
+// blocks of a launch over rows.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>

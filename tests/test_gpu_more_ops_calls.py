@@ -170,3 +170,43 @@ def test_offsets_past_32_bits():
     z = ops.f8_matmul(q, s, qw, sw)
     ref = ops.f8_matmul(qs, ss, qw, sw, dtype=torch.float32)
     assert float((z[idx].float() - ref).abs().max()) <= 2.0 ** -7 * float(ref.abs().max())
+
+
+def _draws(rows, cols, seed, step, site):
+    """The 16-bit draws of the given rows' first columns, from the oracle's generator."""
+    import numpy as np
+    from oracle.philox import philox4x32_10
+    c, r = np.meshgrid(np.arange(-(-cols // 8), dtype=np.uint64), np.asarray(rows, dtype=np.uint64))
+    w = np.stack([np.asarray(x, dtype=np.uint64) for x in philox4x32_10(
+        c, r, np.uint64(site), np.uint64(step), seed & 0xFFFFFFFF, (seed >> 32) ^ (4 << 28))], -1)
+    return np.stack([w & np.uint64(0xFFFF), w >> np.uint64(16)], -1).reshape(len(rows), -1)[:, :cols]
+
+
+def test_more_vectors_than_32_bits_count():
+    """2.2e9 vectors: the kernels' other division, and rows near 2^31."""
+    rows, cols = 1_100_000_000, 9
+    x = torch.ones(rows, cols, dtype=torch.bfloat16, device="cuda")
+    at = [0, 1, 500_000_000, rows - 2, rows - 1]
+    y = ops.dropout(x, 0.5, 9, 8, site=7)
+    keep = torch.from_numpy(_draws(at, cols, 9, 8, 7) >= 32768).cuda()
+    assert torch.equal(y[at] != 0, keep) and bool((y[at][keep] == 2).all())
+    del y
+    x[:3] = torch.randn(3, cols, device="cuda").bfloat16()
+    idx = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    idx[at] = torch.tensor([2, 1, -1, 1, rows - 1], dtype=torch.int32, device="cuda")
+    y = ops.embed(idx, x)
+    assert torch.equal(y[at], torch.stack([x[2], x[1], torch.zeros_like(x[0]), x[1], x[-1]]))
+    assert torch.equal(y[700_000_000:700_000_100], x[0].expand(100, cols))
+
+
+def test_more_rows_than_a_launch_has_blocks():
+    """2^20 blocks of 4 rows: each goes on to rows past the grid."""
+    rows, cols = 4_300_000, 300
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.randn(rows, cols, generator=g, device="cuda", dtype=torch.bfloat16)
+    w = torch.randn(cols, generator=g, device="cuda")
+    y, _, mean, rstd = ops.add_layer_norm(x, w, w)
+    half = rows // 2
+    for part in (slice(0, half), slice(half, rows)):
+        z, _, m, r = ops.add_layer_norm(x[part], w, w)
+        assert torch.equal(y[part], z) and torch.equal(mean[part], m) and torch.equal(rstd[part], r)
