@@ -81,10 +81,21 @@ struct alignas(8) Token {
   uint32_t key, place;
 };
 
-// A token's key: its row, or `rows` for one that adds to none.
-__device__ __forceinline__ uint32_t key_of(const EmbedBwdArgs& a, int64_t t) {
-  const int64_t r = row_of(a.idx, a.idx64, t, a.rows);
-  return (uint32_t)(r < 0 ? a.rows : r);
+// The tokens first + stride j of the batch (past its end: some token's key).  A
+// key is the row, or `rows` for a token that adds to none.
+template <int N>
+__device__ __forceinline__ void keys_of(const EmbedBwdArgs& a, int64_t first, int stride, Token (&t)[N]) {
+  int64_t row[N];
+  if (a.idx64) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) row[j] = static_cast<const int64_t*>(a.idx)[min(first + stride * j, a.tokens - 1)];
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j) row[j] = static_cast<const int32_t*>(a.idx)[min(first + stride * j, a.tokens - 1)];
+  }
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+    t[j] = Token{(uint32_t)(row[j] < 0 || row[j] >= a.rows ? a.rows : row[j]), (uint32_t)(first + stride * j)};
 }
 
 __device__ __forceinline__ void wave_order() {
@@ -155,11 +166,17 @@ __global__ __launch_bounds__(1024) void sort_one_kernel(EmbedBwdArgs a, Token* l
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = (int)a.tokens;
   const int first = wave * 64 * IPT + lane;  // the thread's items: first + 64 j
   uint32_t key[IPT], place[IPT], rank[IPT];
+  if (n > 0) {
+    Token t[IPT];
+    keys_of<IPT>(a, first, 64, t);
 #pragma unroll
-  for (int j = 0; j < IPT; ++j) {
-    const int i = first + 64 * j;
-    key[j] = i < n ? key_of(a, i) : kNoKey;
-    place[j] = (uint32_t)i;
+    for (int j = 0; j < IPT; ++j) {
+      key[j] = first + 64 * j < n ? t[j].key : kNoKey;
+      place[j] = t[j].place;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < IPT; ++j) key[j] = kNoKey, place[j] = 0;
   }
   for (int shift = 0; shift < bits; shift += 8) {
     for (int i = tid; i < 16 * 256; i += 1024) count[i >> 8][i & 255] = 0;
@@ -202,9 +219,11 @@ __global__ __launch_bounds__(1024) void sort_one_kernel(EmbedBwdArgs a, Token* l
 
 // Longer lists, a digit of DB bits in two launches or three: blocks of NT IPT
 // tokens count theirs, then move them.  Up to kDirect blocks a move adds up the
-// counts of the blocks before its own by itself, past that a launch between them
-// does.  The blocks behind the sort's write zeros.  What bounds the moves of a long
-// list is its scattered stores: larger blocks have longer runs of a digit.
+// counts of the blocks before its own by itself (each block counting the whole
+// list instead of a launch of their own for the counts: 16,384 tokens of 32,000 x
+// 1024 49 us, this way 47), past that a launch between them does.  The blocks
+// behind the sort's write zeros.  What bounds the moves of a long list is its
+// scattered stores: larger blocks have longer runs of a digit.
 constexpr uint32_t kDirect = 64;
 struct SortArgs {
   const Token* list;
@@ -214,9 +233,20 @@ struct SortArgs {
   uint32_t blocks;
   int shift, round, launch, launches;  // (launches: those that write zeros)
 };
-__device__ __forceinline__ Token sort_token(const EmbedBwdArgs& a, const SortArgs& s, int64_t i) {
-  if (i >= a.tokens) return Token{kNoKey, 0};
-  return s.round ? s.list[i] : Token{key_of(a, i), (uint32_t)i};
+// The tokens first + stride j, all of them asked for together (past the end:
+// kNoKey).  The lists hold one token at least.
+template <int N>
+__device__ __forceinline__ void sort_tokens(const EmbedBwdArgs& a, const SortArgs& s, int64_t first, int stride,
+                                            Token (&t)[N]) {
+  if (s.round) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) t[j] = s.list[min(first + stride * j, a.tokens - 1)];
+  } else {
+    keys_of<N>(a, first, stride, t);
+  }
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+    if (first + stride * j >= a.tokens) t[j].key = kNoKey;
 }
 template <typename T, int DB, int NT, int IPT>
 __global__ __launch_bounds__(NT) void sort_count_kernel(EmbedBwdArgs a, SortArgs s) {
@@ -228,12 +258,11 @@ __global__ __launch_bounds__(NT) void sort_count_kernel(EmbedBwdArgs a, SortArgs
   for (int d = threadIdx.x; d < 1 << DB; d += NT) count[d] = 0;
   __syncthreads();
   const int64_t first = (int64_t)blockIdx.x * (NT * IPT) + threadIdx.x;
-  uint32_t key[IPT];
-#pragma unroll
-  for (int j = 0; j < IPT; ++j) key[j] = sort_token(a, s, first + NT * j).key;
+  Token token[IPT];
+  sort_tokens(a, s, first, NT, token);
 #pragma unroll
   for (int j = 0; j < IPT; ++j)  // (whole numbers: the order of these additions does not matter)
-    if (first + NT * j < a.tokens) atomicAdd(&count[(key[j] >> s.shift) & ((1 << DB) - 1)], 1u);
+    if (token[j].key != kNoKey) atomicAdd(&count[(token[j].key >> s.shift) & ((1 << DB) - 1)], 1u);
   __syncthreads();
   // (in the order in which a move, or the scan, reads them)
   const int64_t of_digit = s.blocks <= kDirect ? 1 : s.blocks, of_block = s.blocks <= kDirect ? 1 << DB : 1;
@@ -269,8 +298,7 @@ __global__ __launch_bounds__(NT) void sort_move_kernel(EmbedBwdArgs a, SortArgs 
   const int64_t first = (int64_t)blockIdx.x * (NT * IPT) + wave * (64 * IPT) + lane;
   Token token[IPT];
   uint32_t rank[IPT];
-#pragma unroll
-  for (int j = 0; j < IPT; ++j) token[j] = sort_token(a, s, first + 64 * j);
+  sort_tokens(a, s, first, 64, token);
   // a thread's PER digits: tokens with the digit, and those of the blocks before
   uint32_t total[PER], before[PER], sum = 0;
   const bool has = tid * PER < D;
@@ -337,6 +365,7 @@ struct SumArgs {
   int32_t chunk;   // tokens of a chunk
   int32_t chunks, g, columns;  // 1 << g threads own a vector of columns each; groups side by side over the columns
   int32_t per;     // chunks that a block of the join looks through
+  bool many;       // its blocks have 1024 threads, not 256
 };
 __device__ __forceinline__ uint32_t key_at(const EmbedBwdArgs& a, const SumArgs& s, int64_t i) {
   return i < 0 || i >= a.tokens ? kNoKey : s.list[i].key;  // (kNoKey: no token's)
@@ -447,7 +476,7 @@ __global__ __launch_bounds__(256) void run_sum_kernel(EmbedBwdArgs a, SumArgs s)
 // after the other.  Its threads' groups take a row's chunks in turn.
 template <typename T, int NT>
 __global__ __launch_bounds__(NT) void run_join_kernel(EmbedBwdArgs a, SumArgs s) {
-  constexpr int VE = kVec<T>, B = 4;
+  constexpr int VE = kVec<T>, B = NT > 256 ? 32 / VE : 4;
   __shared__ float part[NT][VE + 1];
   __shared__ uint32_t key_of_chunk[16];
   const int64_t first = (int64_t)(blockIdx.x / s.columns) * s.per;
@@ -539,15 +568,17 @@ BwdPlan plan(int prec, int64_t tokens, int64_t rows, int32_t cols) {
   p.sum.chunk = (int)chunk;
   p.sum.chunks = (int)((tokens + chunk - 1) / chunk);
   p.sum.ldp = vectors * ve;
-  // blocks of the join: as many as the chip holds at a time, of 1 to 16 chunks
+  // blocks of the join: as many as the chip holds at a time, of 1 to 16 chunks; large ones where a row takes
+  // many threads, or has hundreds of chunks (1,000,000 tokens of 2 x 32 fp32 103 us, with 256 threads 255)
+  p.sum.many = p.sum.g >= 5 || tokens > 256 * chunk * rows;
   p.sum.per = 1;
-  const int64_t held = p.sum.g >= 5 ? 512 : 4096;
+  const int64_t held = p.sum.many ? 512 : 4096;
   while (p.sum.per < 16 && (int64_t)p.sum.chunks * p.sum.columns > held * p.sum.per) p.sum.per *= 2;
   size_t at = (size_t)up(tokens * 8, 16) * (one ? 1 : 2);
   p.counts = at;
   at += (size_t)up(((int64_t)p.blocks << p.digit) * 4, 16);
   p.totals = at;
-  at += one ? 0 : ((size_t)4 << p.digit);
+  at += p.blocks <= kDirect ? 0 : (size_t)4 << p.digit;
   p.partial = at;
   if (p.sum.chunks > 1) at += (size_t)p.sum.chunks * 2 * (size_t)p.sum.ldp * 4;
   p.bytes = at;
@@ -611,7 +642,7 @@ hipError_t embed_bwd_t(int prec, const EmbedBwdArgs& a, hipStream_t st) {
   hipLaunchKernelGGL((run_sum_kernel<T>), dim3((uint32_t)((units + per - 1) / per)), dim3(256), 0, st, a, s);
   if (s.chunks > 2) {  // (a row over two chunks is short)
     const int64_t joins = ((int64_t)s.chunks + s.per - 1) / s.per * s.columns;
-    if (s.g >= 5)
+    if (s.many)
       hipLaunchKernelGGL((run_join_kernel<T, 1024>), dim3((uint32_t)joins), dim3(1024), 0, st, a, s);
     else
       hipLaunchKernelGGL((run_join_kernel<T, 256>), dim3((uint32_t)joins), dim3(256), 0, st, a, s);
