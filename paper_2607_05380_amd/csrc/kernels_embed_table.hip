@@ -360,7 +360,8 @@ __global__ __launch_bounds__(NT) void sort_move_kernel(EmbedBwdArgs a, SortArgs 
 // begin, and those that they pass through or end in.
 struct SumArgs {
   const Token* list;
-  float* partial;  // [chunks, 2, ldp]: the part of a chunk's first row, begun before it, and of its last one, which goes on
+  // [chunks, 2, ldp]: the part of a chunk's first row, begun before it, and of its last one, which goes on
+  float* partial;
   int64_t ldp;
   int32_t chunk;   // tokens of a chunk
   int32_t chunks, g, columns;  // 1 << g threads own a vector of columns each; groups side by side over the columns
@@ -418,6 +419,7 @@ __global__ __launch_bounds__(256) void run_sum_kernel(EmbedBwdArgs a, SumArgs s)
   const bool follow = tail.open && tail.starts && !tail.lasts;
   const int64_t end = follow ? min(a.tokens, i1 + s.chunk) : i1;
   float* const partial = s.partial + chunk * 2 * s.ldp + c;
+  const T* const dy = static_cast<const T*>(a.dy) + c;
   uint32_t cur = first;
   bool head = begun;  // the present row was begun before the chunk
   float acc[VE];
@@ -438,10 +440,10 @@ __global__ __launch_bounds__(256) void run_sum_kernel(EmbedBwdArgs a, SumArgs s)
     if (n >= VE) {
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        v[u].raw = *reinterpret_cast<const u32x4_any*>(static_cast<const T*>(a.dy) + (int64_t)token[u].place * a.ldy + c);
+        v[u].raw = *reinterpret_cast<const u32x4_any*>(dy + (int64_t)token[u].place * a.ldy);
     } else {
 #pragma unroll
-      for (int u = 0; u < U; ++u) v[u].load(static_cast<const T*>(a.dy) + (int64_t)token[u].place * a.ldy + c, n);
+      for (int u = 0; u < U; ++u) v[u].load(dy + (int64_t)token[u].place * a.ldy, n);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) key[u] = token[u].key;
@@ -656,7 +658,9 @@ hipError_t launch_embed(int prec, const EmbedArgs& a, hipStream_t s) {
   return prec == PACK_PREC_BF16 ? embed_t<__bf16>(a, s) : embed_t<float>(a, s);
 }
 
-size_t embed_bwd_bytes(int prec, int64_t tokens, int64_t rows, int32_t cols) { return plan(prec, tokens, rows, cols).bytes; }
+size_t embed_bwd_bytes(int prec, int64_t tokens, int64_t rows, int32_t cols) {
+  return plan(prec, tokens, rows, cols).bytes;
+}
 
 hipError_t launch_embed_bwd(int prec, const EmbedBwdArgs& a, hipStream_t s) {
   return prec == PACK_PREC_BF16 ? embed_bwd_t<__bf16>(prec, a, s) : embed_bwd_t<float>(prec, a, s);

@@ -311,8 +311,8 @@ def layer_norm_backward(dy, v, weight, mean, rstd, dv=None):
     dx, sums = _empty(v, rows, cols), _empty(v, 2, cols, dtype=torch.float32)
     dw, db = sums.unbind()
     work = _empty(v, _bytes("pack_layer_norm_backward_workspace_size", rows, cols), dtype=torch.uint8)
-    _call("pack_layer_norm_backward", v, (dy, weight, mean, rstd, dv), yp, ldy, vp, ldv, wp, mp, rp, dp, ldd, prec, rows,
-          cols, dx.data_ptr(), cols, dw.data_ptr(), db.data_ptr(), work.data_ptr(), work.numel())
+    _call("pack_layer_norm_backward", v, (dy, weight, mean, rstd, dv), yp, ldy, vp, ldv, wp, mp, rp, dp, ldd, prec,
+          rows, cols, dx.data_ptr(), cols, dw.data_ptr(), db.data_ptr(), work.data_ptr(), work.numel())
     return dx, dw, db
 
 

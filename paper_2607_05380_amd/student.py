@@ -54,6 +54,7 @@ class Student:
             return torch.randn(rows, cols, generator=g, device=device) * cols ** -0.5
 
         self.act, self.dtype, self.eps, self.classes = act, dtype, eps, classes
+        self.codes = "int8"
         self.layer, self.p, self.seed = norm == "layer", dropout, seed & 0xFFFFFFFFFFFFFFFF
         self.params = []
         for _ in range(blocks):
@@ -82,6 +83,8 @@ class Student:
         not have (negative, or too large) is missing: zeros."""
         if not self.columns:
             return x.to(dtype), None
+        if columns is None or columns.shape != (x.shape[0], len(self.columns)):
+            raise ops.PackError(f"columns must hold the classes of {len(self.columns)} columns for each row")
         there = (columns >= 0) & (columns < self.sizes)
         at = torch.where(there, columns.to(torch.int32) + self.offsets, -1).reshape(-1)
         rows = ops.embed(at, self.params[-1].to(dtype) if self.w[-1].dtype != dtype else self.w[-1])
@@ -157,9 +160,10 @@ class Student:
         return torch.stack(losses) if losses else torch.empty(0, device=X.device)
 
     # ------------------------------------------------------------- serving
-    def quantize(self, codes="int8"):
-        """Lays the weights out in 8 bits (once; a later fit() drops them): whole numbers with a scale per output, or
-        "e4m3", floating point with a scale per 128 x 128."""
+    def quantize(self, codes=None):
+        """Lays the weights out in 8 bits (once; a later fit() drops them): "int8", whole numbers with a scale per
+        output, or "e4m3", floating point with a scale per 128 x 128 (None: those of the last call, int8 at first)."""
+        codes = self.codes if codes is None else codes
         if codes not in ("int8", "e4m3"):
             raise ops.PackError(f"unknown codes {codes!r}")
         self.codes = codes

@@ -80,8 +80,8 @@ def _check_gradient(dy, idx, rows, scale, dtype):
     return got
 
 
-# one workgroup's sort (1024, 4096 and 16,384 tokens at most) and the long one, digits of 8 and 11 bits, chunks of 16 and
-# more, rows over chunks, one group of columns and several
+# one workgroup's sort (1024 and 4096 tokens at most) and the long one (blocks of 256 and of 4096), digits of 8 and of
+# 11 bits, chunks of 16 and more, rows over chunks, one group of columns and several
 @pytest.mark.parametrize("dtype", DTYPES, ids=IDS)
 @pytest.mark.parametrize("kind", ["any", "one", "few", "holes", "none"])
 @pytest.mark.parametrize("tokens,rows,cols,pad,shift", [
@@ -96,7 +96,8 @@ def test_gradient(tokens, rows, cols, pad, shift, kind, dtype):
     _check_gradient(dy, idx, rows, 3.0, dtype)
 
 
-@pytest.mark.parametrize("tokens,rows,cols", [(1_000_000, 1600, 8), (700_001, 5_000_000, 4)])
+@pytest.mark.parametrize("tokens,rows,cols", [(1_000_000, 1600, 8), (700_001, 5_000_000, 4), (300_000, 2, 8),
+                                              (262_145, 40, 130)])
 def test_gradient_of_long_lists(tokens, rows, cols):
     print(f"[embed] gradient {tokens} of {rows}x{cols}", flush=True)
     g = torch.Generator(device="cuda").manual_seed(tokens)

@@ -18,6 +18,13 @@ def test_unknown_codes():
         student.Student(8, 3, blocks=1, hidden=4, device="cpu").quantize("int4")
 
 
+def test_missing_columns():
+    s = student.Student(8, 3, blocks=1, hidden=4, device="cpu", columns=(5, 6))
+    for columns in (None, torch.zeros(2, 1), torch.zeros(3, 2)):
+        with pytest.raises(tabpack.PackError, match="columns"):
+            s.forward(torch.zeros(2, 8), columns)
+
+
 def test_parameters():
     s = student.Student(8, 3, blocks=1, hidden=4, device="cpu", norm="layer", columns=(5, 6), d_column=2)
     assert [tuple(p.shape) for p in s.params] == [(12,), (8, 12), (12, 4), (12,), (3, 12), (12,), (12,), (11, 2)]
