@@ -35,8 +35,17 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
+# The current device's number without torch's check that the GPU is initialised (a device tensor is in hand).
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _fail(msg):
     raise PackError(msg)
+
+
+@functools.lru_cache(maxsize=None)
+def _function(fn):
+    return getattr(tabpack.load_library(), fn)
 
 
 def _matrix(t, name, dtype=None, shape=None):
@@ -83,8 +92,8 @@ def _call(fn, like, others, *args):
     if lost:
         _fail("a tensor requires a gradient, which the operators do not record: call them under torch.no_grad() and "
               "take gradients from their backward calls")
-    call = getattr(tabpack.load_library(), fn)
-    if dev == torch.cuda.current_device():
+    call = _function(fn)
+    if dev == _current_device():
         rc = call(*args, _raw_stream(dev))
     else:
         with torch.cuda.device(dev):
@@ -103,6 +112,11 @@ def _bytes(fn, *args):
 
 def _empty(like, *shape, dtype=None):
     return like.new_empty(shape, dtype=dtype)
+
+
+def _empty_as(x):
+    """A dense tensor of a matrix's shape and type (the shorter way where the matrix is dense itself)."""
+    return torch.empty_like(x) if x.is_contiguous() else x.new_empty(x.shape)
 
 
 def _norm_inputs(x, weight, residual):
@@ -291,9 +305,9 @@ def add_layer_norm(x, weight, bias=None, residual=None, eps=1e-5):
     mean and rstd fp32 [rows]."""
     xp, ldx, rp, ldr, wp, prec, rows, cols = _norm_inputs(x, weight, residual)
     bp = None if bias is None else _vector(bias, "bias", cols)
-    v = x if residual is None else _empty(x, rows, cols)
-    y = _empty(x, rows, cols)
-    mean, rstd = _empty(x, rows, dtype=torch.float32), _empty(x, rows, dtype=torch.float32)
+    v = x if residual is None else _empty_as(x)
+    y, mean = _empty_as(x), _empty(x, rows, dtype=torch.float32)
+    rstd = torch.empty_like(mean)
     _call("pack_add_layer_norm", x, (weight, bias, residual), xp, ldx, rp, ldr, wp, bp, prec, rows, cols, float(eps),
           None if residual is None else v.data_ptr(), cols, y.data_ptr(), cols, mean.data_ptr(), rstd.data_ptr())
     return y, v, mean, rstd
@@ -308,8 +322,8 @@ def layer_norm_backward(dy, v, weight, mean, rstd, dv=None):
     rows, cols = v.shape
     dp, ldd = (None, 0) if dv is None else _matrix(dv, "dv", v.dtype, v.shape)
     wp, mp, rp = _vector(weight, "weight", cols), _vector(mean, "mean", rows), _vector(rstd, "rstd", rows)
-    dx, sums = _empty(v, rows, cols), _empty(v, 2, cols, dtype=torch.float32)
-    dw, db = sums.unbind()
+    dx, dw = _empty_as(v), torch.empty_like(weight)
+    db = torch.empty_like(weight)
     work = _empty(v, _bytes("pack_layer_norm_backward_workspace_size", rows, cols), dtype=torch.uint8)
     _call("pack_layer_norm_backward", v, (dy, weight, mean, rstd, dv), yp, ldy, vp, ldv, wp, mp, rp, dp, ldd, prec,
           rows, cols, dx.data_ptr(), cols, dw.data_ptr(), db.data_ptr(), work.data_ptr(), work.numel())
@@ -335,7 +349,7 @@ def dropout(x, p, seed, step, site=0, residual=None):
         _fail("seed must lie in [0, 2^64)")
     if not 0 <= site < 1 << 32:
         _fail("site must lie in [0, 2^32)")
-    y = _empty(x, rows, cols)
+    y = _empty_as(x)
     _call("pack_dropout", x, (residual, step if at else None), xp, ldx, rp, ldr, prec, rows, cols, float(p), int(seed),
           number, at, int(site), y.data_ptr(), cols)
     return y
