@@ -43,8 +43,9 @@
 // multiply-add an element with the row's scale times the columns': 64 of them
 // a step and 64 x 64 block beside 8 MFMAs of 64 cycles, hidden behind them.  8192
 // a side 481 us, 2.28 PFLOP/s (a library product with one scale in all 2.62; whole
-// numbers 440 us), 128 x 128 tiles 567; results in fp32 956 (see f8x_t).  20,011 x 1024 ->
-// 4096 gated 213 us, of which the gate epilogues a third: nothing covers them.
+// numbers 440 us), 128 x 128 tiles 567; results in fp32 956 (see f8x_t).  20,011 x
+// 1024 -> 4096 gated 204 us (8 steps a tile of 1.7 us; start and epilogue, which
+// nothing covers, 7).
 // MFMAs: v_mfma_f32_32x32x16_bf16, v_mfma_i32_32x32x32_i8, v_mfma_f32_32x32x64_f8f6f4,
 // v_mfma_f32_32x32x2_f32, with B as the first operand, so that a lane holds 4
 // consecutive columns of one row of C.  Accumulators are fp32 or int32, added
@@ -1158,6 +1159,58 @@ __device__ __forceinline__ void tie(float (&f)[4]) {
   asm volatile("" : "+v"(f[0]), "+v"(f[1]), "+v"(f[2]), "+v"(f[3]));
 }
 
+// 8-bit floating point, gated, whole tiles: a wave's 128 x 64 sums to 128 x 32
+// outputs in bf16 without LDS.  A lane holds the gate and the up sums of columns
+// 8 q + 4 (lane / 32) .. + 3 of row lane % 32 of a 32 x 32 block; two q's results,
+// exchanged between the halves of the wave, are 8 columns of a row in each lane.
+// 20,011 x 1024 -> 4096 gated 204 us, through LDS 214; plain outputs, whose rows have twice the
+// bytes and which have nothing to compute, are faster through LDS (20,011 x 1024
+// -> 8192 211 us, this way 218).
+__device__ __forceinline__ void f8_gate_out(const MmArgs& a, const f32x16 (&acc)[2][2][2], int m0, int n0, int lane) {
+  const int hi = lane >> 5;
+  // of piece p, 16 columns, the lane's sums are columns n .. n + 3 and n + 8 .. n + 11 with n = n0 + 16 p + 4 hi
+  float bg[2][8], bu[2][8];
+#pragma unroll
+  for (int p = 0; p < 2; ++p)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int n = n0 + 16 * p + 4 * hi + e + (e & 4);
+      bg[p][e] = a.bias ? a.bias[n] : 0.0f;
+      bu[p][e] = a.bias ? a.bias[a.N + n] : 0.0f;
+    }
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int m = m0 + 64 * h + 32 * i + (lane & 31);
+      u32x4 v[2];
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        float c[8], u[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          c[e] = acc[h][i][0][8 * p + e] + bg[p][e];
+          u[e] = acc[h][i][1][8 * p + e] + bu[p][e];
+        }
+        gate8(a.act, c, u);
+        bf16x8 o;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = (__bf16)c[e];
+        const u32x4 w = __builtin_bit_cast(u32x4, o);
+        // the upper half's first pair of words for the lower half's second one
+        const auto x = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+        const auto y = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+        v[p] = u32x4{x[0], y[0], x[1], y[1]};
+      }
+      // (a row's pieces one behind the other: they share a line)
+      if (m < a.M) {
+        __bf16* const out = static_cast<__bf16*>(a.out) + (int64_t)m * a.ldo + n0 + 8 * hi;
+        *reinterpret_cast<u32x4_any*>(out) = v[0];
+        *reinterpret_cast<u32x4_any*>(out + 16) = v[1];
+      }
+    }
+}
+
 // 256 x 256 tiles on 8 waves (2 x 4, two to a SIMD), each 128 x 64.  A K step
 // is two phases, one half (64 x 64) of the wave's sums each; a phase is a read
 // part (the half's fragments from LDS) and a product part (16 MFMAs, with the
@@ -1328,7 +1381,13 @@ __device__ __forceinline__ void huge_tile(const MmArgs& a, uint32_t block, char*
     }
   }
   if (wm == 0) bar();
-  wait_vm<0, true>();
+  wait_vm<0, true>();  // (no load to LDS may outlive the workgroup's hold on it)
+  if constexpr (EPI == MM_F8_GATE) {
+    if (a.splits == 1 && n0 + 128 <= a.N) {  // (the same for the whole workgroup)
+      f8_gate_out(a, acc, m0 + wm * 128, n0 + wn * 32, lane);
+      return;
+    }
+  }
   bar();  // the sums are staged in the operand regions
   huge_out<EPI, T>(a, acc, smem + wave * 16384, m0 + wm * 128, n0 + wn * (is_gate(EPI) ? 32 : 64), w.split, lane);
 }

@@ -22,7 +22,7 @@
 // Measured: 65,536 tokens of 100,003 x 512 bf16 looked up in 18 us; the gradient
 // of 16,384 tokens of 32,000 x 1024 bf16 47 us (sort and zeros 24, six launches of 5
 // to 8 us; sums 14, at 3.3 TB/s; join 7), of 1,000,000 tokens of 1600 x 32 fp32 75 (count 9, scan 4,
-// move 16, sums 32, at 4.1 TB/s of gathered rows of 128 bytes, join 10).
+// move 16, sums 32, at 4.1 TB/s of gathered rows of 128 bytes, join 11).
 #include <algorithm>
 
 #include "ops_internal.h"
@@ -564,14 +564,17 @@ BwdPlan plan(int prec, int64_t tokens, int64_t rows, int32_t cols) {
   const int64_t vectors = ((int64_t)cols + ve - 1) / ve;
   while (p.sum.g < 6 && ((int64_t)1 << p.sum.g) < vectors) ++p.sum.g;
   p.sum.columns = (int)((vectors + (1 << p.sum.g) - 1) >> p.sum.g);
-  // chunks for some 4096 waves, of 16 to 1024 tokens
+  // chunks for some 4096 waves (1,000,000 tokens of 1600 x 32 fp32: as fast with 2048, 8192 3 us slower), of 16 to
+  // 1024 tokens; larger ones where rows have thousands of chunks, whose parts are joined one after the other
   int64_t chunk = 16;
   while (chunk < 1024 && tokens * p.sum.columns * (1 << p.sum.g) / 64 > 4096 * chunk) chunk *= 2;
+  while (chunk < 128 && tokens > 4096 * chunk * rows) chunk *= 2;
   p.sum.chunk = (int)chunk;
   p.sum.chunks = (int)((tokens + chunk - 1) / chunk);
   p.sum.ldp = vectors * ve;
   // blocks of the join: as many as the chip holds at a time, of 1 to 16 chunks; large ones where a row takes
-  // many threads, or has hundreds of chunks (1,000,000 tokens of 2 x 32 fp32 103 us, with 256 threads 255)
+  // many threads, or has hundreds of chunks (1,000,000 tokens of 2 x 32 fp32 69 us; in chunks of 32 103, and with
+  // 256 threads 255)
   p.sum.many = p.sum.g >= 5 || tokens > 256 * chunk * rows;
   p.sum.per = 1;
   const int64_t held = p.sum.many ? 512 : 4096;
