@@ -588,7 +588,11 @@ int pack_quantize_tiles(const void* x, int64_t ldx, int32_t precision, int64_t r
 
 /* Product of such codes, block by block of the depth:
  *   out[m, n] = sum_b x_scale[b, m] w_scale[n / 128, b] sum_(k in block b) x[m, k] w[n, k] (+ bias[n])
- * with sums in fp32.
+ * with sums in fp32.  In PACK_PREC_FP32 the products are exact.  In
+ * PACK_PREC_BF16 the matrix instructions for 8-bit codes form them: those add 8
+ * products at a time and cut each off 13 bits below the largest one's exponent,
+ * so that a sum loses up to 2^-10 of its terms' magnitudes (3e-5 of the results'
+ * norm on normally distributed data, where the rounding to bf16 takes 1.7e-3).
  *   gate     -1: w holds `outputs` rows; PACK_ACT_*: w, w_scale and bias hold
  *            gate rows, then up rows (w_scale as of 2 parts), and out is
  *            act(gate value) up value

@@ -428,7 +428,9 @@ def quantize_tiles(w, gated=False):
 def f8_matmul(q, scale, w, w_scale, bias=None, gate=None, dtype=torch.bfloat16):
     """x w^T (+ bias) of e4m3 codes q [rows, depth] and w [outputs, depth] with the scales of quantize_blocks and
     quantize_tiles, sums in fp32; [rows, outputs] in ``dtype``.  gate: an activation name; w, w_scale and bias then hold
-    the gate rows and the up rows (``quantize_tiles(w, gated=True)``), and the result is act(gate) * up."""
+    the gate rows and the up rows (``quantize_tiles(w, gated=True)``), and the result is act(gate) * up.  Results in
+    float32 are summed from exact products, at half the rate; those in bfloat16 by the instructions for 8-bit codes,
+    which cut off what lies 13 bits below the largest of 8 products (include/tabpack.h)."""
     qp, ldq = _matrix(q, "q", _E4M3)
     rows, depth = q.shape
     wp, ldw = _matrix(w, "w", _E4M3)
