@@ -1358,6 +1358,8 @@ __device__ __forceinline__ void huge_tile(const MmArgs& a, uint32_t block, char*
     fa.template read4<1>(x1, slot * kRegion);
     fb.template read4<0>(y0, after(slot, 1) * kRegion);
     fb.template read4<0>(y1, after(slot, 2) * kRegion);
+    // (8-bit floating point: four loads of row scales a step, asked for before the phase's reads, lie among the
+    // newest: they are single words 128 bytes apart, so their number is fixed)
     products(acc[0], std::integral_constant<int, 0>{}, std::integral_constant<int, kF8<T> ? 12 : 8>{}, [&](int q) {
       if (q < 2)
         ask_a(0, kt + 2, after(slot, 8), q);
