@@ -6,9 +6,9 @@
 // Backward: dtable[v] = scale sum over the t with idx[t] = v of dy[t].  The
 // tokens are sorted by index, stably, so that each row's tokens lie together in
 // the order of the batch; chunks of the sorted list are then summed in fp32 by
-// groups of threads that own columns, dy's rows read once each.  A row whose
-// tokens lie in one chunk is written from its registers; parts of a row that
-// crosses chunks go to memory and a last kernel adds them up in order.  No atomics
+// groups of threads that own columns, dy's rows read once each.  A row of
+// few tokens is written from its registers; parts of one that takes several chunks go
+// to memory and a last kernel adds them up in a fixed order.  No atomics
 // on sums, so the result does not change between runs.  Rows that no token names
 // are zeros, written while the sort runs (it occupies a few CUs and is
 // latency; the table's bytes are bandwidth).
@@ -21,7 +21,7 @@
 //
 // Measured: 65,536 tokens of 100,003 x 512 bf16 looked up in 18 us; the gradient
 // of 16,384 tokens of 32,000 x 1024 bf16 47 us (sort and zeros 24, six launches of 5
-// to 8 us; sums 14, at 3.3 TB/s; join 7), of 1,000,000 tokens of 1600 x 32 fp32 75 (count 9, scan 4,
+// to 8 us; sums 15, at 3.3 TB/s; join 8), of 1,000,000 tokens of 1600 x 32 fp32 72 (count 8, scan 4,
 // move 16, sums 32, at 4.1 TB/s of gathered rows of 128 bytes, join 11).
 #include <algorithm>
 
@@ -218,17 +218,18 @@ __global__ __launch_bounds__(1024) void sort_one_kernel(EmbedBwdArgs a, Token* l
 }
 
 // Longer lists, a digit of DB bits in two launches or three: blocks of NT IPT
-// tokens count theirs, then move them.  Up to kDirect blocks a move adds up the
-// counts of the blocks before its own by itself (each block counting the whole
-// list instead of a launch of their own for the counts: 16,384 tokens of 32,000 x
-// 1024 49 us, this way 47), past that a launch between them does.  The blocks
-// behind the sort's write zeros.  What bounds the moves of a long list is its
+// tokens count theirs, then move them.  Up to kDirect blocks of 256 threads (65,536
+// tokens) a move adds up the counts of the blocks before its own by itself; blocks
+// of 1024 threads take a launch between for that (65,536 tokens of 200,000 x 128 in
+// 16 of them 61 us, in 64 small ones 45; each block counting the whole list instead
+// of a launch for the counts: 16,384 tokens of 32,000 x 1024 49 us, this way 47).  The
+// blocks behind the sort's write zeros.  What bounds the moves of a long list is its
 // scattered stores: larger blocks have longer runs of a digit.
 constexpr uint32_t kDirect = 64;
 struct SortArgs {
   const Token* list;
   Token* out;
-  uint32_t* counts;  // up to kDirect blocks [blocks, digits], past that [digits, blocks]; behind a scan: those before
+  uint32_t* counts;  // small blocks: [blocks, digits]; large ones: [digits, blocks], behind a scan those before
   uint32_t* totals;  // [digits] (with a scan)
   uint32_t blocks;
   int shift, round, launch, launches;  // (launches: those that write zeros)
@@ -265,7 +266,7 @@ __global__ __launch_bounds__(NT) void sort_count_kernel(EmbedBwdArgs a, SortArgs
     if (token[j].key != kNoKey) atomicAdd(&count[(token[j].key >> s.shift) & ((1 << DB) - 1)], 1u);
   __syncthreads();
   // (in the order in which a move, or the scan, reads them)
-  const int64_t of_digit = s.blocks <= kDirect ? 1 : s.blocks, of_block = s.blocks <= kDirect ? 1 << DB : 1;
+  const int64_t of_digit = NT == 256 ? 1 : s.blocks, of_block = NT == 256 ? 1 << DB : 1;
   for (int d = threadIdx.x; d < 1 << DB; d += NT) s.counts[d * of_digit + blockIdx.x * of_block] = count[d];
 }
 // A block: one digit's counts over the blocks of tokens, to those of the blocks before each.
@@ -545,7 +546,7 @@ int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 // How a gradient is laid out over launches, and its workspace.
 struct BwdPlan {
   int bits, digit, rounds;  // of the keys, of a digit, digits
-  bool wide;                // blocks of 4096 tokens, not of 256
+  int tile;                 // tokens of a block of the long sort
   uint32_t blocks;          // of tokens in the long sort
   SumArgs sum;
   size_t counts, totals, partial, bytes;  // byte offsets
@@ -555,11 +556,10 @@ BwdPlan plan(int prec, int64_t tokens, int64_t rows, int32_t cols) {
   const int ve = prec == PACK_PREC_BF16 ? 8 : 4;
   while (p.bits < 32 && (rows >> p.bits) > 0) ++p.bits;  // keys 0 .. rows
   const bool one = tokens <= kSortOne;
-  p.wide = tokens > 256 * (int64_t)kDirect;
-  const int64_t tile = p.wide ? 4096 : 256;
-  p.blocks = one ? 0 : (uint32_t)((tokens + tile - 1) / tile);
-  // digits of 8 bits, or of 11 where that saves a round
-  p.digit = p.wide && (p.bits + 10) / 11 < (p.bits + 7) / 8 ? 11 : 8;
+  p.tile = tokens <= 256 * (int64_t)kDirect ? 256 : tokens <= 1024 * (int64_t)kDirect ? 1024 : 4096;
+  p.blocks = one ? 0 : (uint32_t)((tokens + p.tile - 1) / p.tile);
+  // digits of 8 bits, or in the largest blocks of 11 where that saves a round
+  p.digit = p.tile == 4096 && (p.bits + 10) / 11 < (p.bits + 7) / 8 ? 11 : 8;
   p.rounds = (p.bits + p.digit - 1) / p.digit;
   const int64_t vectors = ((int64_t)cols + ve - 1) / ve;
   while (p.sum.g < 6 && ((int64_t)1 << p.sum.g) < vectors) ++p.sum.g;
@@ -583,7 +583,7 @@ BwdPlan plan(int prec, int64_t tokens, int64_t rows, int32_t cols) {
   p.counts = at;
   at += (size_t)up(((int64_t)p.blocks << p.digit) * 4, 16);
   p.totals = at;
-  at += p.blocks <= kDirect ? 0 : (size_t)4 << p.digit;
+  at += one || p.tile < 4096 ? 0 : (size_t)4 << p.digit;
   p.partial = at;
   if (p.sum.chunks > 1) at += (size_t)p.sum.chunks * 2 * (size_t)p.sum.ldp * 4;
   p.bytes = at;
@@ -603,9 +603,9 @@ hipError_t sort_long(const EmbedBwdArgs& a, const BwdPlan& p, SortArgs s, Token*
     s.launch = 2 * s.round;
     hipLaunchKernelGGL((sort_count_kernel<T, DB, NT, IPT>), grid, block, 0, st, a, s);
     ++s.launch;
-    if (p.blocks <= kDirect) {
+    if constexpr (NT == 256) {  // (up to kDirect blocks)
       hipLaunchKernelGGL((sort_move_kernel<T, DB, NT, IPT, true>), grid, block, 0, st, a, s);
-    } else if constexpr (IPT > 1) {
+    } else {
       hipLaunchKernelGGL(sort_scan_kernel, dim3(1 << DB), dim3(256), 0, st, s);
       hipLaunchKernelGGL((sort_move_kernel<T, DB, NT, IPT, false>), grid, block, 0, st, a, s);
     }
@@ -633,8 +633,10 @@ hipError_t embed_bwd_t(int prec, const EmbedBwdArgs& a, hipStream_t st) {
     SortArgs s{};
     s.counts = reinterpret_cast<uint32_t*>(w + p.counts), s.totals = reinterpret_cast<uint32_t*>(w + p.totals);
     s.blocks = p.blocks;
-    if (!p.wide)
+    if (p.tile == 256)
       e = sort_long<T, 8, 256, 1>(a, p, s, buf, st);
+    else if (p.tile == 1024)
+      e = sort_long<T, 8, 256, 4>(a, p, s, buf, st);
     else
       e = p.digit == 8 ? sort_long<T, 8, 1024, 4>(a, p, s, buf, st) : sort_long<T, 11, 1024, 4>(a, p, s, buf, st);
     last = (p.rounds + 1) & 1;

@@ -80,14 +80,14 @@ def _check_gradient(dy, idx, rows, scale, dtype):
     return got
 
 
-# one workgroup's sort (1024 and 4096 tokens at most) and the long one (blocks of 256 and of 4096), digits of 8 and of
-# 11 bits, chunks of 16 and more, rows over chunks, one group of columns and several
+# one workgroup's sort (1024 and 4096 tokens at most) and the long one (blocks of 256, 1024 and 4096), digits of 8
+# and of 11 bits, chunks of 16 and more, rows over chunks, one group of columns and several
 @pytest.mark.parametrize("dtype", DTYPES, ids=IDS)
 @pytest.mark.parametrize("kind", ["any", "one", "few", "holes", "none"])
 @pytest.mark.parametrize("tokens,rows,cols,pad,shift", [
     (1, 1, 1, 0, 0), (17, 300, 5, 0, 0), (1024, 255, 32, 0, 0), (1025, 256, 40, 3, 1), (4097, 70_000, 24, 0, 0),
     (16_384, 3000, 96, 8, 8), (16_385, 2047, 36, 0, 0), (20_000, 2048, 700, 0, 0), (50_001, 66_000, 9, 1, 1),
-    (30_000, 2, 1100, 0, 0)])
+    (30_000, 2, 1100, 0, 0), (65_536, 70_000, 12, 0, 0), (65_537, 2047, 20, 0, 0), (70_001, 2048, 5, 2, 1)])
 def test_gradient(tokens, rows, cols, pad, shift, kind, dtype):
     print(f"[embed] gradient {tokens} of {rows}x{cols} pad {pad} {kind} {dtype}", flush=True)
     g = torch.Generator(device="cuda").manual_seed(tokens * 7 + cols)
