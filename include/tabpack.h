@@ -514,13 +514,15 @@ int pack_q8_matmul(const int8_t* x, int64_t ldx, const float* x_scale, const int
  *   out          device [rows, cols]
  *   mean_out, rstd_out  device fp32 [rows]: mu and rho, for the backward pass, or NULL
  * Holds for every finite v, also where a sum or square is past the largest fp32
- * value.  A row that holds an infinity or NaN is NaN.  cols <= PACK_ROW_MAX_COLS,
- * eps >= 0 (with eps = 0 a row of equal values is NaN). */
+ * value, and where the mean is large beside the deviation: mu enters out and
+ * rstd_out unrounded.  A row that holds an infinity or NaN is NaN.
+ * cols <= PACK_ROW_MAX_COLS, eps >= 0 (with eps = 0 a row of equal values is NaN). */
 int pack_add_layer_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr, const float* weight,
                         const float* bias, int32_t precision, int64_t rows, int32_t cols, float eps, void* sum_out,
                         int64_t lds, void* out, int64_t ldo, float* mean_out, float* rstd_out, hipStream_t stream);
 
-/* Its gradients from its sum v (as it was stored), mu and rho: with
+/* Its gradients from its sum v, mu and rho as they were stored (so n carries the
+ * roundings of v and of mu, 2^-24 |mu| rho of the latter): with
  * n = (v - mu) rho and g = weight dy,
  *   dx = rho (g - sum_c g / cols - n sum_c g n / cols) + dsum   (of x and of the residual)
  *   dweight = sum over the rows of dy n,  dbias = sum over the rows of dy
