@@ -48,10 +48,12 @@ __device__ __forceinline__ void reduce_row2(float& p, float& q, float* red, floa
 // step of the mean; values lie on steps no smaller than that unless the deviation is
 // of the mean's size, so then e^2 is at most the variance.  (Against one sum of the
 // differences' squares, in turn on one card: 65,536 x 1024 bf16 94 us both ways,
-// 500,000 x 64 66 -> 68.)
+// 500,000 x 64 67 -> 71.)
 // Where a sum or a square overflows (values past 1.8e19) the row goes on 2^-80
-// times smaller, which does not change y; a row that holds an infinity or NaN
-// is NaN throughout.
+// times smaller, and where squares leave fp32's range at its lower end (with an
+// eps there too) 2^80 times larger, neither of which changes y.  A row of equal
+// values has no differences, whatever its scale, and eps alone makes its rho.  A
+// row that holds an infinity or NaN is NaN throughout.
 template <typename T, int G, int EPT>
 __global__ __launch_bounds__(G > 256 ? G : 256) void layer_norm_kernel(LayerNormArgs a) {
   constexpr int VE = kVec<T>, NT = G > 256 ? G : 256, RPB = NT / G, NV = EPT / VE;
@@ -107,14 +109,15 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void layer_norm_kernel(LayerNorm
     const float n = (float)a.cols;
     float shift = reduce_row<G, OpAdd>(total, red[turn][0], tid) / n;
     about(shift, 1);
-    float e1 = s1 / n, down = 1.0f;
-    if (!(s2 < __builtin_inff()) || e1 * s1 > 0x1p-12f * (s2 + n * a.eps)) {  // (the same for all threads of the row)
-      if (!(s2 < __builtin_inff())) {
-        down = 0x1p-80f;
+    float e1 = s1 / n, by = 1.0f;
+    const bool over = !(s2 < __builtin_inff()), under = s2 + n * a.eps < 0x1p-100f && fabsf(shift) < 1.0f;
+    if (over || under || e1 * s1 > 0x1p-12f * (s2 + n * a.eps)) {  // (the same for all threads of the row)
+      if (over || under) {
+        by = over ? 0x1p-80f : 0x1p80f;
         total = 0.0f;
 #pragma unroll
         for (int e = 0; e < EPT; ++e) {
-          v[e] *= down;
+          v[e] *= by;
           total += v[e];
         }
         shift = reduce_row<G, OpAdd>(total, red[turn][3], tid) / n;
@@ -131,9 +134,10 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void layer_norm_kernel(LayerNorm
     }
     float var = s2 / n - e1 * e1;
     var = var < 0.0f ? 0.0f : var;  // (NaN stays)
-    const float rho = 1.0f / sqrtf(var + a.eps * down * down), rstd = rho * down;
+    const float rho = 1.0f / sqrtf(s2 == 0.0f ? a.eps : var + a.eps * by * by), rstd = s2 == 0.0f ? rho : rho * by;
     float mean = shift + e1;
-    if (down < 1.0f) {
+    if (by > 1.0f) mean *= 0x1p-80f;
+    if (by < 1.0f) {
       // (a mean of the largest values may round past them)
       const float m = mean * 0x1p80f;
       mean = fabsf(m) == __builtin_inff() && fabsf(mean) < 0x1p49f ? copysignf(3.402823466e38f, m) : m;

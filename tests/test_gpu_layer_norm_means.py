@@ -71,3 +71,41 @@ def test_equal_values(cols):
     assert float((y - b).abs().max()) <= 4 * U + 2 * U * float(b.abs().max())
     assert float((mean / x[:, 0] - 1).abs().max()) <= 2 * U
     assert float((rstd * 1e-5 ** 0.5 - 1).abs().max()) <= 130 * U
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("cols", COLS)
+def test_equal_values_at_the_ends_of_the_range(cols, dtype):
+    """Where the row goes on at another scale: its bias all the same, with eps of any size that a root has."""
+    x = torch.tensor([1e22 / 7, -3e30, 3.3e38, 1e-30, 1e-42, 0.0], device="cuda").to(dtype)
+    x = x[:, None].expand(6, cols).contiguous()
+    b = torch.randn(cols, device="cuda")
+    for eps in (1e-5, 1e-37, 1e30):
+        y, _, mean, rstd = ops.add_layer_norm(x, torch.ones(cols, device="cuda"), b, eps=eps)
+        assert torch.equal(y, b.to(dtype).expand(6, cols))
+        # (past half of the largest value a sum of the scaled row may round to the next step)
+        assert float((mean.double() - x[:, 0].double()).abs().max()) <= 2 * U * 3.3e38
+        assert bool(((mean - x[:, 0].float()).abs() <= 2 * U * x[:, 0].float().abs())[:4].all())
+        assert float((rstd.double() * eps ** 0.5 - 1).abs().max()) <= 4 * U
+    y, _, _, _ = ops.add_layer_norm(x, torch.ones(cols, device="cuda"), b, eps=0.0)
+    assert bool(y.isnan().all())
+
+
+@pytest.mark.parametrize("size", [1e-18, 1e-23, 1e-30, 1e-36])
+@pytest.mark.parametrize("cols", COLS)
+def test_small_deviations(cols, size):
+    """Squares below fp32's smallest value, without an eps that would outweigh them: the norm is what it is at any other
+    scale."""
+    g = torch.Generator(device="cuda").manual_seed(cols)
+    x = size * (1 + torch.randn(9, cols, generator=g, device="cuda"))
+    for eps in (0.0, 1e-42):  # (1e-42: not seen beside 1e-36; beside 1e-72 all there is)
+        s = x.double()
+        mu = s.mean(1, keepdim=True)
+        at = float(torch.tensor(eps, dtype=torch.float32))
+        dev = ((s - mu).square().mean(1, keepdim=True) + at).sqrt()
+        n = (s - mu) / dev
+        y, _, mean, rstd = ops.add_layer_norm(x, torch.ones(cols, device="cuda"), eps=eps)
+        # (values of 1e-36 have their own steps of 2^-149, below 130 U of them)
+        assert float(((y.double() - n).abs() / (130 * U * (1 + n.abs()))).max()) <= 1
+        assert float((mean.double() - mu[:, 0]).abs().max()) <= 130 * U * size * 4
+        assert float((rstd.double() * dev[:, 0] - 1).abs().max()) <= 130 * U
