@@ -543,7 +543,10 @@ int pack_layer_norm_backward(const void* dy, int64_t ldy, const void* sum, int64
  * (seed mod 2^32, (seed >> 32) xor 2^30) is at least floor(p 2^16): the mask
  * depends on (seed, step, site, r, c) alone.  The gradient of x is the same call
  * on dy without a residual; the residual's is dy itself.
- *   p        in [0, 1]; 0 keeps every element, 1 none
+ *   p        in [0, 1]; 0 keeps every element, 1 none.  The share kept is 1 - p
+ *            rounded up to a multiple of 2^-16, so the mean of what is kept is past
+ *            x's by up to 2^-16 / (1 - p) of it; a p for which that would be more
+ *            than 2^-8 is refused (all up to 1 - 2^-8 are taken)
  *   site     which dropout of a network this is (one step's masks differ by it)
  *   step_at  device int64 or NULL: the step, read when the kernel runs (a
  *            captured graph then draws new masks at each replay); NULL: step

@@ -407,6 +407,11 @@ int pack_dropout(const void* x, int64_t ldx, const void* residual, int64_t ldr, 
   if (rows < 0 || rows > kMaxExtent) return bad("rows=%lld out of [0, 2^31 - 1]", (long long)rows);
   if (cols < 1) return bad("cols=%d must be positive", cols);
   if (!(p >= 0.0 && p <= 1.0)) return bad("p must lie in [0, 1]");
+  const uint32_t threshold = (uint32_t)(p * 65536.0);
+  // (near 1 the draws' 16 bits no longer tell p from its neighbours: a p of 1 - 1e-6 would keep 15 times too many)
+  if (p < 1.0 && (65536 - threshold) / 65536.0 > (1.0 + 1.0 / 256) * (1.0 - p))
+    return bad("p=%.17g must lie nearer to a multiple of 2^-16: elements are kept by draws of 16 bits, of which the share "
+               "kept would be past 1 - p by more than one part in 256", p);
   if (!ld_ok(ldx, cols) || (residual && !ld_ok(ldr, cols)) || !ld_ok(ldo, cols))
     return bad("a leading dimension is smaller than cols=%d or too large", cols);
   if (step_at && !aligned(step_at, 8)) return bad("step_at must be 8-byte aligned");
@@ -415,7 +420,7 @@ int pack_dropout(const void* x, int64_t ldx, const void* residual, int64_t ldr, 
   constexpr uint32_t kTag = 4;  // (the packs' streams have tags 1 to 3)
   DropoutArgs a{};
   a.x = x, a.ldx = ldx, a.residual = residual, a.ldr = ldr, a.out = out, a.ldo = ldo, a.rows = rows, a.cols = cols;
-  a.threshold = (uint32_t)(p * 65536.0), a.scale = p < 1.0 ? (float)(1.0 / (1.0 - p)) : 0.0f;
+  a.threshold = threshold, a.scale = p < 1.0 ? (float)(1.0 / (1.0 - p)) : 0.0f;
   a.key0 = (uint32_t)seed, a.key1 = (uint32_t)(seed >> 32) ^ (kTag << 28);
   a.site = site, a.step = (uint32_t)step, a.step_at = step_at;
   return done("dropout", launch_dropout(precision, a, stream));

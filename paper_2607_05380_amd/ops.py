@@ -334,7 +334,8 @@ def layer_norm_backward(dy, v, weight, mean, rstd, dv=None):
 def dropout(x, p, seed, step, site=0, residual=None):
     """y = (residual +) x / (1 - p) where an element is kept, residual (or 0) elsewhere.  The mask follows from (seed,
     step, site, row, column) alone, so nothing of it is kept: x's gradient is ``dropout(dy, p, seed, step, site)``.
-    x, residual [rows, cols]; p in [0, 1]; seed below 2^64; step (taken mod 2^32) a number, or a device tensor of one
+    x, residual [rows, cols]; p in [0, 1], taken by draws of 16 bits (the share kept is 1 - p rounded up to a multiple of
+    2^-16; a p so near to 1 that this is past it by more than one part in 256 is refused); seed below 2^64; step (taken mod 2^32) a number, or a device tensor of one
     int64, which the kernel reads when it runs: a captured graph then draws new masks at each replay; site below 2^32
     tells the dropouts of one network apart."""
     prec = _prec(x, "x")

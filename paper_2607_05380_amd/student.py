@@ -15,6 +15,7 @@ master weights, applies AdamW to them and does the head's small products in trai
     python -m paper_2607_05380_amd.student            # trains a pack, distils it, serves the student in 8 bits
 """
 import argparse
+import math
 
 import torch
 
@@ -45,6 +46,8 @@ class Student:
             raise ops.PackError(f"unknown norm {norm!r}")
         if not 0 <= dropout < 1:
             raise ops.PackError(f"dropout={dropout} must lie in [0, 1)")
+        if 1 - math.floor(dropout * 65536) / 65536 > (1 + 1 / 256) * (1 - dropout):
+            raise ops.PackError(f"dropout={dropout} is too near to 1 for draws of 16 bits (see ops.dropout)")
         if dtype not in (torch.bfloat16, torch.float32):
             raise ops.PackError(f"dtype must be bfloat16 or float32, not {dtype}")
         g = torch.Generator(device=device).manual_seed(seed)
