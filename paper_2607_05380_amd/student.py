@@ -58,6 +58,7 @@ class Student:
 
         self.act, self.dtype, self.eps, self.classes = act, dtype, eps, classes
         self.codes = "int8"
+        self.step = 0  # training steps taken, which number the dropouts' masks
         self.layer, self.p, self.seed = norm == "layer", dropout, seed & 0xFFFFFFFFFFFFFFFF
         self.params = []
         for _ in range(blocks):
@@ -146,18 +147,20 @@ class Student:
 
     def fit(self, X, idx, teacher, steps, batch=1024, lr=2e-3, temperature=2.0, seed=0, columns=None):
         """Distils: ``steps`` AdamW steps on batches of the rows X (fp32) and their columns' classes with the teacher's
-        entries; the mean loss of each step."""
+        entries; the mean loss of each step.  Batches follow from ``seed``; the steps go on from those taken before, and with
+        them the dropouts' masks."""
         opt = torch.optim.AdamW(self.params, lr=lr, weight_decay=1e-4)
         g = torch.Generator(device=X.device).manual_seed(seed)
         weight = torch.full((batch,), 1.0 / batch, device=X.device)
         losses = []
-        for step in range(steps):
+        for _ in range(steps):
             rows = torch.randint(0, X.shape[0], (batch,), generator=g, device=X.device)
-            logits, kept = self.forward(X[rows], None if columns is None else columns[rows], step)
+            logits, kept = self.forward(X[rows], None if columns is None else columns[rows], self.step)
             loss, dlogits = ops.distill_topk(logits, idx[rows], teacher[rows], temperature, weight)
             for p, grad in zip(self.params, self.backward(dlogits, kept)):
                 p.grad = grad
             opt.step()
+            self.step += 1
             self._copies()
             losses.append(loss.sum())
         return torch.stack(losses) if losses else torch.empty(0, device=X.device)
