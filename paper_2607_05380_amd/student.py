@@ -86,6 +86,8 @@ class Student:
         """(v_0, indices into the table): the features, then each column's embedding; a class that its column does
         not have (negative, or too large) is missing: zeros."""
         if not self.columns:
+            if columns is not None:
+                raise ops.PackError("a student built without columns takes none")
             return x.to(dtype), None
         if columns is None or columns.shape != (x.shape[0], len(self.columns)):
             raise ops.PackError(f"columns must hold the classes of {len(self.columns)} columns for each row")
