@@ -79,10 +79,10 @@ class Student:
     def _copies(self):
         # products read the masters rounded to the student's type; norm weights, biases and the head stay fp32
         self.w = [p if p.dim() == 1 or i == self.head else p.to(self.dtype) for i, p in enumerate(self.params)]
-        self.served = None
+        self.served = self.served_table = None
 
     # ------------------------------------------------------------- parts
-    def _input(self, x, columns, dtype):
+    def _input(self, x, columns, dtype, table):
         """(v_0, indices into the table): the features, then each column's embedding; a class that its column does
         not have (negative, or too large) is missing: zeros."""
         if not self.columns:
@@ -93,7 +93,7 @@ class Student:
             raise ops.PackError(f"columns must hold the classes of {len(self.columns)} columns for each row")
         there = (columns >= 0) & (columns < self.sizes)
         at = torch.where(there, columns.to(torch.int32) + self.offsets, -1).reshape(-1)
-        rows = ops.embed(at, self.params[-1].to(dtype) if self.w[-1].dtype != dtype else self.w[-1])
+        rows = ops.embed(at, table)
         return torch.cat([x.to(dtype), rows.view(x.shape[0], -1)], 1), at
 
     def _norm(self, i, new, stream):
@@ -117,7 +117,7 @@ class Student:
         """(logits fp32, what backward needs) of rows x [rows, d_in] and their columns' classes [rows, columns].  step:
         that of a training step, whose masks the dropout then draws (None: no dropout)."""
         p = self.p if step is not None else 0.0
-        v, at = self._input(x, columns, self.dtype)
+        v, at = self._input(x, columns, self.dtype, self.w[-1])
         keep, branch = [], None
         for b in range(self.blocks):
             n, v, stats = self._norm(b, *((v, None) if branch is None else (branch, v)))
@@ -180,6 +180,7 @@ class Student:
         else:
             self.served = [p if p.dim() == 1 else ops.quantize_tiles(p, gated=i % 3 == 1 and i < self.head)
                            for i, p in enumerate(self.params[:self.head + 1])]
+        self.served_table = self.params[-1].to(torch.bfloat16) if self.columns else None
         return self
 
     def _codes(self, x):
@@ -197,7 +198,7 @@ class Student:
         if self.served is None:
             self.quantize()
         matmul = ops.q8_matmul if self.codes == "int8" else ops.f8_matmul
-        v, _ = self._input(X, columns, torch.bfloat16)
+        v, _ = self._input(X, columns, torch.bfloat16, self.served_table)
         branch = None
         for b in range(self.blocks):
             (wg, sg), (wd, sd) = self.served[3 * b + 1:3 * b + 3]

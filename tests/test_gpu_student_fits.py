@@ -25,3 +25,38 @@ def test_a_second_fit_goes_on_with_the_masks():
     s.fit(x, idx, teacher, steps=0, batch=64)
     s.fit(x, idx, teacher, steps=1, batch=64)
     assert steps[-1] == 5
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+def test_a_prediction_rounds_no_table(dtype):
+    """The table is laid out with the other weights, not in each prediction (its rows are many, a request's few)."""
+    from torch.utils._python_dispatch import TorchDispatchMode
+
+    class Copies(TorchDispatchMode):
+        largest = 0
+
+        def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+            out = func(*args, **(kwargs or {}))
+            if isinstance(out, torch.Tensor):
+                Copies.largest = max(Copies.largest, out.numel())
+            return out
+
+    sizes = (5000, 3000)
+    s = student.Student(12, 4, blocks=1, hidden=32, dtype=dtype, columns=sizes, d_column=16)
+    x = torch.randn(7, 12, device="cuda")
+    columns = torch.stack([torch.arange(7, device="cuda") * 700, 2999 - torch.arange(7, device="cuda")], 1)
+    columns[2, 1] = -1
+    s.quantize()
+    with Copies():
+        out = s.predict(x, columns)
+    assert 0 < Copies.largest < sum(sizes)
+    # the embeddings are those of the masters, rounded once
+    at = torch.where(columns < 0, 0, columns + torch.tensor([0, sizes[0]], device="cuda"))
+    rows = (s.params[-1][at] * (columns >= 0)[:, :, None]).bfloat16()
+    v, _ = s._input(x, columns, torch.bfloat16, s.served_table)
+    assert torch.equal(v, torch.cat([x.bfloat16(), rows.reshape(7, -1)], 1))
+    # another fit's weights serve after it
+    idx, teacher = student.teacher_entries(torch.softmax(torch.randn(7, 4, device="cuda"), 1), 3)
+    s.fit(x, idx, teacher, steps=1, batch=16, columns=columns)
+    assert not torch.equal(s.predict(x, columns), out)
+    assert torch.equal(s.served_table, s.params[-1].bfloat16())
