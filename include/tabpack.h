@@ -336,6 +336,12 @@ typedef struct pack_plan_info {
   int32_t eval_tiles[PACK_EVAL_LEVELS]; /* the tile set of their last layer's launch */
 } pack_plan_info;
 int pack_debug_plan(const pack_config* cfg, const uint8_t* active, pack_plan_info* out);
+/* How pack_f8_matmul of these sizes is laid out (no GPU): the side of its tiles (16:
+ * the thin ones of up to 16 rows; 64, 128 or 256), the workgroups that share a
+ * tile's depth, and whether its operands go straight to LDS.  aligned: whether x and
+ * w have their rows at 16 bytes. */
+int pack_debug_f8_matmul(int64_t rows, int32_t outputs, int32_t depth, int32_t gate, int32_t precision, int32_t aligned,
+                         int32_t* side, int32_t* splits, int32_t* straight);
 
 /* Per-kernel timing of pack_train_step() with HIP events recorded on the
  * stream each kernel runs on, around every launch (measurement aid; it adds

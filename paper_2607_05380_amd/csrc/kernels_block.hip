@@ -1726,6 +1726,13 @@ Plan choose(MmType type, const MmArgs& a, bool dma) {
   return e.plan;
 }
 
+// What a product is launched with.
+Plan plan_of(MmType type, const MmArgs& a, bool dma) {
+  const Plan p = choose(type, a, dma);
+  // (the registers of the largest tiles do not hold widened codes as well)
+  return type == MM_F8 && a.out_f32 && p.tiles == TILES_HUGE ? plan_with(type, a, TILES_SMALL, 1) : p;
+}
+
 size_t partial_bytes(const MmArgs& a, const Plan& p) {
   if (p.splits < 2) return 0;
   return (size_t)p.splits * (size_t)a.M * (size_t)partial_half(a.N) * (is_gate(a.epi) ? 8 : 4);
@@ -1789,9 +1796,7 @@ void launch_join(const MmArgs& a, hipStream_t s) {
 template <typename T, bool RA, bool RB, int EPI>
 hipError_t launch_tiles(MmType type, MmArgs a, hipStream_t s) {
   const bool dma = can_dma(type, a);
-  Plan p = choose(type, a, dma);
-  // (the registers of the largest tiles do not hold widened codes as well)
-  if (kWiden<T> && p.tiles == TILES_HUGE) p = plan_with(type, a, TILES_SMALL, 1);
+  const Plan p = plan_of(type, a, dma);
   const dim3 grid(apply(a, p));
   if (grid.x == 0) return hipErrorInvalidConfiguration;
   if (a.work_bytes < partial_bytes(a, p)) return hipErrorInvalidValue;
@@ -2030,6 +2035,14 @@ size_t mm_workspace(MmType type, const MmArgs& a) {
   Copy c[3];
   const size_t copied = copies_bytes(type, c, copies(type, a, nullptr, c));
   return std::max(copied + partial_bytes(a, choose(type, a, true)), partial_bytes(a, choose(type, a, false)));
+}
+
+MmLayout mm_layout(MmType type, const MmArgs& a, bool aligned) {
+  Copy c[3];
+  const bool dma = copies(type, a, nullptr, c) > 0 || (aligned && !odd_a(type, a) && !odd_b(type, a));
+  const Plan p = plan_of(type, a, dma);
+  constexpr int32_t kSide[] = {16, 64, 128, 256};
+  return {kSide[p.tiles], p.splits, dma};
 }
 
 size_t mm_pair_workspace(MmType type, const MmArgs& a, const MmArgs& b) {

@@ -487,6 +487,19 @@ int pack_f8_matmul_workspace_size(int64_t rows, int32_t outputs, int32_t depth, 
   return PACK_OK;
 }
 
+int pack_debug_f8_matmul(int64_t rows, int32_t outputs, int32_t depth, int32_t gate, int32_t precision, int32_t aligned,
+                         int32_t* side, int32_t* splits, int32_t* straight) {
+  if (!known(precision)) return bad("unknown precision %d", precision);
+  const int rc = check_f8(rows, outputs, depth, gate);
+  if (rc != PACK_OK) return rc;
+  if (!side || !splits || !straight) return bad("NULL pointer");
+  MmArgs a = mm_f8(rows, outputs, depth, gate);
+  a.out_f32 = precision == PACK_PREC_FP32;
+  const MmLayout l = mm_layout(MM_F8, a, aligned != 0);
+  *side = l.side, *splits = l.splits, *straight = l.straight;
+  return PACK_OK;
+}
+
 int pack_f8_matmul(const void* x, int64_t ldx, const float* x_scale, const void* w, int64_t ldw, const float* w_scale,
                    const float* bias, int32_t gate, int32_t precision, int64_t rows, int32_t outputs, int32_t depth,
                    void* out, int64_t ldo, void* work, size_t work_bytes, hipStream_t stream) {

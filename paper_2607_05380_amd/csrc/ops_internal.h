@@ -176,6 +176,13 @@ struct MmArgs {
 // Bytes of `work` that the product needs (0: none).
 size_t mm_workspace(MmType type, const MmArgs& a);
 hipError_t launch_mm(MmType type, const MmArgs& a, hipStream_t s);
+// How launch_mm would lay out a product of these sizes whose operands' rows lie
+// at 16 bytes, or do not: the side of its tiles (16: thin ones).
+struct MmLayout {
+  int32_t side, splits;
+  bool straight;  // to LDS
+};
+MmLayout mm_layout(MmType type, const MmArgs& a, bool aligned);
 // Two independent products of one type, a with depth-contiguous A and
 // rows-contiguous B (MM_PLAIN or MM_GATE_BWD), b with rows-contiguous operands
 // (MM_PLAIN), of the same matrix A and the same work: in one launch where that is

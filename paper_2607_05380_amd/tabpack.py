@@ -36,7 +36,7 @@ SYMBOLS = ["pack_last_error", "pack_init", "pack_destroy", "pack_get_hparams", "
            "pack_q8_matmul_workspace_size", "pack_q8_matmul", "pack_add_layer_norm",
            "pack_layer_norm_backward_workspace_size", "pack_layer_norm_backward", "pack_dropout", "pack_embed",
            "pack_embed_backward_workspace_size", "pack_embed_backward", "pack_quantize_blocks", "pack_quantize_tiles",
-           "pack_f8_matmul_workspace_size", "pack_f8_matmul"]
+           "pack_f8_matmul_workspace_size", "pack_f8_matmul", "pack_debug_f8_matmul"]
 
 
 class MemberHP(ctypes.Structure):
@@ -151,6 +151,7 @@ def load_library(path=LIB_PATH):
         "pack_quantize_blocks": ([vp, i64, i32, i64, i32, vp, i64, vp, vp], ctypes.c_int),
         "pack_quantize_tiles": ([vp, i64, i32, i64, i32, i32, vp, i64, vp, vp], ctypes.c_int),
         "pack_f8_matmul_workspace_size": ([i64, i32, i32, i32, ctypes.POINTER(sz)], ctypes.c_int),
+        "pack_debug_f8_matmul": ([i64, i32, i32, i32, i32, i32] + [ctypes.POINTER(i32)] * 3, ctypes.c_int),
         "pack_f8_matmul": ([vp, i64, vp, vp, i64, vp, vp, i32, i32, i64, i32, i32, vp, i64, vp, sz, vp], ctypes.c_int),
         "pack_distill_topk": ([vp, i64, i32, i64, i32, vp, vp, i32, f32, vp, vp, vp, i64, vp], ctypes.c_int),
     }
@@ -477,3 +478,12 @@ def stream_copy(src, dst):
     n = src.numel() * src.element_size()
     assert src.is_cuda and dst.is_cuda and dst.numel() * dst.element_size() == n
     _check(load_library().pack_stream_copy(src.data_ptr(), dst.data_ptr(), n, _stream()))
+
+
+def debug_f8_matmul(rows, outputs, depth, gate=None, fp32=False, aligned=True):
+    """How f8_matmul of these sizes is laid out (pack_debug_f8_matmul): (side of its tiles, workgroups that share a
+    tile's depth, whether operands go straight to LDS); host only."""
+    out = [ctypes.c_int32() for _ in range(3)]
+    _check(load_library().pack_debug_f8_matmul(rows, outputs, depth, -1 if gate is None else ACTIVATIONS[gate], int(fp32),
+                                               int(aligned), *[ctypes.byref(o) for o in out]))
+    return out[0].value, out[1].value, bool(out[2].value)
