@@ -1666,9 +1666,17 @@ Plan plan_with(MmType type, const MmArgs& a, Tiles t, int64_t splits) {
 // 0.2 us a tile, small ones in 0.6, huge ones in 1.05 on a few CUs and 1.6 where
 // all of them run (the clock falls under their power); operands through
 // registers take 0.42 and 0.9, half as much again for each that is
-// rows-contiguous; fp32 0.62 and 2.2, through registers 0.7 and 2.45.
+// rows-contiguous; fp32 0.62 and 2.2, through registers 0.7 and 2.45.  8-bit
+// floating point codes that are widened (results in fp32) take 0.315 and 0.88,
+// through registers 0.47 in mini tiles (measured at 256..2048 workgroups, depths
+// 2048 and 8192); their registers do not hold huge tiles, and small ones through
+// registers spill and took 1.93, as much as four mini ones.
+bool widened(MmType type, const MmArgs& a) { return type == MM_F8 && a.out_f32; }
 double step_us(MmType type, const MmArgs& a, Tiles t, bool dma, double wgs) {
   const double held = std::ceil(wgs / 256);
+  if (widened(type, a))
+    return t == TILES_SMALL ? std::max(1.0, 0.88 * held)
+                            : dma ? std::max(0.45, 0.315 * held) : std::max(0.85, 0.47 * held);
   if (t == TILES_HUGE) return wgs < 256 ? 1.05 + 0.55 * wgs / 256 : 1.6 * held;
   if (type == MM_FP32)
     return t == TILES_MINI ? (dma ? std::max(0.75, 0.62 * held) : std::max(0.85, 0.7 * held))
@@ -1696,7 +1704,8 @@ Plan search(MmType type, const MmArgs& a, bool dma) {
   best.us = 1e30;
   if (type != MM_FP32 && !a.a_rmaj && !a.b_rmaj && a.M <= 16) return plan_with(type, a, TILES_THIN, 1);
   for (Tiles t : {TILES_MINI, TILES_SMALL, TILES_HUGE}) {
-    if (t == TILES_HUGE && (!dma || type == MM_FP32)) continue;
+    if (t == TILES_HUGE && (!dma || type == MM_FP32 || widened(type, a))) continue;
+    if (t == TILES_SMALL && !dma && widened(type, a)) continue;
     int64_t last = 0;
     for (int64_t s : kSplits) {
       Plan p = plan_with(type, a, t, s);
@@ -1717,20 +1726,14 @@ Plan choose(MmType type, const MmArgs& a, bool dma) {
     Plan plan;
   };
   static thread_local Memo memo[64];
-  const int32_t kind = 1 + (int)type + 4 * a.epi + 32 * a.a_rmaj + 64 * a.b_rmaj + 128 * (int)dma;  // 0: empty
+  const int32_t kind = 1 + (int)type + 4 * a.epi + 32 * a.a_rmaj + 64 * a.b_rmaj + 128 * (int)dma +
+                       256 * (int)widened(type, a);  // 0: empty
   const uint32_t at = ((uint32_t)a.M * 0x9E3779B1u ^ (uint32_t)a.N * 0x85EBCA77u ^ (uint32_t)a.K * 0xC2B2AE3Du ^
                        (uint32_t)kind * 0x27D4EB2Fu) >> 26;
   Memo& e = memo[at];
   if (e.M != a.M || e.N != a.N || e.K != a.K || e.kind != kind)
     e = Memo{a.M, a.N, a.K, kind, search(type, a, dma)};
   return e.plan;
-}
-
-// What a product is launched with.
-Plan plan_of(MmType type, const MmArgs& a, bool dma) {
-  const Plan p = choose(type, a, dma);
-  // (the registers of the largest tiles do not hold widened codes as well)
-  return type == MM_F8 && a.out_f32 && p.tiles == TILES_HUGE ? plan_with(type, a, TILES_SMALL, 1) : p;
 }
 
 size_t partial_bytes(const MmArgs& a, const Plan& p) {
@@ -1796,7 +1799,7 @@ void launch_join(const MmArgs& a, hipStream_t s) {
 template <typename T, bool RA, bool RB, int EPI>
 hipError_t launch_tiles(MmType type, MmArgs a, hipStream_t s) {
   const bool dma = can_dma(type, a);
-  const Plan p = plan_of(type, a, dma);
+  const Plan p = choose(type, a, dma);
   const dim3 grid(apply(a, p));
   if (grid.x == 0) return hipErrorInvalidConfiguration;
   if (a.work_bytes < partial_bytes(a, p)) return hipErrorInvalidValue;
@@ -1814,7 +1817,8 @@ hipError_t launch_tiles(MmType type, MmArgs a, hipStream_t s) {
   } else if (dma) {
     hipLaunchKernelGGL((small_kernel<T, RA, RB, EPI, true, 1, 4>), grid, dim3(256), 0, s, a);
   } else if (p.tiles == TILES_SMALL) {
-    hipLaunchKernelGGL((small_kernel<T, RA, RB, EPI, false, 2, 2>), grid, dim3(256), 0, s, a);
+    if constexpr (!kWiden<T>)
+      hipLaunchKernelGGL((small_kernel<T, RA, RB, EPI, false, 2, 2>), grid, dim3(256), 0, s, a);
   } else {
     hipLaunchKernelGGL((small_kernel<T, RA, RB, EPI, false, 1, 2>), grid, dim3(256), 0, s, a);
   }
@@ -2030,17 +2034,22 @@ hipError_t launch_one(MmType type, const MmArgs& a, hipStream_t s) {
 
 }  // namespace
 
-// (whatever the operands' alignment turns out to be)
-size_t mm_workspace(MmType type, const MmArgs& a) {
-  Copy c[3];
-  const size_t copied = copies_bytes(type, c, copies(type, a, nullptr, c));
-  return std::max(copied + partial_bytes(a, choose(type, a, true)), partial_bytes(a, choose(type, a, false)));
+// (whatever the operands' alignment turns out to be, and whatever type 8-bit floating point results have)
+size_t mm_workspace(MmType type, const MmArgs& product) {
+  MmArgs a = product;
+  size_t n = 0;
+  for (a.out_f32 = 0; a.out_f32 <= (type == MM_F8); ++a.out_f32) {
+    Copy c[3];
+    const size_t copied = copies_bytes(type, c, copies(type, a, nullptr, c));
+    n = std::max({n, copied + partial_bytes(a, choose(type, a, true)), partial_bytes(a, choose(type, a, false))});
+  }
+  return n;
 }
 
 MmLayout mm_layout(MmType type, const MmArgs& a, bool aligned) {
   Copy c[3];
   const bool dma = copies(type, a, nullptr, c) > 0 || (aligned && !odd_a(type, a) && !odd_b(type, a));
-  const Plan p = plan_of(type, a, dma);
+  const Plan p = choose(type, a, dma);
   constexpr int32_t kSide[] = {16, 64, 128, 256};
   return {kSide[p.tiles], p.splits, dma};
 }

@@ -1,9 +1,9 @@
-"""8-bit floating point products on each kind of tile, the largest ones among them (tests/test_f8_tiles.py holds the sizes to
-the tiles): within the bounds of test_gpu_f8.py, and exactly where sums of whole numbers times powers of two are exact."""
+"""8-bit floating point products on each kind of tile, whole and split depths, straight to LDS and through registers
+(tests/test_f8_tiles.py holds the sizes to the tiles): within the bounds of test_gpu_f8.py, and exactly where sums of whole numbers times powers of two are exact."""
 import pytest
 
 torch = pytest.importorskip("torch")
-from f8_tile_cases import HUGE  # noqa: E402
+from f8_tile_cases import ALL  # noqa: E402
 from paper_2607_05380_amd import ops  # noqa: E402
 from test_gpu_f8 import _check_product, _strided  # noqa: E402
 
@@ -11,14 +11,14 @@ pytestmark = pytest.mark.gpu
 
 
 @pytest.mark.parametrize("bias", [False, True])
-@pytest.mark.parametrize("case,layout", HUGE, ids=str)
+@pytest.mark.parametrize("case,layout", ALL, ids=str)
 def test_product(case, layout, bias):
     print(f"[f8 tiles] {case} on {layout} bias {bias}", flush=True)
     M, N, K, gate, fp32, pad, shift = case
     _check_product(M, N, K, gate, pad, shift, bias, torch.float32 if fp32 else torch.bfloat16)
 
 
-@pytest.mark.parametrize("case,layout", HUGE, ids=str)
+@pytest.mark.parametrize("case,layout", ALL, ids=str)
 def test_exact_sums(case, layout):
     """Codes of -1, 0 and 1 and scales 2^-3 .. 2^3 of their own for each block: sums are multiples of 2^-6, at most 64 a
     product, so below 2^18 at depth 4096 (past it, scales 2^-1 .. 2^1: at most 4 a product): exact in fp32 in any order, and no product
