@@ -106,7 +106,7 @@ struct EmbedBwdArgs {
   const void* dy;         // [tokens, cols]
   void* dtable;           // [rows, cols]
   void* work;             // embed_bwd_bytes()
-  int64_t tokens, rows, ldy, ldt;
+  int64_t tokens, rows, ldy;
   int32_t cols, idx64;
   float scale;
 };
