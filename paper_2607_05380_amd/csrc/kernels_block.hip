@@ -43,8 +43,9 @@
 // multiply-add an element with the row's scale times the columns': 64 of them
 // a step and 64 x 64 block beside 8 MFMAs of 64 cycles, hidden behind them.  8192
 // a side 481 us, 2.28 PFLOP/s (a library product with one scale in all 2.62; whole
-// numbers 440 us), 128 x 128 tiles 567; results in fp32 956 (see f8x_t).  20,011 x
-// 1024 -> 4096 gated 204 us (8 steps a tile of 1.7 us; start and epilogue, which
+// numbers 440 us), 128 x 128 tiles 567; results in fp32 931 (see f8x_t).  128 x 128
+// tiles through registers spill 12 of them.  20,011 x
+// 1024 -> 4096 gated 207 us (8 steps a tile of 1.7 us; start and epilogue, which
 // nothing covers, 7).
 // MFMAs: v_mfma_f32_32x32x16_bf16, v_mfma_i32_32x32x32_i8, v_mfma_f32_32x32x64_f8f6f4,
 // v_mfma_f32_32x32x2_f32, with B as the first operand, so that a lane holds 4
@@ -1163,7 +1164,8 @@ __device__ __forceinline__ void tie(float (&f)[4]) {
 // outputs in bf16 without LDS.  A lane holds the gate and the up sums of columns
 // 8 q + 4 (lane / 32) .. + 3 of row lane % 32 of a 32 x 32 block; two q's results,
 // exchanged between the halves of the wave, are 8 columns of a row in each lane.
-// 20,011 x 1024 -> 4096 gated 204 us, through LDS 214; plain outputs, whose rows have twice the
+// 20,011 x 1024 -> 4096 gated 206.5 us, through LDS 219 (medians 209 and 221; 20
+// times each, in turn on one card, on another one the same); plain outputs, whose rows have twice the
 // bytes and which have nothing to compute, are faster through LDS (20,011 x 1024
 // -> 8192 211 us, this way 218).
 __device__ __forceinline__ void f8_gate_out(const MmArgs& a, const f32x16 (&acc)[2][2][2], int m0, int n0, int lane) {

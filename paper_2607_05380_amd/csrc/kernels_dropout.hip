@@ -4,7 +4,8 @@
 //
 // Element (r, c) takes the 16-bit half c % 2 of word (c / 2) % 4 of the Philox
 // block with counter (c / 8, r, site, step) and is kept if the half is at least
-// floor(p 2^16): the packs' rule, one block for 8 neighbours of a row, which are
+// floor(p 2^16) (so the share kept is 1 - p rounded up to a multiple of 2^-16): the
+// packs' rule, one block for 8 neighbours of a row, which are
 // one or two vectors of a thread.  The draws depend on (r, c) alone, not on how
 // the tensor lies or how threads share it.  A block costs some 90 instructions for
 // 8 elements, close to what their bytes take in HBM, which bounds it: 65,536 x

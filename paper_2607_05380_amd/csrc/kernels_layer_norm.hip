@@ -13,6 +13,10 @@
 // writes), 112 backward (4.8) and 5 for the sums of the weight and bias; 4095 x
 // 1023 fp32, rows at 4 bytes, 13, 17 and 5 us (two rows a thread group at least:
 // with one the partial sums take 3 us more, with four the rows 2).
+// Rows past 8192 columns, which take 1024 threads of 128 registers, spill in the
+// backward pass: 5 to 7 registers up to 16,384 columns (4096 x 16,384 bf16 216 us,
+// its bytes 78), 19 (bf16) and 50 (fp32) past them (2048 x 32,768 fp32 395, 156),
+// there 19 in the fp32 forward pass too (245 us for 207).
 #include "ops_internal.h"
 #include "row_tiles.h"
 #include "../../include/tabpack.h"
