@@ -11,6 +11,11 @@
   python -m paper_2607_05380_amd.profiles_summary counters WORKLOAD OUT.md PMC_DIR... --command "..."
       per-kernel hardware counters of `--pmc` runs (MFMA busy share, wave
       wait states, L2 hit rate and latency, LDS bank conflicts)
+  python -m paper_2607_05380_amd.profiles_summary cases STATS_DIR FETCH_DIR WRITE_DIR OUT.md --command "..."
+      per case (a folder of its name in each of the three): the library kernels'
+      launches and times of a `--kernel-trace --stats` run and the HBM bytes per
+      launch of `--pmc FETCH_SIZE` / `--pmc WRITE_SIZE` runs that also time the
+      library's streaming copy, which scales the counters
   python -m paper_2607_05380_amd.profiles_summary mfma PMC_DIR BENCH_LOG WORKLOAD OUT.md --command "..."
       executed MFMA work per launch of every GEMM kernel from a `--pmc
       SQ_INSTS_VALU_MFMA_MOPS_BF16` (or _F32) run of `bench.py --profile-steps N`
@@ -189,6 +194,49 @@ def per_dispatch(d, counter):
 
 def fmt(x):
     return "n/a" if x is None else f"{x:.3f}"
+
+
+def copy_factor(disp, counter):
+    """Counter bytes per true byte, from the run's streaming copies of COPY_BYTES."""
+    cal = [v for name, v in disp.values() if short_name(name) == "stream_copy" and v * 1024 >= 0.4 * COPY_BYTES]
+    if not cal:
+        sys.exit(f"no calibration stream_copy found in the {counter} run")
+    return statistics.median(cal) * 1024 / COPY_BYTES
+
+
+def cases(args):
+    lines = [f"# Kernel time and HBM traffic by case ({os.path.basename(args.out)[:-3]})", "", "Commands:", "", "```",
+             args.command, "```", "",
+             "Library kernels only, of one case each run; bytes are the counters' per dispatch, scaled by what they read for "
+             "the library's streaming copy of 256 MiB in the same run (bytes that the last-level cache serves are not "
+             "counted).  TB/s: the two together over the kernel's time in the run without counters.", "",
+             "| case | kernel | launches | avg us | fetch MB | write MB | TB/s |", "|---|---|---|---|---|---|---|"]
+    for case in sorted(os.listdir(args.stats)):
+        per, order = {}, []
+        for f in glob.glob(os.path.join(args.stats, case, "**", "*kernel_stats.csv"), recursive=True):
+            with open(f) as fh:
+                for r in csv.DictReader(fh):
+                    name = short_name(r["Name"])
+                    if name and name != "stream_copy":
+                        p = per.setdefault(name, [0, 0.0])
+                        p[0] += int(r["Calls"])
+                        p[1] += float(r["TotalDurationNs"])
+        order = sorted(per, key=lambda k: -per[k][1])
+        if not order:
+            sys.exit(f"no library kernels under {os.path.join(args.stats, case)}")
+        moved = {}
+        for counter, d in (("FETCH_SIZE", args.fetch), ("WRITE_SIZE", args.write)):
+            disp = per_dispatch(os.path.join(d, case), counter)
+            factor = copy_factor(disp, counter)
+            for name, v in disp.values():
+                moved.setdefault((short_name(name), counter), []).append(v * 1024 / factor)
+        for k in order:
+            us = per[k][1] / per[k][0] / 1e3
+            mb = [statistics.mean(moved[(k, c)]) / 1e6 for c in ("FETCH_SIZE", "WRITE_SIZE")]
+            lines.append(f"| {case} | {k} | {per[k][0]} | {us:.1f} | {mb[0]:.2f} | {mb[1]:.2f} | {sum(mb) / us:.2f} |")
+    with open(args.out, "w") as f:
+        f.write("\n".join(lines) + "\n")
+    print("\n".join(lines))
 
 
 def traffic(args):
@@ -372,6 +420,10 @@ def main():
     b.add_argument("workload")
     b.add_argument("out_prefix")
     b.add_argument("--command", default="")
+    d = sub.add_parser("cases")
+    for name in ("stats", "fetch", "write", "out"):
+        d.add_argument(name)
+    d.add_argument("--command", default="")
     c = sub.add_parser("mfma")
     c.add_argument("dir")
     c.add_argument("bench_log")
@@ -388,7 +440,7 @@ def main():
     e.add_argument("--also", nargs="*", default=[])
     e.add_argument("--command", default="")
     args = ap.parse_args()
-    {"stats": stats, "traffic": traffic, "mfma": mfma, "counters": counters}[args.cmd](args)
+    {"stats": stats, "traffic": traffic, "cases": cases, "mfma": mfma, "counters": counters}[args.cmd](args)
 
 
 if __name__ == "__main__":
