@@ -527,9 +527,9 @@ int pack_add_layer_norm(const void* x, int64_t ldx, const void* residual, int64_
                         const float* bias, int32_t precision, int64_t rows, int32_t cols, float eps, void* sum_out,
                         int64_t lds, void* out, int64_t ldo, float* mean_out, float* rstd_out, hipStream_t stream);
 
-/* Its gradients from its sum v, mu and rho as they were stored (so n carries the
- * roundings of v and of mu, 2^-24 |mu| rho of the latter): with
- * n = (v - mu) rho and g = weight dy,
+/* Its gradients from its sum v, mu and rho as they were stored: with
+ * n = (v - mu) rho (PACK_PREC_FP32: less n's own row mean, which is what mu's
+ * rounding left in it) and g = weight dy,
  *   dx = rho (g - sum_c g / cols - n sum_c g n / cols) + dsum   (of x and of the residual)
  *   dweight = sum over the rows of dy n,  dbias = sum over the rows of dy
  *   dsum         the gradient that reaches v on its other path, or NULL

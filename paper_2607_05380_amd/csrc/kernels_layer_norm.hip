@@ -13,10 +13,10 @@
 // writes), 112 backward (4.8) and 5 for the sums of the weight and bias; 4095 x
 // 1023 fp32, rows at 4 bytes, 13, 17 and 5 us (two rows a thread group at least:
 // with one the partial sums take 3 us more, with four the rows 2).
-// Rows past 8192 columns, which take 1024 threads of 128 registers, spill in the
-// backward pass: 5 to 7 registers up to 16,384 columns (4096 x 16,384 bf16 216 us,
-// its bytes 78), 19 (bf16) and 50 (fp32) past them (2048 x 32,768 fp32 395, 156),
-// there 19 in the fp32 forward pass too (245 us for 207).
+// Rows past 8192 columns take 1024 threads of 128 registers: 4096 x 16,384 bf16 122
+// and 210 us (its bytes 104 and 78); past 16,384 in fp32 they spill, 23 registers
+// forward and 45 backward (2048 x 32,768 255 and 422 us, 207 and 156), and the
+// backward pass reads v three times and dy twice.
 #include "ops_internal.h"
 #include "row_tiles.h"
 #include "../../include/tabpack.h"
@@ -24,20 +24,30 @@
 namespace tabpack {
 namespace {
 
-// The sums over a row's G threads of two values, behind one barrier (red, more: as reduce_row's).
-template <int G>
-__device__ __forceinline__ void reduce_row2(float& p, float& q, float* red, float* more, int tid) {
-  if constexpr (G <= 64) {
-    p = reduce_row<G, OpAdd>(p, red, tid);
-    q = reduce_row<G, OpAdd>(q, more, tid);
-  } else {
+// The sums over a row's G threads of N values, behind one barrier (red: N times 16 floats, as reduce_row's).
+template <int G, int N>
+__device__ __forceinline__ void reduce_rows(float (&v)[N], float (*red)[16], int tid) {
 #pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) p += __shfl_xor(p, m, 64), q += __shfl_xor(q, m, 64);
-    if ((tid & 63) == 0) red[tid >> 6] = p, more[tid >> 6] = q;
+  for (int m = (G < 64 ? G : 64) / 2; m >= 1; m >>= 1)
+#pragma unroll
+    for (int q = 0; q < N; ++q) v[q] += __shfl_xor(v[q], m, 64);
+  if constexpr (G > 64) {
+    if ((tid & 63) == 0)
+#pragma unroll
+      for (int q = 0; q < N; ++q) red[q][tid >> 6] = v[q];
     __syncthreads();
-    p = red[0], q = more[0];
 #pragma unroll
-    for (int w = 1; w < G / 64; ++w) p += red[w], q += more[w];
+    for (int q = 0; q < N; ++q) {
+      if constexpr (G == 1024) {  // (16 words of each sum would not fit its registers)
+        v[q] = red[q][tid & 15];
+#pragma unroll
+        for (int m = 8; m >= 1; m >>= 1) v[q] += __shfl_xor(v[q], m, 64);
+      } else {
+        v[q] = red[q][0];
+#pragma unroll
+        for (int w = 1; w < G / 64; ++w) v[q] += red[q][w];
+      }
+    }
   }
 }
 
@@ -108,7 +118,9 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void layer_norm_kernel(LayerNorm
           s1 += d;
           s2 = fmaf(d, d, s2);
         }
-      reduce_row2<G>(s1, s2, red[turn][at], red[turn][at + 1], tid);
+      float both[2] = {s1, s2};
+      reduce_rows<G>(both, &red[turn][at], tid);
+      s1 = both[0], s2 = both[1];
     };
     const float n = (float)a.cols;
     float shift = reduce_row<G, OpAdd>(total, red[turn][0], tid) / n;
@@ -174,6 +186,10 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void layer_norm_kernel(LayerNorm
 //   dx = rstd (g - sum(g) / D - n sum(g n) / D) + dsum,
 //   dweight = sum over the rows of dy n,  dbias = sum over the rows of dy.
 // (n is formed as (v / 2 - mean / 2) 2 rstd, whose difference cannot overflow.)
+// In fp32, where v is stored as the norm took it, n less its own row mean h, what
+// the mean's rounding left in it, stands for n: 2^-24 |mean| rstd, 0.03 for rows of
+// 1e6 +- 1; sum(g (n - h)) = sum(g n) - h sum(g).  (In bf16 v's own rounding counts
+// for more.)  65,536 x 1024 fp32 187 us before, 189 with it, 8192 x 8192 232 and 245.
 // A block walks over rows (gridDim apart) and keeps the columns' two sums in
 // registers; they go to one row of `partial`, and a second kernel adds these up
 // in order: no atomics, so the result does not change between runs.  SUMS false:
@@ -183,7 +199,8 @@ template <typename T, int G, int EPT, bool SUMS>
 __global__ __launch_bounds__(G > 256 ? G : 256) void layer_norm_bwd_kernel(LayerNormBwdArgs a) {
   constexpr int VE = kVec<T>, NT = G > 256 ? G : 256, RPB = NT / G, NV = EPT / VE, NS = SUMS ? EPT : 1;
   constexpr bool LATE = G > 256;  // dsum is read behind the sums (the registers of 1024 threads do not hold it)
-  __shared__ float red[2][2][16];
+  constexpr bool OFF = sizeof(T) == 4;
+  __shared__ float red[2][OFF ? 3 : 2][16];
   __shared__ float cols[RPB > 1 ? 2 * G * EPT : 1];
   const int tid = threadIdx.x, t = tid % G, rg = tid / G;
   float dw[NS], db[NS];
@@ -206,7 +223,7 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void layer_norm_bwd_kernel(Layer
         os[i].raw = u32x4{0, 0, 0, 0};
     }
     const float rho = a.rstd[row], half = -0.5f * a.mean[row], twice = 2.0f * rho;
-    float sg = 0.0f, sgn = 0.0f;
+    float sg = 0.0f, sgn = 0.0f, sn = 0.0f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (i * G + t) * VE;
@@ -218,17 +235,20 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void layer_norm_bwd_kernel(Layer
       for (int e = 0; e < VE; ++e) {  // (behind the row's end g and w are 0)
         const float n = fmaf(v[e], 0.5f, half) * twice;
         if constexpr (SUMS) {
-          dw[i * VE + e] = fmaf(g[e], n, dw[i * VE + e]);
+          if constexpr (!OFF) dw[i * VE + e] = fmaf(g[e], n, dw[i * VE + e]);
           db[i * VE + e] += g[e];
         }
+        if constexpr (OFF) sn += c + e < a.cols ? n : 0.0f;
         g[e] *= w[e];
         sg += g[e];
         sgn = fmaf(g[e], n, sgn);
       }
     }
     const float n = (float)a.cols;
-    reduce_row2<G>(sg, sgn, red[turn][0], red[turn][1], tid);
-    const float c1 = sg / n, c2 = sgn / n;
+    float sums[OFF ? 3 : 2] = {sg, sgn};
+    if constexpr (OFF) sums[2] = sn;
+    reduce_rows<G>(sums, red[turn], tid);
+    const float c1 = sums[0] / n, off = OFF ? sums[OFF ? 2 : 0] / n : 0.0f, c2 = fmaf(-off, c1, sums[1] / n);
     T* dx = static_cast<T*>(a.dx) + row * a.ldx;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -241,7 +261,8 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void layer_norm_bwd_kernel(Layer
       os[i].get(o);
 #pragma unroll
       for (int e = 0; e < VE; ++e) {
-        const float nn = fmaf(v[e], 0.5f, half) * twice;
+        const float nn = fmaf(v[e], 0.5f, half) * twice - off;
+        if constexpr (SUMS && OFF) dw[i * VE + e] = fmaf(g[e], nn, dw[i * VE + e]);
         o[e] = fmaf(rho, (g[e] * w[e] - c1) - nn * c2, o[e]);
       }
       store_vec(dx + c, o, a.cols - c);
@@ -282,6 +303,28 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void layer_norm_bwd_kernel(Layer
   }
 }
 
+// The row means of wide rows' n (fp32).
+__global__ __launch_bounds__(1024) void layer_norm_off_kernel(LayerNormBwdArgs a) {
+  __shared__ float red[2][16];
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+    const float* const s = static_cast<const float*>(a.sum) + row * a.lds;
+    const float half = -0.5f * a.mean[row], twice = 2.0f * a.rstd[row];
+    float sn = 0.0f;
+#pragma unroll 8
+    for (int c = threadIdx.x * 4; c < a.cols; c += 4096) {
+      Vec<float> vs;
+      float v[4];
+      vs.load(s + c, a.cols - c);
+      vs.get(v);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sn += c + e < a.cols ? fmaf(v[e], 0.5f, half) * twice : 0.0f;
+    }
+    sn = reduce_row<1024, OpAdd>(sn, red[turn], threadIdx.x);
+    if (threadIdx.x == 0) a.off[row] = sn / (float)a.cols;
+  }
+}
+
 // The sums of wide rows: a block takes 64 vectors of columns and every gridDim.y-th
 // group of 4 rows.
 template <typename T>
@@ -300,12 +343,13 @@ __global__ __launch_bounds__(256) void layer_norm_cols_kernel(LayerNormBwdArgs a
       vs.load(static_cast<const T*>(a.sum) + row * a.lds + c, a.cols - c);
       gs.load(static_cast<const T*>(a.dy) + row * a.ldy + c, a.cols - c);
       const float half = -0.5f * a.mean[row], twice = 2.0f * a.rstd[row];
+      const float off = sizeof(T) == 4 ? a.off[row] : 0.0f;
       float v[VE], g[VE];
       vs.get(v);
       gs.get(g);
 #pragma unroll
       for (int e = 0; e < VE; ++e) {
-        dw[e] = fmaf(g[e], fmaf(v[e], 0.5f, half) * twice, dw[e]);
+        dw[e] = fmaf(g[e], fmaf(v[e], 0.5f, half) * twice - off, dw[e]);
         db[e] += g[e];
       }
     }
@@ -390,6 +434,8 @@ hipError_t backward_t(const LayerNormBwdArgs& a, hipStream_t s) {
   if (a.cols > kRowMaxCols) return hipErrorInvalidValue;
   // the sums first: dx may take dy's place
   const int columns = 64 * kVec<T>;
+  if (sizeof(T) == 4 && a.rows > 0)
+    hipLaunchKernelGGL(layer_norm_off_kernel, dim3(row_blocks(a.rows, 1)), dim3(1024), 0, s, a);
   hipLaunchKernelGGL((layer_norm_cols_kernel<T>), dim3((a.cols + columns - 1) / columns, nblk), dim3(256), 0, s, a);
   hipLaunchKernelGGL(layer_norm_sums_kernel, sums, dim3(1024), 0, s, a.partial, nblk, a.cols, a.dweight, a.dbias);
   if (a.rows > 0)
@@ -407,6 +453,9 @@ int layer_norm_bwd_blocks(int64_t rows, int32_t cols) {
   const int64_t want = (rows + 31) / 32;
   return (int)(want < 64 ? (want > 0 ? want : 1) : 64);
 }
+
+// Rows past 16,384 columns: a float each.
+int64_t layer_norm_bwd_offs(int64_t rows, int32_t cols) { return cols <= 16384 ? 0 : rows; }
 
 hipError_t launch_layer_norm(int prec, const LayerNormArgs& a, hipStream_t s) {
   return prec == PACK_PREC_BF16 ? forward_t<__bf16>(a, s) : forward_t<float>(a, s);

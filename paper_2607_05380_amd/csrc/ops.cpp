@@ -374,7 +374,7 @@ int pack_layer_norm_backward_workspace_size(int64_t rows, int32_t cols, size_t* 
   if (!bytes) return bad("bytes is NULL");
   const int rc = check_rows(PACK_PREC_FP32, rows, cols);
   if (rc != PACK_OK) return rc;
-  *bytes = (size_t)layer_norm_bwd_blocks(rows, cols) * (size_t)cols * 8;
+  *bytes = (size_t)layer_norm_bwd_blocks(rows, cols) * (size_t)cols * 8 + (size_t)layer_norm_bwd_offs(rows, cols) * 4;
   return PACK_OK;
 }
 
@@ -397,6 +397,7 @@ int pack_layer_norm_backward(const void* dy, int64_t ldy, const void* sum, int64
   a.sum = sum, a.lds = lds, a.dy = dy, a.ldy = ldy, a.dsum = dsum, a.ldd = ldd;
   a.weight = weight, a.mean = mean, a.rstd = rstd, a.dx = dx_out, a.ldx = ldx;
   a.dweight = dweight_out, a.dbias = dbias_out, a.partial = static_cast<float*>(work), a.rows = rows, a.cols = cols;
+  a.off = a.partial + (size_t)layer_norm_bwd_blocks(rows, cols) * (size_t)cols * 2;
   return done("layer norm backward", launch_layer_norm_bwd(precision, a, stream));
 }
 

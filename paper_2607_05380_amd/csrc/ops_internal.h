@@ -72,10 +72,12 @@ struct LayerNormBwdArgs {
   float* dweight;         // [cols]
   float* dbias;           // [cols] or NULL
   float* partial;         // [layer_norm_bwd_blocks(rows, cols), 2 cols]
+  float* off;             // [layer_norm_bwd_offs(rows, cols)]
   int64_t rows, lds, ldy, ldd, ldx;
   int32_t cols;
 };
 int layer_norm_bwd_blocks(int64_t rows, int32_t cols);
+int64_t layer_norm_bwd_offs(int64_t rows, int32_t cols);
 hipError_t launch_layer_norm_bwd(int prec, const LayerNormBwdArgs& a, hipStream_t s);
 
 // Dropout with 16-bit draws: kept where the draw is at least `threshold`.

@@ -42,7 +42,7 @@ SIMPLE = ["dropout_words", "grad_sums", "head_fwd", "head_bwd", "head_train", "g
           "eval_score", "dropout_mask", "select_partial", "select_pick", "select_update", "select_init", "select_final",
           "ensemble_mean", "muon_prep", "muon_norm", "muon_convert", "muon_update", "embed_table", "embed_grad",
           "idx_check", "stream_copy", "norm_bwd", "norm_dw", "copy_rows", "rows", "distill",
-          "layer_norm", "layer_norm_bwd", "layer_norm_cols", "layer_norm_sums", "dropout", "embed", "sort_one",
+          "layer_norm", "layer_norm_bwd", "layer_norm_off", "layer_norm_cols", "layer_norm_sums", "dropout", "embed", "sort_one",
           "sort_count", "sort_scan", "sort_move", "run_sum", "run_join", "row_codes", "tile_codes"]
 # kernels of the student's operators: matrix products by tiles, operand kinds and epilogue, row kernels by mode
 MM_EPIS = ["plain", "gate", "gate_bwd", "q8", "q8_gate", "plain", "gate"]
